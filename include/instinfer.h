@@ -69,6 +69,10 @@ typedef enum {
 /* Bits OR-ed into *status_flags by the kernels. */
 #define INSTINFER_FLAG_SEQ_LEN_RANGE 1  /* seq_lens[b] < 0, beyond the cache capacity, or beyond max_seq_len */
 #define INSTINFER_FLAG_BLOCK_RANGE   2  /* a block_table entry that had to be read lies outside [0, num_phys_blocks) */
+#define INSTINFER_FLAG_TREE_RANGE    16 /* draft trees: a tree length, parent, token or path outside its range, or a
+                                           distribution without a positive value */
+#define INSTINFER_FLAG_POOL          32 /* block pools: too few free blocks, an impossible fork, or reference counts that
+                                           do not fit the tables */
 #define INSTINFER_FLAG_BOUNDS_CHECK  8  /* only in the bounds-checking build of the library (compiled with
                                            -DINSTINFER_BOUNDS_CHECK): a kernel computed a global offset outside the
                                            extent that the call's shapes imply and skipped that access; a defect of
@@ -249,6 +253,185 @@ int instinfer_decode_attention_grouped(void *out, float *lse, const void *q, con
 
 size_t instinfer_grouped_workspace_bytes(int32_t batch, int32_t q_tokens, int32_t q_heads,
                                          int32_t kv_heads, int32_t head_dim, int32_t max_seq_len);
+
+/*
+ * ---- Speculative decoding: several drafted tokens per sequence and step ----
+ * (No counterpart in the paper, whose decode phase adds one token per step, Sec. II-B; the work
+ * stays its Logit / Attend operators, Sec. III-B, over the same cache.)
+ *
+ * A draft tree has tree_lens[b] nodes (0 <= tree_lens[b] <= tree_tokens; tree_lens == NULL:
+ * tree_tokens each).  Node 0 is its root, the newest token that is certain; a node comes after
+ * its parent.  The caches hold all nodes behind the sequence's other tokens, node j at position
+ * seq_lens[b] - tree_lens[b] + j (append them with instinfer_kv_append_bulk); seq_lens[b] counts
+ * them.  One step is: make room (instinfer_kv_resize), append, instinfer_tree_mask once, in every
+ * layer instinfer_decode_attention_tree, then instinfer_verify_tree, instinfer_kv_keep_path, and
+ * instinfer_kv_resize to the kept length.
+ * Limit (INSTINFER_ERR_UNSUPPORTED otherwise): tree_tokens <= INSTINFER_MAX_TREE_TOKENS.
+ */
+#define INSTINFER_MAX_TREE_TOKENS 128
+
+/*
+ * Which nodes a node sees: itself and its ancestors.
+ *   tree_mask  uint64 [batch, tree_tokens, W], W = (tree_tokens + 63) / 64: bit j % 64 of word
+ *              j / 64 of row t is set if node t sees node j; rows from tree_lens[b] on are 0
+ *   parents    int32 [batch, tree_tokens]: parents[b][t] < t, -1 for a root.  Any other value is
+ *              flagged (INSTINFER_FLAG_TREE_RANGE) and taken for -1; a tree_lens[b] out of range
+ *              is flagged and taken for 0.
+ */
+int instinfer_tree_mask(uint64_t *tree_mask, const int32_t *parents, const int32_t *tree_lens,
+                        int32_t batch, int32_t tree_tokens, int32_t *status_flags, void *cuda_stream);
+
+/*
+ * Attention of a tree of drafted tokens over the cache: node t of sequence b attends to every
+ * position before the tree and to the nodes whose bits its row of tree_mask has (any mask will do;
+ * bits of nodes from tree_lens[b] on are ignored).
+ *   q, out     fp16 [batch, tree_tokens, q_heads, head_dim]; grouped heads as in
+ *              instinfer_decode_attention_grouped
+ *   lse        nullable fp32 [batch, tree_tokens, q_heads]
+ *   caches     as for instinfer_decode_attention_grouped (block_table == NULL: contiguous)
+ *   tree_mask  as instinfer_tree_mask writes it, 16-byte aligned
+ *   workspace  at least instinfer_tree_workspace_bytes(...) bytes
+ * Rows of nodes from tree_lens[b] on, rows that see nothing, and all rows of a sequence with
+ * seq_lens[b] == 0 are zero with lse = -inf.  A tree_lens[b] out of range or above seq_lens[b] is
+ * flagged (INSTINFER_FLAG_TREE_RANGE) and makes the sequence inactive.  What a row does not see
+ * never influences it, infinities and NaN in hidden nodes' keys and values included; a NaN that
+ * it sees makes the row NaN.
+ * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): head_dim in {64, 128, 256}; paged block_tokens a
+ * multiple of 16; (q_heads / kv_heads) * tree_tokens <= INSTINFER_MAX_TREE_ROWS.
+ */
+#define INSTINFER_MAX_TREE_ROWS 4096
+int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const void *k_cache,
+                                    const void *v_cache, const int32_t *block_table,
+                                    const int32_t *seq_lens, const int32_t *tree_lens,
+                                    const uint64_t *tree_mask, int32_t batch, int32_t tree_tokens,
+                                    int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                    int32_t s_max, int32_t block_tokens,
+                                    int32_t max_blocks_per_seq, int64_t num_phys_blocks,
+                                    int32_t max_seq_len, float scale, void *workspace,
+                                    size_t workspace_bytes, int32_t *status_flags,
+                                    void *cuda_stream);
+
+size_t instinfer_tree_workspace_bytes(int32_t batch, int32_t tree_tokens, int32_t q_heads,
+                                      int32_t kv_heads, int32_t head_dim, int32_t max_seq_len);
+
+/*
+ * Verification of a draft tree against the target's probabilities from given random numbers
+ * (recursive rejection sampling).  With p_v and q_v the target's and the draft's distribution after
+ * node v, the walk starts at the root; at a node v, w = p_v and Z = 1, and v's children c are tried
+ * in index order: c is taken if
+ *     uniforms[b][c] * q_v(token_c) * Z < w(token_c),
+ * and the walk goes on at c; otherwise w <- max(w - Z q_v, 0) and Z <- sum w (if that sum is 0, w
+ * and Z stay as they were).  When no child is taken the next token is the lowest i with
+ * w_0 + ... + w_i > uniforms[b][0] * sum w.  If v's children were drawn independently from q_v the
+ * emitted tokens have the target's distribution.  Computed in 64 bits.
+ *   path        int32 [batch, tree_tokens]: the nodes taken, ascending, the root first; -1 behind
+ *   path_lens   int32 [batch]: how many, 0 for a sequence without a tree
+ *   out_tokens  int32 [batch, tree_tokens]: the tokens of path[1 ..], then the next token; -1 behind
+ *   target_probs, draft_probs  probs_type [batch, tree_tokens, vocab], row t the distributions
+ *               after node t, rows row_stride >= vocab elements apart, 16-byte aligned (rows need not
+ *               be).  Not normalised here; a value that is not positive and finite counts as 0.
+ *               draft_probs == NULL: drafts that were not sampled (q_v is one-hot at token_c).
+ *   tokens, parents  int32 [batch, tree_tokens]; a node (other than the root) whose parent is not
+ *               an earlier node or whose token is outside [0, vocab) is flagged
+ *               (INSTINFER_FLAG_TREE_RANGE) and never taken
+ *   uniforms    fp32 [batch, tree_tokens] in [0, 1)
+ * If w has no positive value the next token is -1, flagged.
+ */
+#define INSTINFER_F32 0
+#define INSTINFER_F16 1
+#define INSTINFER_BF16 2
+int instinfer_verify_tree(int32_t *path, int32_t *path_lens, int32_t *out_tokens,
+                          const void *target_probs, const void *draft_probs, int32_t probs_type,
+                          int64_t row_stride, const int32_t *tokens, const int32_t *parents,
+                          const int32_t *tree_lens, const float *uniforms, int32_t batch,
+                          int32_t tree_tokens, int32_t vocab, int32_t *status_flags,
+                          void *cuda_stream);
+
+/*
+ * Keeps the accepted path of a draft tree in the caches of all layers: the K and V rows of node
+ * path[b][i] move from position P + path[b][i] to P + i, P = seq_lens[b] - tree_lens[b], for
+ * i < path_lens[b], and new_lens[b] = P + path_lens[b].  Bit copies; only those rows change.
+ *   k_caches, v_caches  HOST arrays of n_layers DEVICE pointers, read during the call only; all
+ *              layers have the same shape and share seq_lens and block_table
+ *   path       ascending node numbers (as instinfer_verify_tree writes them)
+ *   new_lens   int32 [batch], a buffer of its own (not seq_lens)
+ * Layout selection and the other arguments as in instinfer_kv_append.  A path or tree out of range
+ * is flagged (INSTINFER_FLAG_TREE_RANGE, or INSTINFER_FLAG_SEQ_LEN_RANGE for the length), the
+ * sequence is left alone and new_lens[b] = seq_lens[b].  n_layers <= INSTINFER_MAX_LAYERS.
+ */
+#define INSTINFER_MAX_LAYERS 128
+int instinfer_kv_keep_path(void *const *k_caches, void *const *v_caches, int32_t n_layers,
+                           const int32_t *path, const int32_t *path_lens, const int32_t *tree_lens,
+                           const int32_t *seq_lens, int32_t *new_lens, const int32_t *block_table,
+                           int32_t max_blocks_per_seq, int32_t block_tokens, int64_t num_phys_blocks,
+                           int32_t batch, int32_t tree_tokens, int32_t heads, int32_t head_dim,
+                           int32_t s_max, int32_t *status_flags, void *cuda_stream);
+
+/*
+ * ---- Blocks of a paged pool that sequences share ----
+ * The state of a pool is block_refs, int32 [num_phys_blocks]: how many sequences' tables list a
+ * block, 0 for a free one.  Sequence b lists the blocks of its seq_lens[b] tokens, the first
+ * (seq_lens[b] + block_tokens - 1) / block_tokens entries of its row of block_table.  The three
+ * calls below keep both in step; all are deterministic (an allocation takes the lowest free ids).
+ * They must not run at the same time on one pool.  Arguments as in instinfer_kv_append, layers'
+ * pools as in instinfer_kv_keep_path.
+ * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): batch <= 8192, batch * max_blocks_per_seq <= 2^28,
+ * n_layers <= INSTINFER_MAX_LAYERS, head_dim in {64, 128, 256}.
+ *
+ * instinfer_kv_fork: sequence dst[i] (empty: length 0) becomes a copy of src[i] that shares all of
+ * its blocks, the partly filled last one included; nothing is copied but table entries.
+ *   src, dst   int32 [n_forks], device; n_forks <= batch.  One source may be forked many times; a
+ *              destination may be listed once (later ones are flagged and skipped) and may not be
+ *              a source (flagged and skipped).  INSTINFER_FLAG_POOL; a destination that is not empty:
+ *              INSTINFER_FLAG_SEQ_LEN_RANGE, skipped.
+ */
+int instinfer_kv_fork(int32_t *block_table, int32_t *block_refs, int32_t *seq_lens,
+                      const int32_t *src, const int32_t *dst, int32_t n_forks,
+                      int32_t max_blocks_per_seq, int32_t block_tokens, int64_t num_phys_blocks,
+                      int32_t batch, int32_t *status_flags, void *cuda_stream);
+
+/*
+ * instinfer_kv_resize: sequence b goes from seq_lens[b] to want_lens[b] tokens (0 frees it).  First
+ * shorter sequences give blocks back, then growing ones get blocks, in the order of b.  A growing
+ * sequence whose last block is partly filled and also listed by others gets a copy of that block in
+ * all layers (copy on write: it is going to write there); if all that list it grow in this call, the
+ * last of them keeps the original.  So after the call positions seq_lens[b] .. want_lens[b] - 1 can
+ * be appended to without touching another sequence.
+ *   new_lens   int32 [batch]: want_lens[b], or seq_lens[b] where the sequence was left as it is; may
+ *              be seq_lens or want_lens itself
+ * When the free blocks do not suffice for a sequence, it and every later one that needs blocks (or
+ * that would keep a shared block) is left as it is, flagged INSTINFER_FLAG_POOL.  Lengths outside
+ * [0, max_blocks_per_seq * block_tokens] are flagged and left.
+ *   workspace  at least instinfer_kv_resize_workspace_bytes(batch, num_phys_blocks) bytes
+ */
+int instinfer_kv_resize(void *const *k_pools, void *const *v_pools, int32_t n_layers,
+                        int32_t *block_table, int32_t *block_refs, const int32_t *seq_lens,
+                        const int32_t *want_lens, int32_t *new_lens, int32_t max_blocks_per_seq,
+                        int32_t block_tokens, int64_t num_phys_blocks, int32_t batch, int32_t heads,
+                        int32_t head_dim, void *workspace, size_t workspace_bytes,
+                        int32_t *status_flags, void *cuda_stream);
+
+size_t instinfer_kv_resize_workspace_bytes(int32_t batch, int64_t num_phys_blocks);
+
+/*
+ * instinfer_kv_defragment: the U blocks in use get the ids 0 .. U-1: those with an id of U or more, in
+ * ascending order, are copied (in all layers) to the free ids below U, in ascending order; the others
+ * stay.  Tables and counts are written to new_block_table [batch, max_blocks_per_seq] and
+ * new_block_refs [num_phys_blocks] (which may be block_table and block_refs themselves; entries
+ * behind a sequence's last block are copied as they are), *blocks_used = U (device).  Blocks from U
+ * on are free afterwards.
+ *   workspace  at least instinfer_kv_defragment_workspace_bytes(num_phys_blocks) bytes
+ */
+int instinfer_kv_defragment(void *const *k_pools, void *const *v_pools, int32_t n_layers,
+                            const int32_t *block_table, int32_t *new_block_table,
+                            const int32_t *block_refs, int32_t *new_block_refs,
+                            const int32_t *seq_lens, int32_t *blocks_used,
+                            int32_t max_blocks_per_seq, int32_t block_tokens,
+                            int64_t num_phys_blocks, int32_t batch, int32_t heads, int32_t head_dim,
+                            void *workspace, size_t workspace_bytes, int32_t *status_flags,
+                            void *cuda_stream);
+
+size_t instinfer_kv_defragment_workspace_bytes(int64_t num_phys_blocks);
 
 /*
  * One whole decode step for a caller whose new vectors live in host memory (the paper's

@@ -18,6 +18,8 @@ LIBRARY = Path(os.environ.get("INSTINFER_LIBRARY") or Path(__file__).resolve().p
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA = range(5)
 FLAG_SEQ_LEN_RANGE, FLAG_BLOCK_RANGE, FLAG_COPY_TIMEOUT, FLAG_BOUNDS_CHECK = 1, 2, 4, 8
+FLAG_TREE_RANGE, FLAG_POOL = 16, 32
+MAX_TREE_TOKENS, MAX_TREE_ROWS, MAX_LAYERS = 128, 4096, 128
 STATIC_WORKSPACE_BYTES = 16 << 20
 
 _lib: Optional[ctypes.CDLL] = None
@@ -68,6 +70,32 @@ def load() -> ctypes.CDLL:
                                                            i64, i32, f32, ptr, sz, ptr, ptr]
         lib.instinfer_grouped_workspace_bytes.restype = sz
         lib.instinfer_grouped_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+        lib.instinfer_tree_mask.restype = ctypes.c_int
+        lib.instinfer_tree_mask.argtypes = [ptr, ptr, ptr, i32, i32, ptr, ptr]
+        lib.instinfer_decode_attention_tree.restype = ctypes.c_int
+        lib.instinfer_decode_attention_tree.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr,
+                                                        i32, i32, i32, i32, i32, i32, i32, i32,
+                                                        i64, i32, f32, ptr, sz, ptr, ptr]
+        lib.instinfer_tree_workspace_bytes.restype = sz
+        lib.instinfer_tree_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+        lib.instinfer_verify_tree.restype = ctypes.c_int
+        lib.instinfer_verify_tree.argtypes = [ptr, ptr, ptr, ptr, ptr, i32, i64, ptr, ptr, ptr, ptr,
+                                              i32, i32, i32, ptr, ptr]
+        lib.instinfer_kv_keep_path.restype = ctypes.c_int
+        lib.instinfer_kv_keep_path.argtypes = [ptr, ptr, i32, ptr, ptr, ptr, ptr, ptr, ptr, i32, i32, i64,
+                                               i32, i32, i32, i32, i32, ptr, ptr]
+        lib.instinfer_kv_fork.restype = ctypes.c_int
+        lib.instinfer_kv_fork.argtypes = [ptr, ptr, ptr, ptr, ptr, i32, i32, i32, i64, i32, ptr, ptr]
+        lib.instinfer_kv_resize.restype = ctypes.c_int
+        lib.instinfer_kv_resize.argtypes = [ptr, ptr, i32, ptr, ptr, ptr, ptr, ptr, i32, i32, i64, i32, i32,
+                                            i32, ptr, sz, ptr, ptr]
+        lib.instinfer_kv_resize_workspace_bytes.restype = sz
+        lib.instinfer_kv_resize_workspace_bytes.argtypes = [i32, i64]
+        lib.instinfer_kv_defragment.restype = ctypes.c_int
+        lib.instinfer_kv_defragment.argtypes = [ptr, ptr, i32, ptr, ptr, ptr, ptr, ptr, ptr, i32, i32, i64,
+                                                i32, i32, i32, ptr, sz, ptr, ptr]
+        lib.instinfer_kv_defragment_workspace_bytes.restype = sz
+        lib.instinfer_kv_defragment_workspace_bytes.argtypes = [i64]
         lib.instinfer_decode_step_host.restype = ctypes.c_int
         lib.instinfer_decode_step_host.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr,
                                                    i32, i32, i64, i32, i32, i32, i32, i32, f32,
@@ -300,6 +328,150 @@ def decode_attention_grouped(out: torch.Tensor, lse: Optional[torch.Tensor], q: 
         _ptr(seq_lens), batch, q_tokens, q_heads, kv_heads, head_dim, s_max, block_tokens,
         max_blocks, phys, int(max_seq_len), float(scale), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _ptr(status_flags), _stream(stream)))
+
+
+def tree_mask(mask: torch.Tensor, parents: torch.Tensor, tree_lens: Optional[torch.Tensor] = None,
+              status_flags: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_tree_mask: mask int64 [B, T, ceil(T / 64)] (the bits of the header's uint64 words),
+    parents int32 [B, T], tree_lens int32 [B] (None: T nodes each)."""
+    batch, tree_tokens = parents.shape
+    _check(load().instinfer_tree_mask(_ptr(mask), _ptr(parents), _ptr(tree_lens), batch, tree_tokens,
+                                      _ptr(status_flags), _stream(stream)))
+
+
+def tree_workspace_bytes(batch: int, tree_tokens: int, q_heads: int, kv_heads: int, head_dim: int,
+                         max_seq_len: int) -> int:
+    return int(load().instinfer_tree_workspace_bytes(batch, tree_tokens, q_heads, kv_heads, head_dim, max_seq_len))
+
+
+def decode_attention_tree(out: torch.Tensor, lse: Optional[torch.Tensor], q: torch.Tensor,
+                          k_cache: torch.Tensor, v_cache: torch.Tensor,
+                          block_table: Optional[torch.Tensor], seq_lens: torch.Tensor,
+                          tree_lens: Optional[torch.Tensor], mask: torch.Tensor, max_seq_len: int,
+                          scale: float, workspace: torch.Tensor,
+                          status_flags: Optional[torch.Tensor] = None,
+                          stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_decode_attention_tree: q, out [B, T, Hq, D]; mask as tree_mask writes it; caches
+    with Hkv heads ([B,Hkv,s_max,D], or pools [P,Hkv,T,D] with block_table)."""
+    batch, tree_tokens, q_heads, head_dim = q.shape
+    kv_heads = k_cache.shape[1]
+    if block_table is None:
+        s_max, block_tokens, max_blocks, phys = k_cache.shape[2], 0, 0, 0
+    else:
+        s_max, block_tokens, max_blocks, phys = (0, k_cache.shape[2], block_table.shape[1],
+                                                 k_cache.shape[0])
+    _check(load().instinfer_decode_attention_tree(
+        _ptr(out), _ptr(lse), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens),
+        _ptr(tree_lens), _ptr(mask), batch, tree_tokens, q_heads, kv_heads, head_dim, s_max, block_tokens,
+        max_blocks, phys, int(max_seq_len), float(scale), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _ptr(status_flags), _stream(stream)))
+
+
+_PROBS_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.Tensor,
+                target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor], tokens: torch.Tensor,
+                parents: torch.Tensor, tree_lens: Optional[torch.Tensor], uniforms: torch.Tensor,
+                status_flags: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_verify_tree: target_probs, draft_probs (None: drafts that were not sampled) fp32,
+    fp16 or bf16 [B, T, V] with rows at one stride (a padded vocabulary sliced to V will do); the
+    other tensors [B, T], path_lens and tree_lens [B]."""
+    batch, tree_tokens, vocab = target_probs.shape
+    stride = target_probs.stride(1) if tree_tokens > 1 else max(vocab, target_probs.stride(0))
+    for probs in (target_probs, draft_probs):
+        if probs is not None and (
+                probs.dtype != target_probs.dtype or probs.shape != target_probs.shape or
+                (vocab > 1 and probs.stride(2) != 1) or (tree_tokens > 1 and probs.stride(1) != stride) or
+                (batch > 1 and probs.stride(0) != tree_tokens * stride)):
+            raise InstInferError(ERR_INVALID_ARG)
+    if target_probs.dtype not in _PROBS_TYPES:
+        raise InstInferError(ERR_UNSUPPORTED)
+    _check(load().instinfer_verify_tree(
+        _ptr(path), _ptr(path_lens), _ptr(out_tokens), _ptr(target_probs), _ptr(draft_probs),
+        _PROBS_TYPES[target_probs.dtype], stride, _ptr(tokens), _ptr(parents), _ptr(tree_lens),
+        _ptr(uniforms), batch, tree_tokens, vocab, _ptr(status_flags), _stream(stream)))
+
+
+def _layers(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor]):
+    """The two HOST pointer arrays of the calls that work on all layers at once."""
+    if len(k_caches) != len(v_caches) or not k_caches:
+        raise InstInferError(ERR_INVALID_ARG)
+    shape = k_caches[0].shape
+    if any(c.shape != shape or not c.is_contiguous() for c in (*k_caches, *v_caches)):
+        raise InstInferError(ERR_INVALID_ARG)
+    array = ctypes.c_void_p * len(k_caches)
+    return array(*(c.data_ptr() for c in k_caches)), array(*(c.data_ptr() for c in v_caches)), len(k_caches)
+
+
+def kv_keep_path(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor], path: torch.Tensor,
+                 path_lens: torch.Tensor, tree_lens: Optional[torch.Tensor], seq_lens: torch.Tensor,
+                 new_lens: torch.Tensor, block_table: Optional[torch.Tensor] = None,
+                 status_flags: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_kv_keep_path: one cache per layer ([B,H,s_max,D], or pools [P,H,T,D] with
+    block_table); path [B, tree_tokens]."""
+    batch, tree_tokens = path.shape
+    k, v, n_layers = _layers(k_caches, v_caches)
+    _, heads, rows, head_dim = k_caches[0].shape
+    if block_table is None:
+        max_blocks, block_tokens, phys, s_max = 0, 0, 0, rows
+    else:
+        max_blocks, block_tokens, phys, s_max = block_table.shape[1], rows, k_caches[0].shape[0], 0
+    _check(load().instinfer_kv_keep_path(
+        k, v, n_layers, _ptr(path), _ptr(path_lens), _ptr(tree_lens), _ptr(seq_lens), _ptr(new_lens),
+        _ptr(block_table), max_blocks, block_tokens, phys, batch, tree_tokens, heads, head_dim, s_max,
+        _ptr(status_flags), _stream(stream)))
+
+
+def kv_fork(block_table: torch.Tensor, block_refs: torch.Tensor, seq_lens: torch.Tensor, src: torch.Tensor,
+            dst: torch.Tensor, block_tokens: int, status_flags: Optional[torch.Tensor] = None,
+            stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_kv_fork: block_table [B, M], block_refs [P], seq_lens [B], src and dst [n]."""
+    batch, max_blocks = block_table.shape
+    _check(load().instinfer_kv_fork(_ptr(block_table), _ptr(block_refs), _ptr(seq_lens), _ptr(src), _ptr(dst),
+                                    src.numel(), max_blocks, int(block_tokens), block_refs.numel(), batch,
+                                    _ptr(status_flags), _stream(stream)))
+
+
+def kv_resize_workspace_bytes(batch: int, num_phys_blocks: int) -> int:
+    return int(load().instinfer_kv_resize_workspace_bytes(batch, num_phys_blocks))
+
+
+def kv_resize(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tensor], block_table: torch.Tensor,
+              block_refs: torch.Tensor, seq_lens: torch.Tensor, want_lens: torch.Tensor, new_lens: torch.Tensor,
+              workspace: torch.Tensor, status_flags: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_kv_resize: one pool [P,H,T,D] per layer; new_lens may be seq_lens."""
+    batch, max_blocks = block_table.shape
+    k, v, n_layers = _layers(k_pools, v_pools)
+    phys, heads, block_tokens, head_dim = k_pools[0].shape
+    _check(load().instinfer_kv_resize(
+        k, v, n_layers, _ptr(block_table), _ptr(block_refs), _ptr(seq_lens), _ptr(want_lens), _ptr(new_lens),
+        max_blocks, block_tokens, phys, batch, heads, head_dim, _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _ptr(status_flags), _stream(stream)))
+
+
+def kv_defragment_workspace_bytes(num_phys_blocks: int) -> int:
+    return int(load().instinfer_kv_defragment_workspace_bytes(num_phys_blocks))
+
+
+def kv_defragment(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tensor], block_table: torch.Tensor,
+                  block_refs: torch.Tensor, seq_lens: torch.Tensor, new_block_table: torch.Tensor,
+                  new_block_refs: torch.Tensor, blocks_used: torch.Tensor, workspace: torch.Tensor,
+                  status_flags: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_kv_defragment: one pool [P,H,T,D] per layer; the new table and counts may be the
+    old ones; blocks_used int32 [1]."""
+    batch, max_blocks = block_table.shape
+    k, v, n_layers = _layers(k_pools, v_pools)
+    phys, heads, block_tokens, head_dim = k_pools[0].shape
+    _check(load().instinfer_kv_defragment(
+        k, v, n_layers, _ptr(block_table), _ptr(new_block_table), _ptr(block_refs), _ptr(new_block_refs),
+        _ptr(seq_lens), _ptr(blocks_used), max_blocks, block_tokens, phys, batch, heads, head_dim,
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status_flags), _stream(stream)))
 
 
 def decode_step_host(out_host: torch.Tensor, qkv_host: torch.Tensor, qkv_dev: torch.Tensor,

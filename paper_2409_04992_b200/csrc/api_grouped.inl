@@ -30,14 +30,14 @@ size_t grouped_workspace_for(int64_t pairs, int32_t rows, int32_t head_dim, cons
     return (floats * sizeof(float) + 255) / 256 * 256 + 256;
 }
 
-template <int D, bool kPaged>
+template <int D, bool kPaged, bool kTree = false>
 int launch_grouped(const GroupedParams &p, unsigned grid, cudaStream_t stream)
 {
     static bool done[kMaxDevices] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return INSTINFER_ERR_CUDA;
     if (!done[dev]) {
-        if (cudaFuncSetAttribute(grouped_attn_split_kernel<D, kPaged>,
+        if (cudaFuncSetAttribute(grouped_attn_split_kernel<D, kPaged, kTree>,
                                  cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  GroupedGeometry<D>::kSmemBytes) != cudaSuccess) {
             (void)cudaGetLastError();
@@ -45,11 +45,11 @@ int launch_grouped(const GroupedParams &p, unsigned grid, cudaStream_t stream)
         }
         done[dev] = true;
     }
-    cudaError_t err = launch_overlapped(grouped_attn_split_kernel<D, kPaged>, grid, kThreads,
+    cudaError_t err = launch_overlapped(grouped_attn_split_kernel<D, kPaged, kTree>, grid, kThreads,
                                         GroupedGeometry<D>::kSmemBytes, stream, p);
     if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) return INSTINFER_ERR_CUDA;
     if (p.a.n_splits > 1) {
-        err = launch_overlapped(grouped_merge_kernel<D>, (unsigned)(p.a.pairs * p.rows), D, 0, stream, p);
+        err = launch_overlapped(grouped_merge_kernel<D, kTree>, (unsigned)(p.a.pairs * p.rows), D, 0, stream, p);
         if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) return INSTINFER_ERR_CUDA;
     }
     return INSTINFER_OK;
@@ -144,7 +144,7 @@ int launch_grouped_umma(const GroupedParams &p, unsigned *ticket, const CUtensor
                                         UmmaGeometry<D>::kSmemBytes, stream, p, ticket, map_q, map_k, map_v);
     if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) return INSTINFER_ERR_CUDA;
     if (p.a.n_splits > 1) {
-        err = launch_overlapped(grouped_merge_kernel<D>, (unsigned)(p.a.pairs * p.rows), D, 0, stream, p);
+        err = launch_overlapped(grouped_merge_kernel<D, false>, (unsigned)(p.a.pairs * p.rows), D, 0, stream, p);
         if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) return INSTINFER_ERR_CUDA;
     }
     return INSTINFER_OK;

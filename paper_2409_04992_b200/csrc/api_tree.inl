@@ -1,0 +1,105 @@
+// C ABI, attention of a tree of drafted tokens over the cache: checks, plan and launches.
+// Included by instinfer_api.cu after api_grouped.inl, whose planner rules it shares.
+
+namespace {
+
+static_assert(kMaxTreeTokens == INSTINFER_MAX_TREE_TOKENS, "limit of the header");
+
+int tree_attention_shape(int32_t batch, int32_t tree_tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                         int32_t max_seq_len)
+{
+    if (head_dim <= 0 || tree_tokens <= 0 || q_heads <= 0 || kv_heads <= 0 || q_heads % kv_heads != 0 ||
+        !sizes_ok(batch, kv_heads, max_seq_len))
+        return INSTINFER_ERR_INVALID_ARG;
+    if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || tree_tokens > kMaxTreeTokens ||
+        (int64_t)(q_heads / kv_heads) * tree_tokens > INSTINFER_MAX_TREE_ROWS)
+        return INSTINFER_ERR_UNSUPPORTED;
+    return INSTINFER_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const void *k_cache, const void *v_cache,
+                                    const int32_t *block_table, const int32_t *seq_lens, const int32_t *tree_lens,
+                                    const uint64_t *tree_mask, int32_t batch, int32_t tree_tokens, int32_t q_heads,
+                                    int32_t kv_heads, int32_t head_dim, int32_t s_max, int32_t block_tokens,
+                                    int32_t max_blocks_per_seq, int64_t num_phys_blocks, int32_t max_seq_len,
+                                    float scale, void *workspace, size_t workspace_bytes, int32_t *status_flags,
+                                    void *cuda_stream)
+{
+    const bool paged = block_table != nullptr;
+    int rc = tree_attention_shape(batch, tree_tokens, q_heads, kv_heads, head_dim, max_seq_len);
+    if (rc != INSTINFER_OK) return rc;
+    if (!std::isfinite(scale)) return INSTINFER_ERR_INVALID_ARG;
+    if (paged) {
+        if (block_tokens <= 0 || max_blocks_per_seq <= 0 || num_phys_blocks <= 0 ||
+            (int64_t)max_seq_len > (int64_t)max_blocks_per_seq * block_tokens)
+            return INSTINFER_ERR_INVALID_ARG;
+        if (block_tokens % kGroupTile != 0) return INSTINFER_ERR_UNSUPPORTED;
+    } else if (s_max <= 0 || max_seq_len > s_max) {
+        return INSTINFER_ERR_INVALID_ARG;
+    }
+    if (batch == 0) return INSTINFER_OK;
+    if (!usable(out) || !usable(q) || !usable(k_cache) || !usable(v_cache) || !usable(tree_mask) || seq_lens == nullptr)
+        return INSTINFER_ERR_INVALID_ARG;
+
+    const int64_t pairs = (int64_t)batch * kv_heads;
+    GroupedParams p = {};
+    p.group = q_heads / kv_heads;
+    p.q_tokens = tree_tokens;
+    p.rows = p.group * tree_tokens;
+    p.row_groups = (p.rows + kGroupRows - 1) / kGroupRows;
+    p.tree.mask = tree_mask;
+    p.tree.lens = tree_lens;
+    p.tree.tokens = tree_tokens;
+    p.tree.words = (tree_tokens + 63) / 64;
+    const SplitPlan plan = make_plan(pairs * p.row_groups, max_seq_len, grouped_rules(head_dim));
+    if (workspace == nullptr || !aligned16(workspace) ||
+        workspace_bytes < grouped_workspace_for(pairs, p.rows, head_dim, plan))
+        return INSTINFER_ERR_WORKSPACE;
+    const int64_t grid = pairs * plan.n_splits * p.row_groups;
+    if (grid >= (int64_t)1 << 31 || pairs * p.rows >= (int64_t)1 << 31) return INSTINFER_ERR_INVALID_ARG;
+    p.a.q = static_cast<const __half *>(q);
+    p.a.k = static_cast<const __half *>(k_cache);
+    p.a.v = static_cast<const __half *>(v_cache);
+    p.a.seq_lens = seq_lens;
+    p.a.block_table = block_table;
+    p.a.out = static_cast<__half *>(out);
+    p.a.lse = lse;
+    p.a.status = status_flags;
+    p.a.num_phys_blocks = paged ? num_phys_blocks : 0;
+    p.a.heads = kv_heads;
+    p.a.pairs = (int32_t)pairs;
+    p.a.s_max = paged ? 0 : s_max;
+    p.a.block_tokens = paged ? block_tokens : 0;
+    p.a.max_blocks_per_seq = paged ? max_blocks_per_seq : 0;
+    p.a.chunk_tokens = plan.chunk_tokens;
+    p.a.n_big = plan.n_big;
+    p.a.tail_chunk = plan.tail_chunk;
+    p.a.n_splits = plan.n_splits;
+    p.a.max_seq_len = max_seq_len;
+    p.a.kv_bytes = (paged ? num_phys_blocks * kv_heads * block_tokens : (int64_t)batch * kv_heads * s_max) * head_dim * 2;
+    p.a.scale_log2e = scale * 1.44269504088896340736f;
+    p.a.part_o = static_cast<float *>(workspace);
+    p.a.part_lse = p.a.part_o + (size_t)pairs * plan.n_splits * p.rows * head_dim;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    switch (head_dim) {
+    case 64: return paged ? launch_grouped<64, true, true>(p, (unsigned)grid, stream) : launch_grouped<64, false, true>(p, (unsigned)grid, stream);
+    case 128: return paged ? launch_grouped<128, true, true>(p, (unsigned)grid, stream) : launch_grouped<128, false, true>(p, (unsigned)grid, stream);
+    default: return paged ? launch_grouped<256, true, true>(p, (unsigned)grid, stream) : launch_grouped<256, false, true>(p, (unsigned)grid, stream);
+    }
+}
+
+size_t instinfer_tree_workspace_bytes(int32_t batch, int32_t tree_tokens, int32_t q_heads, int32_t kv_heads,
+                                      int32_t head_dim, int32_t max_seq_len)
+{
+    if (tree_attention_shape(batch, tree_tokens, q_heads, kv_heads, head_dim, max_seq_len) != INSTINFER_OK) return 0;
+    const int64_t pairs = (int64_t)batch * kv_heads;
+    if (pairs == 0) return 256;
+    const int32_t rows = q_heads / kv_heads * tree_tokens, groups = (rows + kGroupRows - 1) / kGroupRows;
+    return grouped_workspace_for(pairs, rows, head_dim, make_plan(pairs * groups, max_seq_len, grouped_rules(head_dim)));
+}
+
+}  // extern "C"

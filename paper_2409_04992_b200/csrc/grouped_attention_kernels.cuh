@@ -23,6 +23,7 @@
 #pragma once
 
 #include "decode_attention_kernels.cuh"
+#include "tree_common.cuh"
 
 namespace instinfer {
 
@@ -45,6 +46,10 @@ struct GroupedParams {
     int32_t group;         // query heads per KV head
     int32_t q_tokens;      // new tokens per sequence; token t sees positions < len - (q_tokens-1-t)
     int32_t rows;          // group * q_tokens <= kGroupRows; row r = t * group + g
+    // Trees of drafted tokens only (kTree): q_tokens nodes per sequence, any number of rows, which
+    // blocks take kGroupRows at a time (row_groups blocks per chunk, side by side in the grid).
+    TreeShape tree;
+    int32_t row_groups;
 };
 
 template <int D>
@@ -96,10 +101,11 @@ __device__ __forceinline__ int64_t grouped_row_index(const GroupedParams &p, int
 // One 16-token tile against the 16 query rows: logits, online softmax, and O += P V.  `base`
 // is the stage's shared-memory address; the running state (references, sums, output fragments)
 // is updated in place.
-template <int D>
+template <int D, bool kTree>
 __device__ __forceinline__ void grouped_tile(unsigned base, unsigned k_rd, unsigned v_rd, unsigned q_rd,
                                              const unsigned (&qa)[GroupedGeometry<D>::kQInSmem ? 1 : GroupedGeometry<D>::kKSteps][4],
                                              int tok0, int unmasked_end, int vis_lo, int vis_hi,
+                                             const TreeRow &tree_lo, const TreeRow &tree_hi,
                                              float scale_log2e, int quad, float &m_lo, float &m_hi,
                                              float &l_lo, float &l_hi, float (&o)[D / 8][4])
 {
@@ -135,6 +141,11 @@ __device__ __forceinline__ void grouped_tile(unsigned base, unsigned k_rd, unsig
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int tok = tok0 + n * 8 + quad * 2 + e;
+                if (kTree) {                     // unmasked_end: where the tree begins
+                    if (!tree_lo.sees(tok - unmasked_end)) s[n][e] = -INFINITY;
+                    if (!tree_hi.sees(tok - unmasked_end)) s[n][2 + e] = -INFINITY;
+                    continue;
+                }
                 if (tok >= vis_lo) s[n][e] = -INFINITY;
                 if (tok >= vis_hi) s[n][2 + e] = -INFINITY;
             }
@@ -210,7 +221,8 @@ __device__ __forceinline__ void grouped_tile(unsigned base, unsigned k_rd, unsig
     }
 }
 
-template <int D, bool kPaged>
+// kTree: the rows are nodes of a draft tree, see tree_common.cuh.
+template <int D, bool kPaged, bool kTree>
 __global__ void __launch_bounds__(kThreads, GroupedGeometry<D>::kCtasPerSm)
 grouped_attn_split_kernel(const GroupedParams p)
 {
@@ -219,22 +231,30 @@ grouped_attn_split_kernel(const GroupedParams p)
     const AttnParams &a = p.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int gid = lane >> 2, quad = lane & 3;          // MMA fragment coordinates
-    const int order = blockIdx.x / a.pairs;
-    const int pair = blockIdx.x - order * a.pairs;
+    const int block = kTree ? blockIdx.x / p.row_groups : blockIdx.x;
+    const int row0 = kTree ? (blockIdx.x - block * p.row_groups) * kGroupRows : 0;    // this block's first row ...
+    const int rows_here = kTree ? min(kGroupRows, p.rows - row0) : p.rows;            // ... and how many
+    const int order = block / a.pairs;
+    const int pair = block - order * a.pairs;
     const int split = scheduled_chunk(a, order);
     const int b = pair / a.heads, hk = pair - b * a.heads;
     const bool final_writer = a.n_splits == 1;
     allow_next_kernel();
     wait_for_previous_kernels();
 
-    const int len = checked_seq_len(a, b, threadIdx.x == 0 && hk == 0 && final_writer);
+    const bool reports = threadIdx.x == 0 && hk == 0 && final_writer && row0 == 0;
+    int nodes = 0;
+    const int len = kTree ? checked_tree(p.tree, a.seq_lens, a.max_seq_len, a.status, b, reports, nodes)
+                          : checked_seq_len(a, b, reports);
+    __shared__ unsigned poison[kTree ? 4 : 1];       // kTree: nodes of this chunk whose value row is not finite
+    if (kTree && threadIdx.x < 4) poison[threadIdx.x] = 0u;
     int begin, chunk_size;
     chunk_range(a, split, begin, chunk_size);
     if (begin >= len) {
         if (final_writer) {                    // inactive slot: zero output, lse = -inf
-            for (int i = threadIdx.x; i < p.rows * D; i += kThreads) {
+            for (int i = threadIdx.x; i < rows_here * D; i += kThreads) {
                 const int r = i / D, d = i - r * D;
-                const int64_t row = grouped_row_index(p, b, hk, r);
+                const int64_t row = grouped_row_index(p, b, hk, row0 + r);
                 a.out[row * D + d] = __float2half_rn(0.f);
                 if (a.lse && d == 0) a.lse[row] = -INFINITY;
             }
@@ -247,7 +267,12 @@ grouped_attn_split_kernel(const GroupedParams p)
 
     // Rows gid and gid + 8 of the MMA tile belong to this lane: their query rows and how many
     // cached positions each may see (rows beyond p.rows are padding and see nothing).
-    const bool has_lo = gid < p.rows, has_hi = gid + 8 < p.rows;
+    const bool has_lo = gid < rows_here, has_hi = gid + 8 < rows_here;
+    TreeRow tree_lo = {}, tree_hi = {};
+    if (kTree) {
+        tree_lo = tree_row(p.tree, b, has_lo ? (row0 + gid) / p.group : -1, nodes);
+        tree_hi = tree_row(p.tree, b, has_hi ? (row0 + gid + 8) / p.group : -1, nodes);
+    }
     const int vis_lo = has_lo ? len - (p.q_tokens - 1 - gid / p.group) : 0;
     const int vis_hi = has_hi ? len - (p.q_tokens - 1 - (gid + 8) / p.group) : 0;
     const unsigned smem_base = static_cast<unsigned>(__cvta_generic_to_shared(smem));
@@ -262,14 +287,14 @@ grouped_attn_split_kernel(const GroupedParams p)
         for (int i = threadIdx.x; i < kGroupRows * (D / 8); i += kThreads) {
             const int r = i / (D / 8), seg = i - r * (D / 8);
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < p.rows)
-                v = reinterpret_cast<const uint4 *>(a.q + grouped_row_index(p, b, hk, r) * D)[seg];
+            if (r < rows_here)
+                v = reinterpret_cast<const uint4 *>(a.q + grouped_row_index(p, b, hk, row0 + r) * D)[seg];
             *reinterpret_cast<uint4 *>(q_sm + r * G::kRowStride + seg * 16) = v;
         }
         __syncthreads();
     } else {
-        const __half *q_lo = a.q + (has_lo ? grouped_row_index(p, b, hk, gid) : 0) * D;
-        const __half *q_hi = a.q + (has_hi ? grouped_row_index(p, b, hk, gid + 8) : 0) * D;
+        const __half *q_lo = a.q + (has_lo ? grouped_row_index(p, b, hk, row0 + gid) : 0) * D;
+        const __half *q_hi = a.q + (has_hi ? grouped_row_index(p, b, hk, row0 + gid + 8) : 0) * D;
 #pragma unroll
         for (int ks = 0; ks < G::kKSteps; ++ks) {
             const int c = ks * 16 + quad * 2;
@@ -381,7 +406,8 @@ grouped_attn_split_kernel(const GroupedParams p)
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
     // Tiles that end at or before this position need no causal or length mask for any row.
-    const int unmasked_end = len - (p.q_tokens - 1);
+    const int unmasked_end = kTree ? len - nodes : len - (p.q_tokens - 1);
+    if (kTree) __syncthreads();          // `poison` is cleared
 
 #pragma unroll
     for (int j = 0; j < kGroupStages - 1; ++j) issue();
@@ -395,8 +421,24 @@ grouped_attn_split_kernel(const GroupedParams p)
         stage = stage + 1 == kGroupStages ? 0 : stage + 1;
         const int tok0 = first_token + j * kStepTokens;
 
-        grouped_tile<D>(base, k_rd, v_rd, q_rd, qa, tok0, unmasked_end, vis_lo, vis_hi, a.scale_log2e, quad,
-                        m_lo, m_hi, l_lo, l_hi, o);
+        if (kTree && tok0 + kGroupTile > unmasked_end) {
+            // A node's value row may hold anything as far as the rows that do not see it are
+            // concerned, but weight 0 times NaN is NaN: a row that is not finite leaves the tile and
+            // is added at the end to the rows that see it.  Two lanes look through one row.
+            const int row = lane >> 1, node = tok0 + row - unmasked_end;
+            uint4 *v_row = reinterpret_cast<uint4 *>(smem + (base - smem_base) + G::kTileBytes + row * G::kRowStride);
+            bool bad = false;
+            if (node >= 0 && tok0 + row < end)
+                for (int i = lane & 1; i < D / 8; i += 2) bad = bad || !finite8(v_row[i]);
+            bad = __shfl_xor_sync(0xffffffffu, (int)bad, 1) || bad;
+            if (bad) {
+                for (int i = lane & 1; i < D / 8; i += 2) v_row[i] = make_uint4(0u, 0u, 0u, 0u);
+                atomicOr(&poison[node >> 5], 1u << (node & 31));
+            }
+            __syncwarp();
+        }
+        grouped_tile<D, kTree>(base, k_rd, v_rd, q_rd, qa, tok0, unmasked_end, vis_lo, vis_hi, tree_lo, tree_hi,
+                               a.scale_log2e, quad, m_lo, m_hi, l_lo, l_hi, o);
     }
     cp_async_wait<0>();
 
@@ -424,7 +466,7 @@ grouped_attn_split_kernel(const GroupedParams p)
     }
     __syncthreads();
 
-    for (int i = threadIdx.x; i < p.rows * D; i += kThreads) {
+    for (int i = threadIdx.x; i < rows_here * D; i += kThreads) {
         const int r = i / D, d = i - r * D;
         float top = kMinusHuge;
 #pragma unroll
@@ -437,15 +479,28 @@ grouped_attn_split_kernel(const GroupedParams p)
             acc = fmaf(weight, sm_o[(w * kGroupRows + r) * D + d], acc);
         }
         // A row that sees no position of this chunk (causal limit before the chunk) has total 0.
-        const bool empty = !(total > 0.f);
-        const float value = empty ? 0.f : acc / total;
+        // (kTree: a NaN total is not an empty row's, so that what a row sees shows in it; rows behind the
+        // tree have met the tiles before it unmasked and end here.)
+        const bool empty = kTree ? total == 0.f || (row0 + r) / p.group >= nodes : !(total > 0.f);
+        float value = empty ? 0.f : acc / total;
         const float lse2 = empty ? kMinusHuge : top + log2f(total) - kGroupWeightLog2;
+        if (kTree && (poison[0] | poison[1] | poison[2] | poison[3]) != 0u) {
+            const TreeRow seen = tree_row(p.tree, b, (row0 + r) / p.group, nodes);
+            const __half *q_row = a.q + grouped_row_index(p, b, hk, row0 + r) * D;
+            for (int node = 0; node < nodes; ++node) {
+                if (!(poison[node >> 5] >> (node & 31) & 1u) || !seen.sees(node)) continue;
+                const int64_t kv_row = tree_cache_row(a, b, hk, unmasked_end + node);
+                float dot = 0.f;
+                for (int c = 0; c < D; ++c) dot = fmaf(__half2float(q_row[c]), __half2float(a.k[kv_row * D + c]), dot);
+                value += fast_exp2(dot * a.scale_log2e - lse2) * __half2float(a.v[kv_row * D + d]);
+            }
+        }
         if (final_writer) {
-            const int64_t row = grouped_row_index(p, b, hk, r);
+            const int64_t row = grouped_row_index(p, b, hk, row0 + r);
             a.out[row * D + d] = __float2half_rn(value);
             if (a.lse && d == 0) a.lse[row] = empty ? -INFINITY : lse2 * kLn2;
         } else {
-            const int64_t slot = ((int64_t)pair * a.n_splits + split) * p.rows + r;
+            const int64_t slot = ((int64_t)pair * a.n_splits + split) * p.rows + row0 + r;
             a.part_o[slot * D + d] = value;
             if (d == 0) a.part_lse[slot] = lse2;
         }
@@ -454,7 +509,7 @@ grouped_attn_split_kernel(const GroupedParams p)
 
 // Log-sum-exp merge of the chunk partials of one query row; one block per (sequence, KV
 // head, row), one thread per output dim.
-template <int D>
+template <int D, bool kTree>
 __global__ void __launch_bounds__(D)
 grouped_merge_kernel(const GroupedParams p)
 {
@@ -463,13 +518,21 @@ grouped_merge_kernel(const GroupedParams p)
     const int b = pair / a.heads, hk = pair - b * a.heads;
     allow_next_kernel();
     wait_for_previous_kernels();
-    const int len = checked_seq_len(a, b, threadIdx.x == 0 && hk == 0 && r == 0);
+    const bool reports = threadIdx.x == 0 && hk == 0 && r == 0;
+    int nodes = 0;
+    const int len = kTree ? checked_tree(p.tree, a.seq_lens, a.max_seq_len, a.status, b, reports, nodes)
+                          : checked_seq_len(a, b, reports);
     const int parts = live_chunks(a, len);
     const int64_t row = grouped_row_index(p, b, hk, r);
     const int64_t first = (int64_t)pair * a.n_splits * p.rows + r;      // slot of chunk 0
     float top = kMinusHuge;
-    for (int s = 0; s < parts; ++s) top = fmaxf(top, a.part_lse[first + (int64_t)s * p.rows]);
-    if (!(top > kMinusHuge)) {                 // no part holds a position this row may see
+    bool any_nan = false;                      // kTree: a part that is NaN makes the row NaN
+    for (int s = 0; s < parts; ++s) {
+        const float part = a.part_lse[first + (int64_t)s * p.rows];
+        top = fmaxf(top, part);
+        any_nan = any_nan || (kTree && part != part);
+    }
+    if (!(top > kMinusHuge) && !any_nan) {     // no part holds a position this row may see
         a.out[row * D + threadIdx.x] = __float2half_rn(0.f);
         if (a.lse && threadIdx.x == 0) a.lse[row] = -INFINITY;
         return;

@@ -534,3 +534,5 @@ const char *instinfer_status_string(int status)
 
 #include "api_grouped.inl"
 #include "api_sparf.inl"
+#include "api_tree.inl"
+#include "api_draft.inl"

@@ -1,0 +1,326 @@
+// Draft trees for sm_100a: the ancestors' bit masks that tree attention reads, and the
+// verification of a tree of drafted tokens against the target's probabilities.
+//
+// Verification is recursive rejection sampling.  At node v, w = p_v (the target's distribution
+// after v) and Z = 1; the children c of v are tried in index order: c is taken if
+//     u_c q_v(x_c) Z < w(x_c),
+// and the walk goes on from c; otherwise w <- max(w - Z q_v, 0), Z <- sum w, which is Z times the
+// residual distribution (an empty residual, sum 0, leaves w and Z as they were).  Where no child
+// is taken, the next token is the first i with w_0 + ... + w_i > u_0 sum w.  If the children of v
+// were drawn from q_v independently, the emitted tokens are distributed as the target's.  Without
+// draft distributions q_v is one-hot at x_c (drafts that were not sampled).
+//
+// Everything is decided in 64 bits: a decision compares numbers that differ by as little as one
+// rounding, and the sums run over a vocabulary.  Only the node where the walk ends (and nodes with
+// a rejected child before a later one) needs passes over whole rows, so the work is a row or two
+// of p and q per sequence: latency for one sequence, HBM bandwidth for many.  A cluster of up to
+// 8 blocks shares a sequence's rows; all blocks walk the tree alike on the few gathered values,
+// and exchange only their partial sums, through distributed shared memory.
+#pragma once
+
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "kv_pages_kernels.cuh"
+
+namespace instinfer {
+
+// ---- ancestors -------------------------------------------------------------------------------
+// One block per sequence, one thread per node: its bits are itself and every node on its way to a
+// root.  Parents come before their children, so a walk takes at most its node's index in steps.
+__global__ void __launch_bounds__(kMaxTreeTokens)
+tree_mask_kernel(uint64_t *mask, const int32_t *parents, const int32_t *tree_lens, int32_t tree_tokens, int32_t words,
+                 int32_t *status)
+{
+    __shared__ int up[kMaxTreeTokens];
+    const int b = blockIdx.x, t = threadIdx.x;
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    int nodes = tree_lens ? tree_lens[b] : tree_tokens;
+    bool bad = nodes < 0 || nodes > tree_tokens;
+    if (bad) nodes = 0;
+    if (t < nodes) {
+        int parent = parents[(int64_t)b * tree_tokens + t];
+        if (parent < -1 || parent >= t) {                     // treated as a root
+            parent = -1;
+            bad = true;
+        }
+        up[t] = parent;
+    }
+    if (bad && status) atomicOr(status, kFlagTreeRange);
+    __syncthreads();
+    uint64_t bits[2] = {0, 0};
+    if (t < nodes)
+        for (int a = t; a >= 0; a = up[a]) bits[a >> 6] |= (uint64_t)1 << (a & 63);
+    if (t < tree_tokens)
+        for (int w = 0; w < words; ++w) mask[((int64_t)b * tree_tokens + t) * words + w] = bits[w];
+}
+
+// ---- verification ----------------------------------------------------------------------------
+struct VerifyParams {
+    int32_t *path;                // [batch, tree_tokens]
+    int32_t *path_lens;           // [batch]
+    int32_t *out_tokens;          // [batch, tree_tokens]
+    const void *target;           // rows of `vocab` probabilities, row_stride elements apart
+    const void *draft;            // the same rows of the draft's distributions, nullable
+    const int32_t *tokens;        // [batch, tree_tokens]
+    const int32_t *parents;
+    const int32_t *tree_lens;     // nullable
+    const float *uniforms;        // [batch, tree_tokens]
+    int32_t *status;
+    int64_t row_stride;
+    int32_t tree_tokens, vocab;
+};
+
+constexpr int kVerifyThreads = 256;
+constexpr int kVerifyWarps = kVerifyThreads / 32;
+constexpr int kVerifyMaxCtas = 8;
+
+// A probability as the verification sees it: what is not a positive finite number counts as 0.
+__device__ __forceinline__ double clean(float x) { return x > 0.f && x < INFINITY ? (double)x : 0.0; }
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(__half x) { return __half2float(x); }
+__device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// 16 bytes of a row: group g holds elements g * kVec - shift ..., where `shift` makes groups fall
+// on 16-byte boundaries of memory (rows of an odd vocabulary start anywhere); elements outside
+// the row read as 0.
+template <typename E>
+struct RowReader {
+    static constexpr int kVec = 16 / (int)sizeof(E);
+    const E *row;
+    int vocab, shift;
+    __device__ __forceinline__ RowReader(const void *base, int64_t offset, int vocab_)
+        : row(static_cast<const E *>(base) + offset), vocab(vocab_),
+          shift((int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(E))) {}
+    __device__ __forceinline__ int groups() const { return (vocab + shift + kVec - 1) / kVec; }
+    __device__ __forceinline__ void load(int g, float (&x)[kVec]) const
+    {
+        const int first = g * kVec - shift;
+        if (first >= 0 && first + kVec <= vocab) {
+            const uint4 raw = __ldg(reinterpret_cast<const uint4 *>(row + first));
+            const E *e = reinterpret_cast<const E *>(&raw);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) x[i] = widen(e[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) x[i] = first + i >= 0 && first + i < vocab ? widen(row[first + i]) : 0.f;
+        }
+    }
+};
+
+__device__ __forceinline__ double warp_sum(double v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+template <typename E>
+__global__ void __launch_bounds__(kVerifyThreads)
+verify_tree_kernel(const VerifyParams p)
+{
+    namespace cg = cooperative_groups;
+    constexpr int kVec = RowReader<E>::kVec;
+    cg::cluster_group cluster = cg::this_cluster();
+    __shared__ int s_parent[kMaxTreeTokens], s_token[kMaxTreeTokens], s_path[kMaxTreeTokens], s_rejected[kMaxTreeTokens];
+    __shared__ double s_target[kMaxTreeTokens], s_draft[kMaxTreeTokens], s_u[kMaxTreeTokens], s_total[kMaxTreeTokens];
+    __shared__ double s_sums[2][kVerifyMaxCtas * kVerifyWarps];         // every warp's share of a pass, by the pass's parity
+    const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int b = blockIdx.x / ctas, t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int N = p.tree_tokens;
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    const int64_t first_row = (int64_t)b * N;
+    int nodes = p.tree_lens ? p.tree_lens[b] : N;
+    if (nodes < 0 || nodes > N) {
+        if (rank == 0 && t == 0 && p.status) atomicOr(p.status, kFlagTreeRange);
+        nodes = 0;
+    }
+    // The values that the walk compares: each node's token under its parent's two distributions.
+    if (t < N) {
+        int parent = -1, token = -1;
+        double pt = 0.0, qt = 1.0;
+        if (t < nodes) {
+            token = p.tokens[first_row + t];
+            parent = p.parents[first_row + t];
+            const bool token_ok = token >= 0 && token < p.vocab;
+            if (t > 0) {                                      // the root is given, not tried
+                if (parent < 0 || parent >= t || !token_ok) {
+                    if (rank == 0 && p.status) atomicOr(p.status, kFlagTreeRange);
+                    parent = -1;                              // never tried
+                } else {
+                    const int64_t at = (first_row + parent) * p.row_stride + token;
+                    pt = clean(widen(static_cast<const E *>(p.target)[at]));
+                    if (p.draft) qt = clean(widen(static_cast<const E *>(p.draft)[at]));
+                }
+            }
+            s_u[t] = (double)p.uniforms[first_row + t];
+        }
+        s_parent[t] = t > 0 ? parent : -1;
+        s_token[t] = token;
+        s_target[t] = pt;
+        s_draft[t] = qt;
+    }
+    cluster.sync();                                           // also: every block runs before its shared memory is written to
+
+    int at = 0, kept = nodes > 0 ? 1 : 0, pass = 0;
+    if (nodes > 0) {
+        // ---- the walk: the same in every thread of the cluster ----
+        int rejected = 0;                                     // residuals taken at the current node: s_total[0 .. rejected)
+        bool summed = false;                                  // the sums of the current w are in s_sums
+        double total = 1.0;
+        // w at one element of the current node, from its p and q values
+        auto residual = [&](double w, double q, int element) -> double {
+            for (int k = 0; k < rejected; ++k) {
+                const double qk = p.draft ? q : (element == s_rejected[k] ? 1.0 : 0.0);
+                w = fmax(__dsub_rn(w, __dmul_rn(s_total[k], qk)), 0.0);
+            }
+            return w;
+        };
+        // Sums of w over the vocabulary: a warp's share of the row is a run of groups, so that the
+        // sums of the warps in order are those of consecutive pieces of the row.
+        const int pieces = ctas * kVerifyWarps, piece = rank * kVerifyWarps + warp;
+        auto sum_row = [&]() -> double {
+            const int64_t offset = (first_row + at) * p.row_stride;
+            const RowReader<E> pr(p.target, offset, p.vocab), qr(p.draft ? p.draft : p.target, offset, p.vocab);
+            const int groups = pr.groups();
+            const int g0 = (int)((int64_t)groups * piece / pieces), g1 = (int)((int64_t)groups * (piece + 1) / pieces);
+            const bool read_q = p.draft != nullptr && rejected > 0;
+            double sum = 0.0;
+            for (int g = g0 + lane; g < g1; g += 32) {
+                float x[kVec], y[kVec];
+                pr.load(g, x);
+                if (read_q) qr.load(g, y);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i)
+                    sum += residual(clean(x[i]), read_q ? clean(y[i]) : 0.0, g * kVec - pr.shift + i);
+            }
+            sum = warp_sum(sum);
+            const int parity = pass & 1;
+            if (lane < ctas) cluster.map_shared_rank(&s_sums[0][0], lane)[parity * kVerifyMaxCtas * kVerifyWarps + piece] = sum;
+            cluster.sync();
+            ++pass;
+            const double *sums = s_sums[parity];
+            return warp_sum((lane < pieces ? sums[lane] : 0.0) + (lane + 32 < pieces ? sums[lane + 32] : 0.0));
+        };
+        if (t == 0) s_path[0] = 0;
+        for (int c = 1; c < nodes;) {
+            // the next child of `at` from c on
+            int next = nodes;
+            for (int base = c & ~31; base < nodes && next == nodes; base += 32) {
+                const int n = base + lane;
+                const unsigned hit = __ballot_sync(0xffffffffu, n >= c && n < nodes && s_parent[n] == at);
+                if (hit) next = base + __ffs(hit) - 1;
+            }
+            if (next == nodes) break;
+            const double q = s_draft[next];
+            const double w = residual(s_target[next], q, s_token[next]);
+            if (s_u[next] * q * total < w) {
+                at = next;
+                if (t == 0) s_path[kept] = next;
+                ++kept;
+                rejected = 0;
+                total = 1.0;
+                summed = false;
+            } else {
+                __syncthreads();                              // earlier readers of the lists are done
+                if (t == 0) {
+                    s_total[rejected] = total;
+                    s_rejected[rejected] = s_token[next];
+                }
+                __syncthreads();
+                ++rejected;
+                const double left = sum_row();
+                summed = left > 0.0;
+                if (summed) total = left;
+                else --rejected;                              // an empty residual: w stays as it was
+            }
+            c = next + 1;
+        }
+        if (!summed) total = sum_row();
+        // ---- the next token: the first element at which the running sum exceeds u_0 * total ----
+        const double *sums = s_sums[(pass - 1) & 1];
+        const double goal = s_u[0] * total;
+        double before = 0.0;
+        int chosen = -1, last_live = -1;
+        double before_last = 0.0;
+        for (int i = 0; i < pieces; ++i) {
+            const double s = sums[i];
+            if (s > 0.0) {
+                last_live = i;
+                before_last = before;
+                if (chosen < 0 && before + s > goal) {
+                    chosen = i;
+                    break;
+                }
+            }
+            before += s;
+        }
+        if (chosen < 0) {                                     // u_0 is not below 1
+            chosen = last_live;
+            before = before_last;
+        }
+        if (chosen < 0) {                                     // no positive probability at all
+            if (rank == 0 && t == 0) {
+                p.out_tokens[first_row + kept - 1] = -1;
+                if (p.status) atomicOr(p.status, kFlagTreeRange);
+            }
+        } else if (chosen == piece) {
+            const int64_t offset = (first_row + at) * p.row_stride;
+            const RowReader<E> pr(p.target, offset, p.vocab), qr(p.draft ? p.draft : p.target, offset, p.vocab);
+            const int groups = pr.groups();
+            const int g0 = (int)((int64_t)groups * piece / pieces), g1 = (int)((int64_t)groups * (piece + 1) / pieces);
+            const bool read_q = p.draft != nullptr && rejected > 0;
+            int found = -1, last = -1;                        // `last`: the last element with any weight
+            for (int g = g0; g < g1 && found < 0; g += 32) {
+                double w[kVec], mine = 0.0;
+                float x[kVec], y[kVec];
+                const bool live = g + lane < g1;
+                if (live) pr.load(g + lane, x);
+                if (live && read_q) qr.load(g + lane, y);
+                int mine_last = -1;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    const int element = (g + lane) * kVec - pr.shift + i;
+                    w[i] = live ? residual(clean(x[i]), read_q ? clean(y[i]) : 0.0, element) : 0.0;
+                    if (w[i] > 0.0) mine_last = element;
+                    mine += w[i];
+                }
+                double run = mine;                            // inclusive over the lanes
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const double up = __shfl_up_sync(0xffffffffu, run, o);
+                    if (lane >= o) run += up;
+                }
+                double upto = before + (run - mine);
+                int here = -1;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    upto += w[i];
+                    if (here < 0 && w[i] > 0.0 && upto > goal) here = (g + lane) * kVec - pr.shift + i;
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, here >= 0);
+                if (hit) found = __shfl_sync(0xffffffffu, here, __ffs(hit) - 1);
+                last = max(last, (int)__reduce_max_sync(0xffffffffu, mine_last));
+                before += __shfl_sync(0xffffffffu, run, 31);
+            }
+            if (lane == 0) p.out_tokens[first_row + kept - 1] = found >= 0 ? found : last;
+        }
+    }
+    __syncthreads();
+    if (rank == 0) {
+        if (t < N) {
+            p.path[first_row + t] = t < kept ? s_path[t] : -1;
+            if (t < kept - 1) p.out_tokens[first_row + t] = s_token[s_path[t + 1]];
+            else if (t >= kept) p.out_tokens[first_row + t] = -1;
+        }
+        if (t == 0) p.path_lens[b] = kept;
+    }
+}
+
+}  // namespace instinfer
