@@ -102,16 +102,16 @@ bool umma_shape(int32_t head_dim, bool paged, int32_t block_tokens)
 }
 
 // The query tensor [B, Tq, Hq, head_dim] as the copy engine sees it: a box is 64 dims of the `group`
-// heads of one KV head for all Tq new tokens, i.e. the chunk's rows t * group + g in order.
+// heads of one KV head for `box_tokens` (all Tq) new tokens, i.e. the chunk's rows t * group + g in order.
 bool make_query_map(CUtensorMap *map, const void *q, int32_t batch, int32_t q_tokens, int32_t q_heads, int32_t group,
-                    int32_t head_dim)
+                    int32_t head_dim, int32_t box_tokens)
 {
     EncodeTiledFn encode = tensor_map_encoder();
     if (encode == nullptr) return false;
     const cuuint64_t row = (cuuint64_t)head_dim * 2;
     const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)q_heads, (cuuint64_t)q_tokens, (cuuint64_t)batch};
     const cuuint64_t strides[3] = {row, (cuuint64_t)q_heads * row, (cuuint64_t)q_tokens * q_heads * row};
-    const cuuint32_t box[4] = {64, (cuuint32_t)group, (cuuint32_t)q_tokens, 1};
+    const cuuint32_t box[4] = {64, (cuuint32_t)group, (cuuint32_t)box_tokens, 1};
     const cuuint32_t elem[4] = {1, 1, 1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void *>(q), dims, strides, box, elem,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
@@ -219,7 +219,7 @@ int instinfer_decode_attention_grouped(void *out, float *lse, const void *q, con
     // 2^31 rows or more, or a driver without the encoder, takes the warp-level form.
     CUtensorMap map_q, map_k, map_v;
     const bool umma = g_grouped_path != 1 && umma_shape(head_dim, paged, block_tokens) &&
-                      make_query_map(&map_q, q, batch, q_tokens, q_heads, p.group, head_dim) &&
+                      make_query_map(&map_q, q, batch, q_tokens, q_heads, p.group, head_dim, q_tokens) &&
                       make_cache_map(&map_k, k_cache, kv_bytes / (2 * head_dim), head_dim,
                                      paged && block_tokens < kUmmaTile ? block_tokens : kUmmaTile) &&
                       make_cache_map(&map_v, v_cache, kv_bytes / (2 * head_dim), head_dim,

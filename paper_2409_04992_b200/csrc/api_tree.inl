@@ -1,5 +1,6 @@
 // C ABI, attention of a tree of drafted tokens over the cache: checks, plan and launches.
-// Included by instinfer_api.cu after api_grouped.inl, whose planner rules it shares.
+// Included by instinfer_api.cu after api_grouped.inl, whose planner rules and tensor maps it shares.
+#include "tree_umma_kernels.cuh"
 
 namespace {
 
@@ -15,6 +16,74 @@ int tree_attention_shape(int32_t batch, int32_t tree_tokens, int32_t q_heads, in
         (int64_t)(q_heads / kv_heads) * tree_tokens > INSTINFER_MAX_TREE_ROWS)
         return INSTINFER_ERR_UNSUPPORTED;
     return INSTINFER_OK;
+}
+
+// ---- the tcgen05 form ----
+
+// How the rows of a (sequence, KV head) are cut: row blocks of at most 128 rows, whole nodes each.  With
+// more than one, two share every K and V tile (head size 256 has no room in tensor memory for two).
+struct TreeRows {
+    int32_t streams, nodes_per_block, row_blocks, item_rows;
+};
+TreeRows tree_rows(int32_t tree_tokens, int32_t group, int32_t head_dim)
+{
+    TreeRows r;
+    const int32_t most = kTreeTile / group;
+    const int32_t blocks = (tree_tokens + most - 1) / most;
+    r.streams = blocks > 1 && head_dim != 256 ? 2 : 1;
+    r.row_blocks = (blocks + r.streams - 1) / r.streams;
+    r.nodes_per_block = (tree_tokens + r.row_blocks * r.streams - 1) / (r.row_blocks * r.streams);
+    r.item_rows = r.streams * r.nodes_per_block * group;
+    return r;
+}
+
+size_t tree_umma_workspace(int32_t tree_tokens, int32_t group, int32_t head_dim)
+{
+    if (group > kTreeTile) return 0;
+    const size_t rows = (size_t)2 * sm_count() * tree_rows(tree_tokens, group, head_dim).item_rows;
+    return (rows * (head_dim + 1) * sizeof(float) + 255) / 256 * 256;
+}
+
+// Blocks of 16, 32 or 64 tokens, or of a multiple of 128: no tile straddles blocks of another kind.
+bool tree_umma_shape(int32_t group, bool paged, int32_t block_tokens)
+{
+    return group <= kTreeTile && (!paged || block_tokens == 16 || block_tokens == 32 || block_tokens == 64 || block_tokens % kTreeTile == 0);
+}
+
+template <int D, bool kPaged, int kStreams>
+int launch_tree_umma(const TreeParams &p, unsigned grid, unsigned merge_grid, int row_parts, const CUtensorMap &map_q,
+                     const CUtensorMap &map_k, const CUtensorMap &map_v, cudaStream_t stream)
+{
+    using Geo = TreeGeometry<D, kStreams>;
+    static bool done[kMaxDevices] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return INSTINFER_ERR_CUDA;
+    if (!done[dev]) {
+        if (cudaFuncSetAttribute(tree_attn_umma_kernel<D, kPaged, kStreams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 Geo::kSmemBytes) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return INSTINFER_ERR_CUDA;
+        }
+        done[dev] = true;
+    }
+    cudaError_t err = launch_overlapped(tree_attn_umma_kernel<D, kPaged, kStreams>, grid, Geo::kThreads, Geo::kSmemBytes, stream, p,
+                                        map_q, map_k, map_v);
+    if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) return INSTINFER_ERR_CUDA;
+    err = launch_overlapped(tree_merge_kernel<D>, merge_grid, kTreeMergeThreads, 0, stream, p, (int)grid, row_parts);
+    return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? INSTINFER_OK : INSTINFER_ERR_CUDA;
+}
+
+template <int D>
+int launch_tree_umma_for(bool paged, int32_t streams, const TreeParams &p, unsigned grid, unsigned merge_grid, int row_parts,
+                         const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, cudaStream_t stream)
+{
+    if constexpr (D != 256) {
+        if (streams == 2)
+            return paged ? launch_tree_umma<D, true, 2>(p, grid, merge_grid, row_parts, map_q, map_k, map_v, stream)
+                         : launch_tree_umma<D, false, 2>(p, grid, merge_grid, row_parts, map_q, map_k, map_v, stream);
+    }
+    return paged ? launch_tree_umma<D, true, 1>(p, grid, merge_grid, row_parts, map_q, map_k, map_v, stream)
+                 : launch_tree_umma<D, false, 1>(p, grid, merge_grid, row_parts, map_q, map_k, map_v, stream);
 }
 
 }  // namespace
@@ -55,10 +124,9 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
     p.tree.lens = tree_lens;
     p.tree.tokens = tree_tokens;
     p.tree.words = (tree_tokens + 63) / 64;
-    const SplitPlan plan = make_plan(pairs * p.row_groups, max_seq_len, grouped_rules(head_dim));
-    if (workspace == nullptr || !aligned16(workspace) ||
-        workspace_bytes < grouped_workspace_for(pairs, p.rows, head_dim, plan))
+    if (!usable(workspace) || workspace_bytes < instinfer_tree_workspace_bytes(batch, tree_tokens, q_heads, kv_heads, head_dim, max_seq_len))
         return INSTINFER_ERR_WORKSPACE;
+    const SplitPlan plan = make_plan(pairs * p.row_groups, max_seq_len, grouped_rules(head_dim));
     const int64_t grid = pairs * plan.n_splits * p.row_groups;
     if (grid >= (int64_t)1 << 31 || pairs * p.rows >= (int64_t)1 << 31) return INSTINFER_ERR_INVALID_ARG;
     p.a.q = static_cast<const __half *>(q);
@@ -85,6 +153,36 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
     p.a.part_o = static_cast<float *>(workspace);
     p.a.part_lse = p.a.part_o + (size_t)pairs * plan.n_splits * p.rows * head_dim;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+
+    // The tcgen05 form, where the copy engine can take the shape (a cache of 2^31 rows or more, or a
+    // driver without the encoder, takes the warp-level one).
+    if (g_grouped_path != 1 && tree_umma_shape(p.group, paged, block_tokens)) {
+        const TreeRows rows = tree_rows(tree_tokens, p.group, head_dim);
+        const int64_t items = pairs * rows.row_blocks;
+        const int row_parts = (rows.item_rows + kTreeMergeRows - 1) / kTreeMergeRows;
+        const int32_t box = paged && block_tokens < kTreeTile ? block_tokens : kTreeTile;
+        CUtensorMap map_q, map_k, map_v;
+        if (items * row_parts < (int64_t)1 << 31 &&
+            make_query_map(&map_q, q, batch, tree_tokens, q_heads, p.group, head_dim, rows.nodes_per_block) &&
+            make_cache_map(&map_k, k_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box) &&
+            make_cache_map(&map_v, v_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box)) {
+            TreeParams u = {};
+            u.a = p.a;
+            u.tree = p.tree;
+            u.batch = batch;
+            u.group = p.group;
+            u.nodes_per_block = rows.nodes_per_block;
+            u.row_blocks = rows.row_blocks;
+            u.item_rows = rows.item_rows;
+            const int64_t most_tiles = items * ceil_div(max_seq_len, kTreeTile);
+            const unsigned blocks = (unsigned)(most_tiles < sm_count() ? most_tiles : sm_count());
+            u.a.part_lse = u.a.part_o + (size_t)2 * sm_count() * rows.item_rows * head_dim;
+            const unsigned merge = (unsigned)(items * row_parts);
+            return head_dim == 64 ? launch_tree_umma_for<64>(paged, rows.streams, u, blocks, merge, row_parts, map_q, map_k, map_v, stream)
+                   : head_dim == 128 ? launch_tree_umma_for<128>(paged, rows.streams, u, blocks, merge, row_parts, map_q, map_k, map_v, stream)
+                                     : launch_tree_umma_for<256>(paged, rows.streams, u, blocks, merge, row_parts, map_q, map_k, map_v, stream);
+        }
+    }
     switch (head_dim) {
     case 64: return paged ? launch_grouped<64, true, true>(p, (unsigned)grid, stream) : launch_grouped<64, false, true>(p, (unsigned)grid, stream);
     case 128: return paged ? launch_grouped<128, true, true>(p, (unsigned)grid, stream) : launch_grouped<128, false, true>(p, (unsigned)grid, stream);
@@ -99,7 +197,10 @@ size_t instinfer_tree_workspace_bytes(int32_t batch, int32_t tree_tokens, int32_
     const int64_t pairs = (int64_t)batch * kv_heads;
     if (pairs == 0) return 256;
     const int32_t rows = q_heads / kv_heads * tree_tokens, groups = (rows + kGroupRows - 1) / kGroupRows;
-    return grouped_workspace_for(pairs, rows, head_dim, make_plan(pairs * groups, max_seq_len, grouped_rules(head_dim)));
+    // enough for either implementation: which one runs also depends on the cache layout
+    const size_t warp_level = grouped_workspace_for(pairs, rows, head_dim, make_plan(pairs * groups, max_seq_len, grouped_rules(head_dim)));
+    const size_t umma = tree_umma_workspace(tree_tokens, q_heads / kv_heads, head_dim);
+    return warp_level > umma ? warp_level : umma;
 }
 
 }  // extern "C"

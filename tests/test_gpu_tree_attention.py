@@ -21,6 +21,14 @@ from tests import gpu_util as gu
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True, params=[2, 1], ids=["tcgen05", "warp-mma"])
+def path(request):
+    """Both implementations (shapes the tcgen05 form does not take fall back inside the library)."""
+    binding.set_grouped_path(request.param)
+    yield request.param
+    binding.set_grouped_path(0)
+
+
 def random_tree(rng, nodes, width):
     parents = np.full(width, -1, dtype=np.int32)
     for t in range(1, nodes):
