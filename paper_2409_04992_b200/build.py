@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
 _HERE = Path(__file__).resolve().parent
@@ -11,9 +12,10 @@ CSRC = _HERE / "csrc"
 INCLUDE = _HERE.parent / "include"
 LIBRARY = _HERE / "libinstinfer.so"
 CHECKED_LIBRARY = _HERE / "libinstinfer_checked.so"     # the bounds-checking build (-DINSTINFER_BOUNDS_CHECK)
-SOURCES = [CSRC / "instinfer_api.cu"]      # it includes the api_*.inl parts
+# instinfer_api.cu includes the api_*.inl parts; the others hold instances of large kernels, one head size each
+SOURCES = [CSRC / "instinfer_api.cu", CSRC / "tree_d64.cu", CSRC / "tree_d128.cu", CSRC / "tree_d256.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
-              "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-Xptxas", "-v"]
+              "-Xcompiler", "-fPIC", "-cudart", "static", "-Xptxas", "-v"]
 
 
 def _nvcc() -> str:
@@ -40,14 +42,28 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     library = CHECKED_LIBRARY if checked else LIBRARY
     if not force and is_current(library):
         return library
-    tmp = library.with_suffix(f".{os.getpid()}.tmp.so")
     extra = ["-DINSTINFER_BOUNDS_CHECK"] if checked else []
-    cmd = [_nvcc(), *NVCC_FLAGS, *extra, "-I", str(INCLUDE), *map(str, SOURCES), "-o", str(tmp)]
-    done = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or done.returncode:
-        print(done.stdout + done.stderr)
-    if done.returncode:
-        raise RuntimeError("nvcc failed")
+    stem = f"{library.stem}.{os.getpid()}.tmp"
+    objects = [library.with_name(f"{stem}.{source.stem}.o") for source in SOURCES]
+    tmp = library.with_name(f"{stem}.so")
+
+    def run(*args):
+        done = subprocess.run([_nvcc(), *NVCC_FLAGS, *args], capture_output=True, text=True)
+        if verbose or done.returncode:
+            print(done.stdout + done.stderr)
+        if done.returncode:
+            raise RuntimeError("nvcc failed")
+
+    try:
+        with ThreadPoolExecutor(max_workers=len(SOURCES)) as pool:      # the sources side by side
+            jobs = [pool.submit(run, *extra, "-I", str(INCLUDE), "-c", str(source), "-o", str(obj))
+                    for source, obj in zip(SOURCES, objects)]
+            for job in jobs:
+                job.result()
+        run("-shared", *map(str, objects), "-o", str(tmp))
+    finally:
+        for obj in objects:
+            obj.unlink(missing_ok=True)
     os.replace(tmp, library)
     return library
 

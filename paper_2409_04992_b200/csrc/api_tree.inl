@@ -1,6 +1,6 @@
 // C ABI, attention of a tree of drafted tokens over the cache: checks, plan and launches.
 // Included by instinfer_api.cu after api_grouped.inl, whose planner rules and tensor maps it shares.
-#include "tree_umma_kernels.cuh"
+#include "tree_launch.cuh"
 
 namespace {
 
@@ -20,23 +20,6 @@ int tree_attention_shape(int32_t batch, int32_t tree_tokens, int32_t q_heads, in
 
 // ---- the tcgen05 form ----
 
-// How the rows of a (sequence, KV head) are cut: row blocks of at most 128 rows, whole nodes each.  With
-// more than one, two share every K and V tile (head size 256 has no room in tensor memory for two).
-struct TreeRows {
-    int32_t streams, nodes_per_block, row_blocks, item_rows;
-};
-TreeRows tree_rows(int32_t tree_tokens, int32_t group, int32_t head_dim)
-{
-    TreeRows r;
-    const int32_t most = kTreeTile / group;
-    const int32_t blocks = (tree_tokens + most - 1) / most;
-    r.streams = blocks > 1 && head_dim != 256 ? 2 : 1;
-    r.row_blocks = (blocks + r.streams - 1) / r.streams;
-    r.nodes_per_block = (tree_tokens + r.row_blocks * r.streams - 1) / (r.row_blocks * r.streams);
-    r.item_rows = r.streams * r.nodes_per_block * group;
-    return r;
-}
-
 size_t tree_umma_workspace(int32_t tree_tokens, int32_t group, int32_t head_dim)
 {
     if (group > kTreeTile) return 0;
@@ -48,42 +31,6 @@ size_t tree_umma_workspace(int32_t tree_tokens, int32_t group, int32_t head_dim)
 bool tree_umma_shape(int32_t group, bool paged, int32_t block_tokens)
 {
     return group <= kTreeTile && (!paged || block_tokens == 16 || block_tokens == 32 || block_tokens == 64 || block_tokens % kTreeTile == 0);
-}
-
-template <int D, bool kPaged, int kStreams>
-int launch_tree_umma(const TreeParams &p, unsigned grid, unsigned merge_grid, int row_parts, const CUtensorMap &map_q,
-                     const CUtensorMap &map_k, const CUtensorMap &map_v, cudaStream_t stream)
-{
-    using Geo = TreeGeometry<D, kStreams>;
-    static bool done[kMaxDevices] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return INSTINFER_ERR_CUDA;
-    if (!done[dev]) {
-        if (cudaFuncSetAttribute(tree_attn_umma_kernel<D, kPaged, kStreams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 Geo::kSmemBytes) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return INSTINFER_ERR_CUDA;
-        }
-        done[dev] = true;
-    }
-    cudaError_t err = launch_overlapped(tree_attn_umma_kernel<D, kPaged, kStreams>, grid, Geo::kThreads, Geo::kSmemBytes, stream, p,
-                                        map_q, map_k, map_v);
-    if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) return INSTINFER_ERR_CUDA;
-    err = launch_overlapped(tree_merge_kernel<D>, merge_grid, kTreeMergeThreads, 0, stream, p, (int)grid, row_parts);
-    return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? INSTINFER_OK : INSTINFER_ERR_CUDA;
-}
-
-template <int D>
-int launch_tree_umma_for(bool paged, int32_t streams, const TreeParams &p, unsigned grid, unsigned merge_grid, int row_parts,
-                         const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, cudaStream_t stream)
-{
-    if constexpr (D != 256) {
-        if (streams == 2)
-            return paged ? launch_tree_umma<D, true, 2>(p, grid, merge_grid, row_parts, map_q, map_k, map_v, stream)
-                         : launch_tree_umma<D, false, 2>(p, grid, merge_grid, row_parts, map_q, map_k, map_v, stream);
-    }
-    return paged ? launch_tree_umma<D, true, 1>(p, grid, merge_grid, row_parts, map_q, map_k, map_v, stream)
-                 : launch_tree_umma<D, false, 1>(p, grid, merge_grid, row_parts, map_q, map_k, map_v, stream);
 }
 
 }  // namespace
@@ -161,26 +108,29 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
         const int64_t items = pairs * rows.row_blocks;
         const int row_parts = (rows.item_rows + kTreeMergeRows - 1) / kTreeMergeRows;
         const int32_t box = paged && block_tokens < kTreeTile ? block_tokens : kTreeTile;
-        CUtensorMap map_q, map_k, map_v;
+        TreeLaunch t = {};
         if (items * row_parts < (int64_t)1 << 31 &&
-            make_query_map(&map_q, q, batch, tree_tokens, q_heads, p.group, head_dim, rows.nodes_per_block) &&
-            make_cache_map(&map_k, k_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box) &&
-            make_cache_map(&map_v, v_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box)) {
-            TreeParams u = {};
-            u.a = p.a;
-            u.tree = p.tree;
-            u.batch = batch;
-            u.group = p.group;
-            u.nodes_per_block = rows.nodes_per_block;
-            u.row_blocks = rows.row_blocks;
-            u.item_rows = rows.item_rows;
+            make_query_map(&t.map_q, q, batch, tree_tokens, q_heads, p.group, head_dim, rows.nodes_per_block) &&
+            make_cache_map(&t.map_k, k_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box) &&
+            make_cache_map(&t.map_v, v_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box)) {
+            t.p.a = p.a;
+            t.p.a.part_lse = p.a.part_o + (size_t)2 * sm_count() * rows.item_rows * head_dim;
+            t.p.tree = p.tree;
+            t.p.batch = batch;
+            t.p.group = p.group;
+            t.p.nodes_per_block = rows.nodes_per_block;
+            t.p.row_blocks = rows.row_blocks;
+            t.p.item_rows = rows.item_rows;
             const int64_t most_tiles = items * ceil_div(max_seq_len, kTreeTile);
-            const unsigned blocks = (unsigned)(most_tiles < sm_count() ? most_tiles : sm_count());
-            u.a.part_lse = u.a.part_o + (size_t)2 * sm_count() * rows.item_rows * head_dim;
-            const unsigned merge = (unsigned)(items * row_parts);
-            return head_dim == 64 ? launch_tree_umma_for<64>(paged, rows.streams, u, blocks, merge, row_parts, map_q, map_k, map_v, stream)
-                   : head_dim == 128 ? launch_tree_umma_for<128>(paged, rows.streams, u, blocks, merge, row_parts, map_q, map_k, map_v, stream)
-                                     : launch_tree_umma_for<256>(paged, rows.streams, u, blocks, merge, row_parts, map_q, map_k, map_v, stream);
+            t.grid = (unsigned)(most_tiles < sm_count() ? most_tiles : sm_count());
+            t.merge_grid = (unsigned)(items * row_parts);
+            t.row_parts = row_parts;
+            t.stream = stream;
+            switch (head_dim) {
+            case 64: return paged ? launch_tree<64, true>(rows, t) : launch_tree<64, false>(rows, t);
+            case 128: return paged ? launch_tree<128, true>(rows, t) : launch_tree<128, false>(rows, t);
+            default: return paged ? launch_tree<256, true>(rows, t) : launch_tree<256, false>(rows, t);
+            }
         }
     }
     switch (head_dim) {

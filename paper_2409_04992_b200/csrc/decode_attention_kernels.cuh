@@ -684,7 +684,7 @@ decode_attn_split_kernel(const AttnParams p)
 
 // Log-sum-exp merge of the chunk partials of one (sequence, head); one block per pair,
 // one thread per output dim.  Only the chunks that hold tokens are read.
-__global__ void __launch_bounds__(kHeadDim)
+static __global__ void __launch_bounds__(kHeadDim)
 lse_merge_kernel(const AttnParams p)
 {
     const int pair = blockIdx.x;

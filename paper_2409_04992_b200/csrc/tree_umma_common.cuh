@@ -1,0 +1,640 @@
+// What the tcgen05 kernels for draft trees share (tree_umma_rows.cuh, tree_umma_tokens.cuh), for sm_100a: the
+// split of the work, the walk through it, the copies, and the merge of partial results.
+//
+// Work split: the tiles of 128 tokens of all (sequence, KV head, row block) items lie in one row, and
+// block c of G takes the tiles [W c / G, W (c + 1) / G) of the W there are, whatever items they belong
+// to.  So every SM reads the same number of bytes, and only the items that a block starts or ends inside
+// leave partial results: at most two per block (with fixed chunks the partials of a 16-sequence batch of
+// 64 rows were 8 % of the traffic).  The cuts follow from the lengths alone, not from the placement of blocks.
+//
+// A block has softmax warps and four single-purpose warps, which hand tiles over through mbarriers:
+//   K producer, V producer   tensor-map copies into a ring each (128-byte swizzle); a paged tile is 128 / T
+//                            copies of one (block, head) run; unreadable blocks are zero-filled;
+//   logit and output issuer  one elected thread each issues the MMAs of the logits and of the output.
+// Every wait is bounded by the clock; one that runs out sets kFlagCopyTimeout, after which that warp
+// waits no more, issues nothing more and ends.
+#pragma once
+
+#include "grouped_umma_kernels.cuh"
+#include "tree_common.cuh"
+
+namespace instinfer {
+
+constexpr int kTreeTile = 128;                         // tokens per tile
+constexpr int kTreePanelBytes = kTreeTile * 128;       // 64 dims of 128 rows
+
+// Ring geometry of a head size: an item is up to 128 dims of a tile (32 KiB; 16 KiB at head size 64).
+template <int D, int kBytes>
+struct TreeRing {
+    static constexpr int kPanels = D / 64;
+    static constexpr int kItemPanels = kPanels < 2 ? kPanels : 2;
+    static constexpr int kItems = kPanels / kItemPanels;                 // items per tile and cache
+    static constexpr int kItemBytes = kItemPanels * kTreePanelBytes;
+    static constexpr int kTotal = kBytes / kItemBytes;
+    static constexpr int kKSlots = kTotal / 2 < 6 ? kTotal / 2 : 6;
+    static constexpr int kVSlots = kTotal - kKSlots < 6 ? kTotal - kKSlots : 6;
+    static constexpr int kVOffset = kKSlots * kItemBytes;
+    static constexpr int kRingBytes = (kKSlots + kVSlots) * kItemBytes;
+    static_assert(kKSlots >= kItems && kVSlots >= kItems, "a whole tile has to fit each ring");
+};
+
+// Offsets inside the misc region that the kernels have in common.
+constexpr int kTreeBarKFull = 0;       // [6]
+constexpr int kTreeBarKEmpty = 48;     // [6]
+constexpr int kTreeBarVFull = 96;      // [6]
+constexpr int kTreeBarVEmpty = 144;    // [6]
+constexpr int kTreeBarSFull = 192;     // [2] logits of a unit are in tensor memory
+constexpr int kTreeBarPFull = 208;     // [2] its weights are where the output MMAs read them
+constexpr int kTreeBarPvDone = 224;    // [2] its output MMAs are complete
+constexpr int kTreeBarQFull = 240;
+constexpr int kTreeBarQEmpty = 248;
+constexpr int kTreeBarSFree = 256;     // [2] the logits have been read
+constexpr int kTreeTmemPtr = 272;
+constexpr int kTreeStart = 288;        // where the block's tiles begin: sequence, tile inside it (64 bits), number of tiles
+constexpr int kTreePoison = 320;       // [8][4] words: nodes of a segment whose value row is not finite, by segment number
+constexpr int kTreeScan = 448;         // [16] int64: per-warp sums of the set-up's scan
+constexpr int kTreeMiscBytes = 576;
+static_assert(kTreeScan + 16 * 8 <= kTreeMiscBytes && kTreeMiscBytes % 16 == 0, "misc region too small");
+
+struct TreeParams {
+    AttnParams a;              // heads = KV heads; part_o [2 G, item_rows, D], part_lse [2 G, item_rows]
+    TreeShape tree;
+    int32_t batch;
+    int32_t group;             // query heads per KV head
+    int32_t nodes_per_block;   // a row block is this many nodes' heads: row t * group + g of the block
+    int32_t row_blocks;        // items per (sequence, KV head), of one or two row blocks each
+    int32_t item_rows;         // rows of an item: all its row blocks'
+};
+
+// Number of tiles of a sequence's items.
+__device__ __forceinline__ int tree_tiles(int len, int nodes)
+{
+    return nodes > 0 ? (int)(((unsigned)len + kTreeTile - 1) / kTreeTile) : 0;
+}
+
+// The tile at which block `c` of `blocks` starts; blocks beyond the number of tiles have none.
+__device__ __forceinline__ int64_t tree_first_tile(int64_t total, int c, int blocks)
+{
+    const int64_t working = min((int64_t)blocks, total);
+    return c < working ? total * c / working : total;
+}
+
+// Tiles [t0, t1) of the n_tiles of one item.
+struct TreeSegment {
+    int b, len, nodes, hk, rb, t0, t1, n_tiles;
+    __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == n_tiles; }
+    __device__ __forceinline__ int prefix() const { return len - nodes; }
+};
+
+// The segments of one block, in order; every warp walks them by itself (all 32 lanes together).
+struct TreeWalk {
+    int b, len, nodes, item, tile;
+    int64_t left;
+    __device__ __forceinline__ void find(const TreeParams &p, int from, int lane)
+    {
+        // the next sequence from `from` on that has tiles (there is one as long as `left` is not 0)
+        for (b = from; b < p.batch; b += 32) {
+            int n = 0, l = 0;
+            if (b + lane < p.batch) l = checked_tree(p.tree, p.a.seq_lens, p.a.max_seq_len, nullptr, b + lane, false, n);
+            const unsigned live = __ballot_sync(0xffffffffu, tree_tiles(l, n) > 0);
+            if (live == 0) continue;
+            const int first = __ffs(live) - 1;
+            b += first;
+            len = __shfl_sync(0xffffffffu, l, first);
+            nodes = __shfl_sync(0xffffffffu, n, first);
+            return;
+        }
+        left = 0;
+    }
+    __device__ __forceinline__ void start(const TreeParams &p, const unsigned char *misc, int lane)
+    {
+        const int *at = reinterpret_cast<const int *>(misc + kTreeStart);
+        const int64_t inside = *reinterpret_cast<const int64_t *>(misc + kTreeStart + 8);
+        left = *reinterpret_cast<const int64_t *>(misc + kTreeStart + 16);
+        find(p, at[0], lane);
+        const int n = tree_tiles(len, nodes);
+        item = n > 0 ? (int)(inside / n) : 0;
+        tile = n > 0 ? (int)(inside - (int64_t)item * n) : 0;
+    }
+    __device__ __forceinline__ bool next(const TreeParams &p, TreeSegment &s, int lane)
+    {
+        if (left > 0 && item == p.a.heads * p.row_blocks) {
+            find(p, b + 1, lane);
+            item = 0;
+            tile = 0;
+        }
+        if (left <= 0) return false;
+        s.b = b;
+        s.len = len;
+        s.nodes = nodes;
+        s.hk = item / p.row_blocks;
+        s.rb = item - s.hk * p.row_blocks;
+        s.n_tiles = tree_tiles(len, nodes);
+        s.t0 = tile;
+        s.t1 = (int)min((int64_t)s.n_tiles, tile + left);
+        left -= s.t1 - s.t0;
+        tile = s.t1;
+        if (tile == s.n_tiles) {
+            tile = 0;
+            ++item;
+        }
+        return true;
+    }
+};
+
+// Finds where this block's tiles begin and leaves it in the misc region (all threads; the caller
+// synchronises before a walk starts).
+__device__ __forceinline__ void tree_find_start(const TreeParams &p, unsigned char *misc_ptr, int threads)
+{
+    const AttnParams &a = p.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int per_thread = (p.batch + threads - 1) / threads;
+    const int b0 = min((int)threadIdx.x * per_thread, p.batch), b1 = min(b0 + per_thread, p.batch);
+    const int items = a.heads * p.row_blocks;
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) {
+        int nodes;
+        const int len = checked_tree(p.tree, a.seq_lens, a.max_seq_len, a.status, b, blockIdx.x == 0, nodes);
+        mine += (int64_t)tree_tiles(len, nodes) * items;
+    }
+    int64_t run = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t up = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += up;
+    }
+    int64_t *scan = reinterpret_cast<int64_t *>(misc_ptr + kTreeScan);
+    if (lane == 31) scan[warp] = run;
+    if (threadIdx.x == 0) {                        // no tiles, unless a thread finds the first one below
+        *reinterpret_cast<int *>(misc_ptr + kTreeStart) = 0;
+        *reinterpret_cast<int64_t *>(misc_ptr + kTreeStart + 8) = 0;
+        *reinterpret_cast<int64_t *>(misc_ptr + kTreeStart + 16) = 0;
+    }
+    __syncthreads();
+    int64_t before = 0, total = 0;
+    for (int w = 0; w < threads / 32; ++w) {
+        if (w < warp) before += scan[w];
+        total += scan[w];
+    }
+    const int64_t first = tree_first_tile(total, blockIdx.x, gridDim.x), last = tree_first_tile(total, blockIdx.x + 1, gridDim.x);
+    int64_t at = before + run - mine;
+    if (first < last && at <= first && first < at + mine) {
+        for (int b = b0; b < b1; ++b) {
+            int nodes;
+            const int len = checked_tree(p.tree, a.seq_lens, a.max_seq_len, nullptr, b, false, nodes);
+            const int64_t n = (int64_t)tree_tiles(len, nodes) * items;
+            if (first < at + n) {
+                *reinterpret_cast<int *>(misc_ptr + kTreeStart) = b;
+                *reinterpret_cast<int64_t *>(misc_ptr + kTreeStart + 8) = first - at;
+                *reinterpret_cast<int64_t *>(misc_ptr + kTreeStart + 16) = last - first;
+                break;
+            }
+            at += n;
+        }
+    }
+}
+
+// ---- tensor-memory accesses of 32 columns ----
+__device__ __forceinline__ void tc_issue_load32(float (&v)[32], unsigned taddr)      // valid after tc_loaded32
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+                   "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+                   "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+                   "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+                 : "r"(taddr) : "memory");
+}
+// Waits for this thread's loads; the values pass through, so that nothing uses them earlier.
+__device__ __forceinline__ void tc_loaded32(float (&v)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                   "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+                   "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+                   "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+                 :: "memory");
+}
+__device__ __forceinline__ void tc_store32(unsigned taddr, const unsigned (&v)[32])  // complete after tc_stored
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 :: "r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+                    "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+                    "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+                    "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
+}
+__device__ __forceinline__ void tc_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D[tmem] (+)= A[tmem] B[smem]
+__device__ __forceinline__ void tc_mma_f16_ts(unsigned d_tmem, unsigned a_tmem, uint64_t b_desc, unsigned idesc, unsigned accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 :: "r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t x, y, z, d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(z) : "f"(c.x), "f"(c.y));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(x), "l"(y), "l"(z));
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    uint64_t x, y, d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(x), "l"(y));
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
+    return r;
+}
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t x, y, d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(x), "l"(y));
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// The largest of 32 values and `top`, as two chains (NaN does not count).
+__device__ __forceinline__ float max32(const float (&x)[32], float top)
+{
+    float even = max3(top, x[0], x[1]), odd = fmaxf(x[2], x[3]);
+#pragma unroll
+    for (int c = 4; c < 32; c += 4) {
+        even = max3(even, x[c], x[c + 1]);
+        odd = max3(odd, x[c + 2], x[c + 3]);
+    }
+    return fmaxf(even, odd);
+}
+
+// 128 bits: what a row sees of a tile, one word per 32 tokens.
+struct Bits128 {
+    uint64_t lo, hi;
+    __device__ __forceinline__ Bits128 shifted_up(int n) const           // 0 <= n < 128
+    {
+        if (n == 0) return *this;
+        if (n >= 64) return {0, lo << (n - 64)};
+        return {lo << n, hi << n | lo >> (64 - n)};
+    }
+    __device__ __forceinline__ Bits128 shifted_down(int n) const
+    {
+        if (n == 0) return *this;
+        if (n >= 64) return {hi >> (n - 64), 0};
+        return {lo >> n | hi << (64 - n), hi >> n};
+    }
+    __device__ __forceinline__ unsigned word(int i) const { return (unsigned)((i < 2 ? lo : hi) >> (32 * (i & 1))); }
+};
+
+
+// The copies of one block: K and V tiles into their rings, the query rows, and the clean-up of value rows
+// that must not meet a weight of 0.  `ring` and `misc` are shared-memory addresses, smem the ring's pointer.
+template <int D, bool kPaged, typename Ring>
+struct TreeCopies {
+    const TreeParams &p;
+    unsigned char *smem;
+    unsigned ring, misc;
+    int lane;
+
+    __device__ __forceinline__ int run_tokens() const { return kPaged ? min(p.a.block_tokens, kTreeTile) : kTreeTile; }
+    // lane i: the physical block of the i-th run of tile j
+    __device__ __forceinline__ int fetch_ids(const TreeSegment &s, int j) const
+    {
+        if (!kPaged) return 0;
+        const int T = run_tokens(), start = j * kTreeTile;
+        if (j >= s.t1 || lane >= (min(s.len - start, kTreeTile) + T - 1) / T) return -1;
+        const int idx = (start + lane * T) / p.a.block_tokens;
+        if (!bounds_ok(idx < p.a.max_blocks_per_seq, p.a.status)) return -1;
+        return __ldg(p.a.block_table + (int64_t)s.b * p.a.max_blocks_per_seq + idx);
+    }
+    // One tile of one cache (all lanes); false if a wait ran out.
+    template <bool kIsV>
+    __device__ __forceinline__ bool copy_tile(const TreeSegment &s, int j, int phys, const CUtensorMap *map, int &count) const
+    {
+        constexpr int slots = kIsV ? Ring::kVSlots : Ring::kKSlots, ring_offset = kIsV ? Ring::kVOffset : 0;
+        constexpr int bar_full = kIsV ? kTreeBarVFull : kTreeBarKFull, bar_empty = kIsV ? kTreeBarVEmpty : kTreeBarKEmpty;
+        const AttnParams &a = p.a;
+        const int T = run_tokens(), start = j * kTreeTile;
+        const int nb = kPaged ? (min(s.len - start, kTreeTile) + T - 1) / T : 1;
+        bool good = lane < nb;
+        int row0;
+        if (kPaged) {
+            const bool in_range = phys >= 0 && (int64_t)phys < a.num_phys_blocks;
+            if (good && !in_range && a.status) atomicOr(a.status, kFlagBlockRange);
+            // (< 2^31 rows: checked by the host)
+            row0 = in_range ? (phys * a.heads + s.hk) * a.block_tokens + (start + lane * T) % a.block_tokens : 0;
+            good = good && in_range && bounds_ok((int64_t)row0 + T <= a.kv_bytes / (2 * D), a.status);
+        } else {
+            row0 = (s.b * a.heads + s.hk) * a.s_max + start;      // rows past the tensor's end read as zeros
+        }
+        const unsigned fetched = __popc(__ballot_sync(0xffffffffu, good));
+#pragma unroll
+        for (int item = 0; item < Ring::kItems; ++item, ++count) {
+            const int slot = count % slots;
+            if (count >= slots &&
+                !__all_sync(0xffffffffu, mbarrier_wait_bounded(misc + bar_empty + slot * 8, (count / slots - 1) & 1)))
+                return false;
+            const int slot_offset = ring_offset + slot * Ring::kItemBytes + (kPaged ? lane * T * 128 : 0);
+            const unsigned bar = misc + bar_full + slot * 8;
+            if (kPaged && lane < nb && !good) {                   // a block that cannot be read counts as zeros
+                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                for (int i = 0; i < T * 8; ++i) {
+#pragma unroll
+                    for (int panel = 0; panel < Ring::kItemPanels; ++panel)
+                        *reinterpret_cast<uint4 *>(smem + slot_offset + panel * kTreePanelBytes + i * 16) = zero;
+                }
+                fence_async_proxy();
+            }
+            if (lane == 0) mbarrier_expect_bytes(bar, fetched * (unsigned)(T * 128 * Ring::kItemPanels));
+            __syncwarp();
+            if (good) {
+#pragma unroll
+                for (int panel = 0; panel < Ring::kItemPanels; ++panel)
+                    tma_load_2d(ring + slot_offset + panel * kTreePanelBytes, map, (item * Ring::kItemPanels + panel) * 64, row0, bar);
+            }
+        }
+        return true;
+    }
+    // copies in flight must land (or be given up, bounded) before shared memory is handed on
+    template <bool kIsV>
+    __device__ __forceinline__ void drain(int count) const
+    {
+        constexpr int slots = kIsV ? Ring::kVSlots : Ring::kKSlots, bar_full = kIsV ? kTreeBarVFull : kTreeBarKFull;
+        for (int i = max(count - slots, 0); i < count; ++i)
+            (void)mbarrier_poll_bounded(misc + bar_full + (i % slots) * 8, (i / slots) & 1);
+    }
+    // The K producer's whole job: K tiles, and behind the first tile of every segment its query rows, kBlocks
+    // row blocks of kQRows rows (64 dims of them per kQPanel bytes) at q_smem.
+    template <int kBlocks, int kQPanel>
+    __device__ __forceinline__ void produce_k(TreeWalk walk, const CUtensorMap *map_q, const CUtensorMap *map_k, unsigned q_smem) const
+    {
+        TreeSegment seg;
+        int count = 0, k = 0;
+        bool fine = true;
+        for (; fine && walk.next(p, seg, lane); ++k) {
+            int ids = fetch_ids(seg, seg.t0);
+            for (int j = seg.t0; j < seg.t1 && fine; ++j) {
+                const int now = ids;
+                ids = fetch_ids(seg, j + 1);
+                fine = copy_tile<false>(seg, j, now, map_k, count);
+                if (j > seg.t0 || !fine) continue;
+                // the query rows wait for the last segment's logits
+                if (k >= 1) fine = __all_sync(0xffffffffu, mbarrier_wait_bounded(misc + kTreeBarQEmpty, (k - 1) & 1));
+                if (fine && lane == 0) {
+                    const int panel_bytes = p.nodes_per_block * p.group * 128;
+                    int blocks = 0;
+#pragma unroll
+                    for (int s = 0; s < kBlocks; ++s) blocks += (seg.rb * kBlocks + s) * p.nodes_per_block < p.tree.tokens;
+                    mbarrier_expect_bytes(misc + kTreeBarQFull, (unsigned)(blocks * panel_bytes * Ring::kPanels));
+#pragma unroll
+                    for (int s = 0; s < kBlocks; ++s) {
+                        const int node0 = (seg.rb * kBlocks + s) * p.nodes_per_block;
+                        if (node0 >= p.tree.tokens) continue;
+#pragma unroll
+                        for (int panel = 0; panel < Ring::kPanels; ++panel)
+                            tma_load_4d(q_smem + (s * Ring::kPanels + panel) * kQPanel, map_q, panel * 64, seg.hk * p.group, node0,
+                                        seg.b, misc + kTreeBarQFull);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        if (!fine) {
+            if (lane == 0 && p.a.status) atomicOr(p.a.status, kFlagCopyTimeout);
+            drain<false>(count);
+            if (k >= 1) (void)mbarrier_poll_bounded(misc + kTreeBarQFull, (k - 1) & 1);
+        }
+    }
+    __device__ __forceinline__ void produce_v(TreeWalk walk, const CUtensorMap *map_v) const
+    {
+        TreeSegment seg;
+        int count = 0;
+        bool fine = true;
+        while (fine && walk.next(p, seg, lane)) {
+            int ids = fetch_ids(seg, seg.t0);
+            for (int j = seg.t0; j < seg.t1 && fine; ++j) {
+                const int now = ids;
+                ids = fetch_ids(seg, j + 1);
+                fine = copy_tile<true>(seg, j, now, map_v, count);
+            }
+        }
+        if (!fine) {
+            if (lane == 0 && p.a.status) atomicOr(p.a.status, kFlagCopyTimeout);
+            drain<true>(count);
+        }
+    }
+    // Rows row0 .. row0 + 31 of the V tile number g of this block (one warp).  Value rows behind the sequence get
+    // weight 0 but may hold anything, and 0 x NaN is NaN: they are cleared.  A node's row that is not finite is
+    // cleared too and noted in `poison`; the rows that see it get it added at the end.
+    __device__ __forceinline__ void clean_values(const TreeSegment &s, int j, int g, int row0, unsigned *poison, bool &fine) const
+    {
+        const int start = j * kTreeTile + row0;
+        if (start + 31 < s.prefix()) return;                          // uniform
+        unsigned char *rows[Ring::kItems];
+#pragma unroll
+        for (int item = 0; item < Ring::kItems; ++item) {
+            const int n = g * Ring::kItems + item, slot = n % Ring::kVSlots;
+            if (fine) fine = mbarrier_poll_bounded(misc + kTreeBarVFull + slot * 8, (n / Ring::kVSlots) & 1);
+            rows[item] = smem + Ring::kVOffset + slot * Ring::kItemBytes + row0 * 128;
+        }
+        __syncwarp();
+        unsigned bad_rows = 0;
+#pragma unroll 1
+        for (int r0 = 0; r0 < 32; r0 += 4) {                          // four rows at a time, 8 lanes a row
+            const int pos = start + r0 + (lane >> 3);
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < Ring::kPanels; ++i)
+                bad = bad || !finite8(*reinterpret_cast<const uint4 *>(rows[i / Ring::kItemPanels] + i % Ring::kItemPanels * kTreePanelBytes +
+                                                                       r0 * 128 + lane * 16));
+            const unsigned found = __ballot_sync(0xffffffffu, bad && pos >= s.prefix() && pos < s.len);
+            const bool mine = (found >> (lane & 24) & 0xffu) != 0;
+            if (mine || pos >= s.len) {
+#pragma unroll
+                for (int i = 0; i < Ring::kPanels; ++i)
+                    *reinterpret_cast<uint4 *>(rows[i / Ring::kItemPanels] + i % Ring::kItemPanels * kTreePanelBytes + r0 * 128 +
+                                               lane * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bad_rows |= (unsigned)((found >> (8 * i) & 0xffu) != 0) << (r0 + i);
+        }
+        fence_async_proxy();
+        if (lane == 0) {
+            for (; bad_rows != 0; bad_rows &= bad_rows - 1) {
+                const int node = start + __ffs(bad_rows) - 1 - s.prefix();
+                atomicOr(poison + (node >> 5), 1u << (node & 31));
+            }
+        }
+        __syncwarp();
+    }
+};
+
+// What row `r` of a segment's first row block (of the only one, for the kernel with the tokens as the long side)
+// or `row` sees of the value rows that were taken out of its tiles (rare): weights against the row's
+// log-sum-exp.  Adds dims d0 .. d0 + 31 to o, or returns dim d.
+__device__ __forceinline__ float tree_stray_weight(const AttnParams &a, const TreeSegment &s, int64_t out_row, int64_t kv_row, int D, float lse2)
+{
+    float dot = 0.f;
+    for (int c = 0; c < D; ++c) dot = fmaf(__half2float(a.q[out_row * D + c]), __half2float(a.k[kv_row * D + c]), dot);
+    return fast_exp2(dot * a.scale_log2e - lse2);
+}
+static __device__ __noinline__ void tree_add_poisoned(const AttnParams &a, const TreeSegment &s, const TreeRow &row, const unsigned *poison,
+                                               int64_t out_row, int D, int d0, float lse2, float *o)
+{
+    for (int n = 0; n < s.nodes; ++n) {
+        if (!(poison[n >> 5] >> (n & 31) & 1u) || !row.sees(n)) continue;
+        const int64_t kv_row = tree_cache_row(a, s.b, s.hk, s.prefix() + n);
+        const float weight = tree_stray_weight(a, s, out_row, kv_row, D, lse2);
+        for (int c = 0; c < 32; ++c) o[c] += weight * __half2float(a.v[kv_row * D + d0 + c]);
+    }
+}
+static __device__ __noinline__ float tree_poisoned_value(const TreeParams &p, const TreeSegment &s, const unsigned *poison, int r, int D, int d,
+                                                  float lse2)
+{
+    const AttnParams &a = p.a;
+    const int node = r / p.group;
+    const TreeRow row = tree_row(p.tree, s.b, node, s.nodes);
+    const int64_t out_row = ((int64_t)s.b * p.tree.tokens + node) * ((int64_t)a.heads * p.group) + (int64_t)s.hk * p.group + (r - node * p.group);
+    float value = 0.f;
+    for (int n = 0; n < s.nodes; ++n) {
+        if (!(poison[n >> 5] >> (n & 31) & 1u) || !row.sees(n)) continue;
+        const int64_t kv_row = tree_cache_row(a, s.b, s.hk, s.prefix() + n);
+        value += tree_stray_weight(a, s, out_row, kv_row, D, lse2) * __half2float(a.v[kv_row * D + d]);
+    }
+    return value;
+}
+
+// The barriers that the kernels have in common, and the poison words (one thread).
+__device__ __forceinline__ void tree_init_barriers(unsigned misc, unsigned char *misc_ptr, int softmax_warps)
+{
+#pragma unroll
+    for (int s = 0; s < 6; ++s) {
+        mbarrier_init(misc + kTreeBarKFull + s * 8, 1);
+        mbarrier_init(misc + kTreeBarKEmpty + s * 8, 1);
+        mbarrier_init(misc + kTreeBarVFull + s * 8, 1);
+        mbarrier_init(misc + kTreeBarVEmpty + s * 8, 1);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        mbarrier_init(misc + kTreeBarSFull + s * 8, 1);
+        mbarrier_init(misc + kTreeBarPFull + s * 8, softmax_warps);
+        mbarrier_init(misc + kTreeBarPvDone + s * 8, 1);
+        mbarrier_init(misc + kTreeBarSFree + s * 8, softmax_warps);
+    }
+    mbarrier_init(misc + kTreeBarQFull, 1);
+    mbarrier_init(misc + kTreeBarQEmpty, 1);
+    mbarrier_init_fence();
+    for (int i = 0; i < 32; ++i) reinterpret_cast<unsigned *>(misc_ptr + kTreePoison)[i] = 0u;
+}
+
+// Joins the partial results of the items that more than one block worked on, and zeroes the rows of
+// sequences without work; one thread block per item and kTreeMergeRows rows, one warp per row.
+constexpr int kTreeMergeThreads = 128;
+constexpr int kTreeMergeRows = 16;
+
+template <int D>
+__global__ void __launch_bounds__(kTreeMergeThreads)
+tree_merge_kernel(const TreeParams p, int blocks, int row_parts)
+{
+    const AttnParams &a = p.a;
+    __shared__ int64_t sums[2][kTreeMergeThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int part = blockIdx.x % row_parts;
+    const int item = blockIdx.x / row_parts;                          // (sequence, KV head, row block)
+    const int items = a.heads * p.row_blocks;
+    const int b = item / items, in_seq = item - b * items;
+    const int hk = in_seq / p.row_blocks, rb = in_seq - hk * p.row_blocks;
+    allow_next_kernel();
+    wait_for_previous_kernels();
+    int nodes;
+    const int len = checked_tree(p.tree, a.seq_lens, a.max_seq_len, nullptr, b, false, nodes);
+    const int n_tiles = tree_tiles(len, nodes);
+    int c0 = 0, c1 = 0;
+    if (n_tiles > 0) {
+        // tiles before this sequence, and all of them
+        int64_t before = 0, all = 0;
+        for (int i = threadIdx.x; i < p.batch; i += kTreeMergeThreads) {
+            int n;
+            const int other = checked_tree(p.tree, a.seq_lens, a.max_seq_len, nullptr, i, false, n);
+            const int64_t tiles = (int64_t)tree_tiles(other, n) * items;
+            if (i < b) before += tiles;
+            all += tiles;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            before += __shfl_xor_sync(0xffffffffu, before, o);
+            all += __shfl_xor_sync(0xffffffffu, all, o);
+        }
+        if (lane == 0) {
+            sums[0][warp] = before;
+            sums[1][warp] = all;
+        }
+        __syncthreads();
+        before = all = 0;
+        for (int w = 0; w < kTreeMergeThreads / 32; ++w) {
+            before += sums[0][w];
+            all += sums[1][w];
+        }
+        const int64_t first = before + (int64_t)in_seq * n_tiles, last = first + n_tiles - 1;
+        auto block_of = [&](int64_t tile) -> int {
+            int c = (int)(tile * min((int64_t)blocks, all) / all);
+            while (tree_first_tile(all, c + 1, blocks) <= tile) ++c;
+            while (tree_first_tile(all, c, blocks) > tile) --c;
+            return c;
+        };
+        c0 = block_of(first);
+        c1 = block_of(last);
+        if (c0 == c1) return;                                         // one block had it all: the result is written
+    }
+    constexpr int kPer = D / 32;                                      // dims per lane
+    for (int r = part * kTreeMergeRows + warp; r < min((part + 1) * kTreeMergeRows, p.item_rows); r += kTreeMergeThreads / 32) {
+        const int node = rb * (p.item_rows / p.group) + r / p.group, head = r % p.group;
+        if (node >= p.tree.tokens) continue;
+        const int64_t out_row = ((int64_t)b * p.tree.tokens + node) * ((int64_t)a.heads * p.group) + (int64_t)hk * p.group + head;
+        float top = kMinusHuge, total = 0.f, acc[kPer];
+        bool any_nan = false;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
+        auto slot_row = [&](int c) -> int64_t { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * p.item_rows + r; };
+        if (n_tiles > 0) {
+            for (int c = c0; c <= c1; ++c) {
+                const float lse = a.part_lse[slot_row(c)];
+                top = fmaxf(top, lse);
+                any_nan = any_nan || lse != lse;
+            }
+            if (top > kMinusHuge || any_nan) {
+                for (int c = c0; c <= c1; ++c) {
+                    const float w = fast_exp2(a.part_lse[slot_row(c)] - top);
+                    total += w;
+                    const float *from = a.part_o + slot_row(c) * D + lane * kPer;
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) acc[i] = fmaf(w, from[i], acc[i]);
+                }
+            }
+        }
+        const bool empty = !(top > kMinusHuge) && !any_nan;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) a.out[out_row * D + lane * kPer + i] = __float2half_rn(empty ? 0.f : acc[i] / total);
+        if (a.lse && lane == 0) a.lse[out_row] = empty ? -INFINITY : (top + log2f(total)) * kLn2;
+    }
+}
+
+}  // namespace instinfer
