@@ -20,11 +20,14 @@ int tree_attention_shape(int32_t batch, int32_t tree_tokens, int32_t q_heads, in
 
 // ---- the tcgen05 form ----
 
+// Rows of the partial results: two slots per piece, at most 1 + short_pieces pieces per block and one more; the
+// ticket counter lies behind them.
+size_t tree_slot_rows(const TreeRows &r) { return (size_t)2 * (sm_count() * (1 + r.short_pieces) + 1) * r.item_rows; }
+
 size_t tree_umma_workspace(int32_t tree_tokens, int32_t group, int32_t head_dim)
 {
     if (group > kTreeTile) return 0;
-    const size_t rows = (size_t)2 * sm_count() * tree_rows(tree_tokens, group, head_dim).item_rows;
-    return (rows * (head_dim + 1) * sizeof(float) + 255) / 256 * 256;
+    return (tree_slot_rows(tree_rows(tree_tokens, group, head_dim)) * (head_dim + 1) * sizeof(float) + 255) / 256 * 256 + 256;
 }
 
 // Blocks of 16, 32 or 64 tokens, or of a multiple of 128: no tile straddles blocks of another kind.
@@ -109,12 +112,15 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
         const int row_parts = (rows.item_rows + kTreeMergeRows - 1) / kTreeMergeRows;
         const int32_t box = paged && block_tokens < kTreeTile ? block_tokens : kTreeTile;
         TreeLaunch t = {};
-        if (items * row_parts < (int64_t)1 << 31 &&
+        if (items * row_parts < (int64_t)1 << 31 && items * ceil_div(max_seq_len, kTreeTile) < (int64_t)1 << 31 &&
             make_query_map(&t.map_q, q, batch, tree_tokens, q_heads, p.group, head_dim, rows.nodes_per_block) &&
             make_cache_map(&t.map_k, k_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box) &&
             make_cache_map(&t.map_v, v_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box)) {
             t.p.a = p.a;
-            t.p.a.part_lse = p.a.part_o + (size_t)2 * sm_count() * rows.item_rows * head_dim;
+            t.p.a.part_lse = p.a.part_o + tree_slot_rows(rows) * head_dim;
+            t.p.short_pieces = rows.short_pieces;
+            t.p.ticket = reinterpret_cast<unsigned *>(static_cast<unsigned char *>(workspace) +
+                                                      tree_umma_workspace(tree_tokens, p.group, head_dim) - 256);
             t.p.tree = p.tree;
             t.p.batch = batch;
             t.p.group = p.group;
@@ -125,6 +131,7 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
             t.grid = (unsigned)(most_tiles < sm_count() ? most_tiles : sm_count());
             t.merge_grid = (unsigned)(items * row_parts);
             t.row_parts = row_parts;
+            t.draws = most_tiles >= (int64_t)kTreeDrawnTiles * t.grid;
             t.stream = stream;
             switch (head_dim) {
             case 64: return paged ? launch_tree<64, true>(rows, t) : launch_tree<64, false>(rows, t);

@@ -22,6 +22,10 @@ int launch_tree_umma(const TreeLaunch &t)
         }
         done[dev] = true;
     }
+    if (t.draws && cudaMemsetAsync(t.p.ticket, 0, sizeof(unsigned), t.stream) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return INSTINFER_ERR_CUDA;
+    }
     cudaError_t err = launch_overlapped(kKernel, t.grid, kThreadsOf, kSmem, t.stream, t.p, t.map_q, t.map_k, t.map_v);
     if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) return INSTINFER_ERR_CUDA;
     err = launch_overlapped(tree_merge_kernel<D>, t.merge_grid, kTreeMergeThreads, 0, t.stream, t.p, (int)t.grid, t.row_parts);

@@ -14,6 +14,7 @@ namespace api {
 struct TreeRows {
     int32_t columns;              // 16, 32 or 64; 0: the kernel with the rows as the long side
     int32_t streams, nodes_per_block, row_blocks, item_rows;
+    int32_t short_pieces;         // drawn pieces per block: fewer where a partial result is larger
 };
 inline TreeRows tree_rows(int32_t tree_tokens, int32_t group, int32_t head_dim)
 {
@@ -26,6 +27,7 @@ inline TreeRows tree_rows(int32_t tree_tokens, int32_t group, int32_t head_dim)
     r.row_blocks = (blocks + r.streams - 1) / r.streams;
     r.nodes_per_block = (tree_tokens + r.row_blocks * r.streams - 1) / (r.row_blocks * r.streams);
     r.item_rows = r.streams * r.nodes_per_block * group;
+    r.short_pieces = r.columns ? 4 : 2;
     return r;
 }
 
@@ -34,6 +36,7 @@ struct TreeLaunch {
     CUtensorMap map_q, map_k, map_v;
     unsigned grid, merge_grid;
     int row_parts;
+    bool draws;                   // there may be enough tiles for drawn pieces
     cudaStream_t stream;
 };
 

@@ -1,14 +1,19 @@
 // What the tcgen05 kernels for draft trees share (tree_umma_rows.cuh, tree_umma_tokens.cuh), for sm_100a: the
 // split of the work, the walk through it, the copies, and the merge of partial results.
 //
-// Work split: the tiles of 128 tokens of all (sequence, KV head, row block) items lie in one row, and
-// block c of G takes the tiles [W c / G, W (c + 1) / G) of the W there are, whatever items they belong
-// to.  So every SM reads the same number of bytes, and only the items that a block starts or ends inside
-// leave partial results: at most two per block (with fixed chunks the partials of a 16-sequence batch of
-// 64 rows were 8 % of the traffic).  The cuts follow from the lengths alone, not from the placement of blocks.
+// Work split: the tiles of 128 tokens of all (sequence, KV head, row block) items lie in one row of W tiles,
+// which is cut into pieces whatever items they belong to: first one long piece per block, 11/16 of the
+// tiles together, then short ones that the blocks draw from a ticket counter.  Only the items that a
+// piece starts or ends inside leave partial results, two per piece at most (with the fixed chunks of the
+// other kernels the partials of 64 rows are 8 % of the traffic).  Why not equal shares alone: the SMs do not reach
+// memory equally fast, with equal shares of 207 tiles the first was done after 312 us and the last after 399.
+// Few tiles are cut into equal shares, one per block.  The cuts follow from the lengths alone, so a result
+// depends neither on which block draws a piece nor on the placement of the cache's blocks.
 //
 // A block has softmax warps and four single-purpose warps, which hand tiles over through mbarriers:
-//   K producer, V producer   tensor-map copies into a ring each (128-byte swizzle); a paged tile is 128 / T
+//   K producer               draws the pieces and announces their segments (a piece's part of one item) to the
+//                            others through a queue in shared memory; copies K tiles and query rows;
+//   V producer               the V tiles.  Both: tensor-map copies into a ring each (128-byte swizzle); a paged tile is 128 / T
 //                            copies of one (block, head) run; unreadable blocks are zero-filled;
 //   logit and output issuer  one elected thread each issues the MMAs of the logits and of the output.
 // Every wait is bounded by the clock; one that runs out sets kFlagCopyTimeout, after which that warp
@@ -22,6 +27,20 @@ namespace instinfer {
 
 constexpr int kTreeTile = 128;                         // tokens per tile
 constexpr int kTreePanelBytes = kTreeTile * 128;       // 64 dims of 128 rows
+
+// Bounded waits with the loop out of line (see mbarrier_wait_bounded and mbarrier_poll_bounded): the first test
+// succeeds more often than not, and some thirty of them are in each kernel.
+static __device__ __noinline__ bool tree_wait_more(unsigned bar, unsigned parity) { return mbarrier_wait_bounded(bar, parity); }
+static __device__ __noinline__ bool tree_poll_more(unsigned bar, unsigned parity)
+{
+    const long long start = clock64();
+    for (;;) {
+        if (mbarrier_test(bar, parity)) return true;
+        if (clock64() - start > kWaitCycles) return false;
+    }
+}
+__device__ __forceinline__ bool tree_wait(unsigned bar, unsigned parity) { return mbarrier_test(bar, parity) || tree_wait_more(bar, parity); }
+__device__ __forceinline__ bool tree_poll(unsigned bar, unsigned parity) { return mbarrier_test(bar, parity) || tree_poll_more(bar, parity); }
 
 // Ring geometry of a head size: an item is up to 128 dims of a tile (32 KiB; 16 KiB at head size 64).
 template <int D, int kBytes>
@@ -50,11 +69,14 @@ constexpr int kTreeBarQFull = 240;
 constexpr int kTreeBarQEmpty = 248;
 constexpr int kTreeBarSFree = 256;     // [2] the logits have been read
 constexpr int kTreeTmemPtr = 272;
-constexpr int kTreeStart = 288;        // where the block's tiles begin: sequence, tile inside it (64 bits), number of tiles
-constexpr int kTreePoison = 320;       // [8][4] words: nodes of a segment whose value row is not finite, by segment number
-constexpr int kTreeScan = 448;         // [16] int64: per-warp sums of the set-up's scan
-constexpr int kTreeMiscBytes = 576;
-static_assert(kTreeScan + 16 * 8 <= kTreeMiscBytes && kTreeMiscBytes % 16 == 0, "misc region too small");
+constexpr int kTreeTotal = 280;        // number of tiles
+constexpr int kTreeBarSegFull = 288;   // [4] a segment is announced
+constexpr int kTreeBarSegEmpty = 320;  // [4] everyone is done with it
+constexpr int kTreePoison = 352;       // [8][4] words: nodes of a segment whose value row is not finite, by segment number
+constexpr int kTreeSegments = 480;     // [4] TreeSegment
+constexpr int kTreeScan = 480;         // [16] ints: per-warp sums of the set-up's scan, before the first segment
+constexpr int kTreeMiscBytes = 480 + 4 * 48;
+static_assert(kTreeScan + 16 * 4 <= kTreeMiscBytes && kTreeMiscBytes % 16 == 0, "misc region too small");
 
 struct TreeParams {
     AttnParams a;              // heads = KV heads; part_o [2 G, item_rows, D], part_lse [2 G, item_rows]
@@ -64,6 +86,8 @@ struct TreeParams {
     int32_t nodes_per_block;   // a row block is this many nodes' heads: row t * group + g of the block
     int32_t row_blocks;        // items per (sequence, KV head), of one or two row blocks each
     int32_t item_rows;         // rows of an item: all its row blocks'
+    int32_t short_pieces;      // drawn pieces per block
+    unsigned *ticket;          // zero before the launch where W can reach kTreeDrawnTiles per block
 };
 
 // Number of tiles of a sequence's items.
@@ -72,125 +96,153 @@ __device__ __forceinline__ int tree_tiles(int len, int nodes)
     return nodes > 0 ? (int)(((unsigned)len + kTreeTile - 1) / kTreeTile) : 0;
 }
 
-// The tile at which block `c` of `blocks` starts; blocks beyond the number of tiles have none.
-__device__ __forceinline__ int64_t tree_first_tile(int64_t total, int c, int blocks)
-{
-    const int64_t working = min((int64_t)blocks, total);
-    return c < working ? total * c / working : total;
-}
+// The cut of the row of tiles (see above); piece c is [first(c), first(c + 1)), count() pieces in all.
+constexpr int kTreeDrawnTiles = 24;    // tiles per block from which on pieces are drawn
+struct TreePieces {
+    int total, length, drawn;          // W; tiles of a long piece; first tile of the short pieces
+    int blocks, step;                  // step: tiles of a short piece, 0: none
+    __device__ __forceinline__ TreePieces(int total_, int grid, int short_pieces)
+        : total(total_), length(0), drawn(0), blocks(min(grid, total_)), step(0)
+    {
+        if (total / kTreeDrawnTiles < grid) return;
+        length = total / blocks * 11 / 16;
+        drawn = length * blocks;
+        const int pieces = short_pieces * blocks;
+        step = (total - drawn + pieces - 1) / pieces;
+    }
+    __device__ __forceinline__ int count() const { return step == 0 ? blocks : blocks + (total - drawn + step - 1) / step; }
+    __device__ __forceinline__ int first(int c) const
+    {
+        // (equal shares: the first total % blocks ones are one tile longer)
+        if (step == 0) return c < blocks ? total / blocks * c + min(c, total % blocks) : total;
+        return c <= blocks ? length * c : min(total, drawn + (c - blocks) * step);
+    }
+    __device__ __forceinline__ int piece_of(int tile) const
+    {
+        if (step > 0) return tile < drawn ? tile / length : blocks + (tile - drawn) / step;
+        const int share = total / blocks, longer = total % blocks;
+        return tile < longer * (share + 1) ? tile / (share + 1) : longer + (tile - longer * (share + 1)) / share;
+    }
+};
 
-// Tiles [t0, t1) of the n_tiles of one item.
+// Tiles [t0, t1) of the n_tiles of one item; b < 0: no more.  `slot`: where its partial result goes: what starts
+// inside an item goes to its piece's first slot, what ends inside one to its second.
 struct TreeSegment {
-    int b, len, nodes, hk, rb, t0, t1, n_tiles;
+    int b, len, nodes, hk, rb, t0, t1, n_tiles, slot;
     __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == n_tiles; }
     __device__ __forceinline__ int prefix() const { return len - nodes; }
 };
+static_assert(sizeof(TreeSegment) <= 48, "queue entry");
 
-// The segments of one block, in order; every warp walks them by itself (all 32 lanes together).
-struct TreeWalk {
-    int b, len, nodes, item, tile;
-    int64_t left;
-    __device__ __forceinline__ void find(const TreeParams &p, int from, int lane)
+// Draws this block's pieces and finds their segments (all 32 lanes of one warp together).  Out of line: the kernel's
+// loops should stay in the instruction cache.
+struct TreeFinder {
+    TreePieces pieces;
+    int n_pieces, piece, tile, end;
+    unsigned drawn;                // lane 0: the next piece, asked for when this one began
+    int b, len, nodes;             // a sequence with tiles ...
+    int base, limit;               // ... the row's tiles [base, limit)
+    __device__ __forceinline__ TreeFinder() : pieces(0, 1, 1) {}
+    __device__ __noinline__ void start(const TreeParams &p, int total, int lane)
     {
-        // the next sequence from `from` on that has tiles (there is one as long as `left` is not 0)
-        for (b = from; b < p.batch; b += 32) {
+        pieces = TreePieces(total, gridDim.x, p.short_pieces);
+        n_pieces = pieces.count();
+        b = -1;
+        len = nodes = base = limit = 0;
+        begin(p, (int)blockIdx.x < pieces.blocks ? blockIdx.x : n_pieces, lane);
+    }
+    __device__ __forceinline__ void begin(const TreeParams &p, int which, int lane)
+    {
+        piece = min(which, n_pieces);
+        tile = end = 0;
+        drawn = n_pieces;
+        if (piece >= n_pieces) return;
+        tile = pieces.first(piece);
+        end = pieces.first(piece + 1);
+        if (lane == 0 && pieces.step > 0) drawn = pieces.blocks + atomicAdd(p.ticket, 1u);
+    }
+    __device__ __noinline__ TreeSegment next(const TreeParams &p, int lane)
+    {
+        TreeSegment s;
+        s.b = -1;
+        if (tile >= end && piece < n_pieces) {
+            const unsigned got = __shfl_sync(0xffffffffu, drawn, 0);
+            begin(p, got < (unsigned)n_pieces ? (int)got : n_pieces, lane);
+        }
+        if (piece >= n_pieces) return s;
+        const int items = p.a.heads * p.row_blocks;
+        while (tile >= limit) {    // (tile < W: some sequence has it)
+            const int from = b + 1;
+            if (from >= p.batch) return s;
             int n = 0, l = 0;
-            if (b + lane < p.batch) l = checked_tree(p.tree, p.a.seq_lens, p.a.max_seq_len, nullptr, b + lane, false, n);
-            const unsigned live = __ballot_sync(0xffffffffu, tree_tiles(l, n) > 0);
-            if (live == 0) continue;
-            const int first = __ffs(live) - 1;
-            b += first;
-            len = __shfl_sync(0xffffffffu, l, first);
-            nodes = __shfl_sync(0xffffffffu, n, first);
-            return;
+            if (from + lane < p.batch) l = checked_tree(p.tree, p.a.seq_lens, p.a.max_seq_len, nullptr, from + lane, false, n);
+            const int mine = tree_tiles(l, n) * items;
+            int sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += up;
+            }
+            const unsigned reached = __ballot_sync(0xffffffffu, limit + sum > tile);
+            const int at = reached ? __ffs(reached) - 1 : 31;
+            len = __shfl_sync(0xffffffffu, l, at);
+            nodes = __shfl_sync(0xffffffffu, n, at);
+            base = limit + __shfl_sync(0xffffffffu, sum - mine, at);
+            limit = limit + __shfl_sync(0xffffffffu, sum, at);
+            b = from + at;
         }
-        left = 0;
-    }
-    __device__ __forceinline__ void start(const TreeParams &p, const unsigned char *misc, int lane)
-    {
-        const int *at = reinterpret_cast<const int *>(misc + kTreeStart);
-        const int64_t inside = *reinterpret_cast<const int64_t *>(misc + kTreeStart + 8);
-        left = *reinterpret_cast<const int64_t *>(misc + kTreeStart + 16);
-        find(p, at[0], lane);
-        const int n = tree_tiles(len, nodes);
-        item = n > 0 ? (int)(inside / n) : 0;
-        tile = n > 0 ? (int)(inside - (int64_t)item * n) : 0;
-    }
-    __device__ __forceinline__ bool next(const TreeParams &p, TreeSegment &s, int lane)
-    {
-        if (left > 0 && item == p.a.heads * p.row_blocks) {
-            find(p, b + 1, lane);
-            item = 0;
-            tile = 0;
-        }
-        if (left <= 0) return false;
-        s.b = b;
         s.len = len;
         s.nodes = nodes;
+        s.n_tiles = tree_tiles(len, nodes);
+        if (b >= p.batch || s.n_tiles == 0) return s;         // (lengths that change under the kernel's hands)
+        s.b = b;
+        const int inside = tile - base, item = inside / s.n_tiles;
         s.hk = item / p.row_blocks;
         s.rb = item - s.hk * p.row_blocks;
-        s.n_tiles = tree_tiles(len, nodes);
-        s.t0 = tile;
-        s.t1 = (int)min((int64_t)s.n_tiles, tile + left);
-        left -= s.t1 - s.t0;
-        tile = s.t1;
-        if (tile == s.n_tiles) {
-            tile = 0;
-            ++item;
-        }
-        return true;
+        s.t0 = inside - item * s.n_tiles;
+        s.t1 = min(s.n_tiles, s.t0 + (end - tile));
+        s.slot = 2 * piece + (s.t0 == 0 ? 1 : 0);
+        tile += s.t1 - s.t0;
+        return s;
     }
 };
 
-// Finds where this block's tiles begin and leaves it in the misc region (all threads; the caller
-// synchronises before a walk starts).
-__device__ __forceinline__ void tree_find_start(const TreeParams &p, unsigned char *misc_ptr, int threads)
+// The announced segments, for the warps that work on them: segment k of the block is entry k % 4.
+struct TreeQueue {
+    unsigned misc;
+    unsigned char *misc_ptr;
+    __device__ __forceinline__ TreeSegment &entry(int k) const { return reinterpret_cast<TreeSegment *>(misc_ptr + kTreeSegments + (k & 3) * 48)[0]; }
+    // Waits for segment k (all lanes); false if the wait ran out.
+    __device__ __forceinline__ bool wait(int k) const
+    {
+        return __all_sync(0xffffffffu, tree_wait(misc + kTreeBarSegFull + (k & 3) * 8, (k >> 2) & 1));
+    }
+    __device__ __forceinline__ void done(int k, int lane) const
+    {
+        __syncwarp();
+        if (lane == 0) mbarrier_arrive(misc + kTreeBarSegEmpty + (k & 3) * 8);
+    }
+};
+
+// Adds up all sequences' tiles and leaves the sum in the misc region (all threads; the caller synchronises).
+__device__ __forceinline__ void tree_count_tiles(const TreeParams &p, unsigned char *misc_ptr, int threads)
 {
-    const AttnParams &a = p.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int per_thread = (p.batch + threads - 1) / threads;
-    const int b0 = min((int)threadIdx.x * per_thread, p.batch), b1 = min(b0 + per_thread, p.batch);
-    const int items = a.heads * p.row_blocks;
-    int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) {
+    int mine = 0;                      // (all tiles are fewer than 2^31: checked by the host)
+    for (int b = threadIdx.x; b < p.batch; b += threads) {
         int nodes;
-        const int len = checked_tree(p.tree, a.seq_lens, a.max_seq_len, a.status, b, blockIdx.x == 0, nodes);
-        mine += (int64_t)tree_tiles(len, nodes) * items;
+        const int len = checked_tree(p.tree, p.a.seq_lens, p.a.max_seq_len, p.a.status, b, blockIdx.x == 0, nodes);
+        mine += tree_tiles(len, nodes);
     }
-    int64_t run = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t up = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += up;
-    }
-    int64_t *scan = reinterpret_cast<int64_t *>(misc_ptr + kTreeScan);
-    if (lane == 31) scan[warp] = run;
-    if (threadIdx.x == 0) {                        // no tiles, unless a thread finds the first one below
-        *reinterpret_cast<int *>(misc_ptr + kTreeStart) = 0;
-        *reinterpret_cast<int64_t *>(misc_ptr + kTreeStart + 8) = 0;
-        *reinterpret_cast<int64_t *>(misc_ptr + kTreeStart + 16) = 0;
-    }
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    int *scan = reinterpret_cast<int *>(misc_ptr + kTreeScan);
+    if (lane == 0) scan[warp] = mine;
     __syncthreads();
-    int64_t before = 0, total = 0;
-    for (int w = 0; w < threads / 32; ++w) {
-        if (w < warp) before += scan[w];
-        total += scan[w];
-    }
-    const int64_t first = tree_first_tile(total, blockIdx.x, gridDim.x), last = tree_first_tile(total, blockIdx.x + 1, gridDim.x);
-    int64_t at = before + run - mine;
-    if (first < last && at <= first && first < at + mine) {
-        for (int b = b0; b < b1; ++b) {
-            int nodes;
-            const int len = checked_tree(p.tree, a.seq_lens, a.max_seq_len, nullptr, b, false, nodes);
-            const int64_t n = (int64_t)tree_tiles(len, nodes) * items;
-            if (first < at + n) {
-                *reinterpret_cast<int *>(misc_ptr + kTreeStart) = b;
-                *reinterpret_cast<int64_t *>(misc_ptr + kTreeStart + 8) = first - at;
-                *reinterpret_cast<int64_t *>(misc_ptr + kTreeStart + 16) = last - first;
-                break;
-            }
-            at += n;
-        }
+    if (threadIdx.x == 0) {
+        int total = 0;
+        for (int w = 0; w < threads / 32; ++w) total += scan[w];
+        *reinterpret_cast<int *>(misc_ptr + kTreeTotal) = total * p.a.heads * p.row_blocks;
     }
 }
 
@@ -350,12 +402,13 @@ struct TreeCopies {
         for (int item = 0; item < Ring::kItems; ++item, ++count) {
             const int slot = count % slots;
             if (count >= slots &&
-                !__all_sync(0xffffffffu, mbarrier_wait_bounded(misc + bar_empty + slot * 8, (count / slots - 1) & 1)))
+                !__all_sync(0xffffffffu, tree_wait(misc + bar_empty + slot * 8, (count / slots - 1) & 1)))
                 return false;
             const int slot_offset = ring_offset + slot * Ring::kItemBytes + (kPaged ? lane * T * 128 : 0);
             const unsigned bar = misc + bar_full + slot * 8;
             if (kPaged && lane < nb && !good) {                   // a block that cannot be read counts as zeros
                 const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
                 for (int i = 0; i < T * 8; ++i) {
 #pragma unroll
                     for (int panel = 0; panel < Ring::kItemPanels; ++panel)
@@ -379,25 +432,40 @@ struct TreeCopies {
     {
         constexpr int slots = kIsV ? Ring::kVSlots : Ring::kKSlots, bar_full = kIsV ? kTreeBarVFull : kTreeBarKFull;
         for (int i = max(count - slots, 0); i < count; ++i)
-            (void)mbarrier_poll_bounded(misc + bar_full + (i % slots) * 8, (i / slots) & 1);
+            (void)tree_poll(misc + bar_full + (i % slots) * 8, (i / slots) & 1);
     }
-    // The K producer's whole job: K tiles, and behind the first tile of every segment its query rows, kBlocks
-    // row blocks of kQRows rows (64 dims of them per kQPanel bytes) at q_smem.
+    // The K producer's whole job: draws the pieces, announces their segments, copies the K tiles, and behind the
+    // first tile of every segment its query rows, kBlocks row blocks (64 dims of one per kQPanel bytes) at q_smem.
     template <int kBlocks, int kQPanel>
-    __device__ __forceinline__ void produce_k(TreeWalk walk, const CUtensorMap *map_q, const CUtensorMap *map_k, unsigned q_smem) const
+    __device__ __forceinline__ void produce_k(const TreeQueue &queue, const CUtensorMap *map_q, const CUtensorMap *map_k, unsigned q_smem) const
     {
-        TreeSegment seg;
+        TreeFinder finder;
+        finder.start(p, *reinterpret_cast<const int *>(queue.misc_ptr + kTreeTotal), lane);
         int count = 0, k = 0;
         bool fine = true;
-        for (; fine && walk.next(p, seg, lane); ++k) {
-            int ids = fetch_ids(seg, seg.t0);
+        // Segments are found one ahead, while the copies of the one before wait for their slots: lengths, block ids
+        // and the ticket's answer come from a busy memory system, some 2000 cycles each.
+        auto announce = [&](const TreeSegment &s, int n) -> bool {
+            if (n >= 4 && !__all_sync(0xffffffffu, tree_wait(misc + kTreeBarSegEmpty + (n & 3) * 8, ((n >> 2) - 1) & 1))) return false;
+            if (lane == 0) {
+                queue.entry(n) = s;
+                mbarrier_arrive(misc + kTreeBarSegFull + (n & 3) * 8);
+            }
+            return true;
+        };
+        TreeSegment seg = finder.next(p, lane);
+        (void)announce(seg, 0);
+        int ids = seg.b >= 0 ? fetch_ids(seg, seg.t0) : -1;
+        for (; fine && seg.b >= 0; ++k) {
+            TreeSegment after;
+            int ids_after = -1;
             for (int j = seg.t0; j < seg.t1 && fine; ++j) {
                 const int now = ids;
                 ids = fetch_ids(seg, j + 1);
                 fine = copy_tile<false>(seg, j, now, map_k, count);
                 if (j > seg.t0 || !fine) continue;
                 // the query rows wait for the last segment's logits
-                if (k >= 1) fine = __all_sync(0xffffffffu, mbarrier_wait_bounded(misc + kTreeBarQEmpty, (k - 1) & 1));
+                if (k >= 1) fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarQEmpty, (k - 1) & 1));
                 if (fine && lane == 0) {
                     const int panel_bytes = p.nodes_per_block * p.group * 128;
                     int blocks = 0;
@@ -415,50 +483,81 @@ struct TreeCopies {
                     }
                 }
                 __syncwarp();
+                after = finder.next(p, lane);
+                fine = fine && announce(after, k + 1);
+                if (after.b >= 0) ids_after = fetch_ids(after, after.t0);
             }
+            if (!fine) break;
+            seg = after;
+            ids = ids_after;
         }
         if (!fine) {
             if (lane == 0 && p.a.status) atomicOr(p.a.status, kFlagCopyTimeout);
             drain<false>(count);
-            if (k >= 1) (void)mbarrier_poll_bounded(misc + kTreeBarQFull, (k - 1) & 1);
+            (void)tree_poll(misc + kTreeBarQFull, k & 1);     // (the query rows of this segment, if they were asked for)
         }
     }
-    __device__ __forceinline__ void produce_v(TreeWalk walk, const CUtensorMap *map_v) const
+    __device__ __forceinline__ void produce_v(const TreeQueue &queue, const CUtensorMap *map_v) const
     {
+        int count = 0, k = 0;
+        bool fine = queue.wait(0);
+        auto take = [&](int n) -> TreeSegment {
+            const TreeSegment s = queue.entry(n);
+            queue.done(n, lane);
+            return s;
+        };
         TreeSegment seg;
-        int count = 0;
-        bool fine = true;
-        while (fine && walk.next(p, seg, lane)) {
-            int ids = fetch_ids(seg, seg.t0);
+        seg.b = -1;
+        if (fine) seg = take(0);
+        int ids = seg.b >= 0 ? fetch_ids(seg, seg.t0) : -1;
+        for (; fine && seg.b >= 0; ++k) {
+            TreeSegment after;
+            bool have = false;                        // the next segment is announced by now, and its first ids are asked for
+            int ids_after = -1;
             for (int j = seg.t0; j < seg.t1 && fine; ++j) {
                 const int now = ids;
                 ids = fetch_ids(seg, j + 1);
                 fine = copy_tile<true>(seg, j, now, map_v, count);
+                if (!have && fine) have = __all_sync(0xffffffffu, mbarrier_test(misc + kTreeBarSegFull + ((k + 1) & 3) * 8, ((k + 1) >> 2) & 1));
+                else continue;
+                if (have) {
+                    after = take(k + 1);
+                    if (after.b >= 0) ids_after = fetch_ids(after, after.t0);
+                }
             }
+            if (!have && fine) {
+                fine = queue.wait(k + 1);
+                if (!fine) break;
+                after = take(k + 1);
+                if (after.b >= 0) ids_after = fetch_ids(after, after.t0);
+            }
+            seg = after;
+            ids = ids_after;
         }
         if (!fine) {
             if (lane == 0 && p.a.status) atomicOr(p.a.status, kFlagCopyTimeout);
             drain<true>(count);
         }
     }
-    // Rows row0 .. row0 + 31 of the V tile number g of this block (one warp).  Value rows behind the sequence get
+    // Rows row0 .. row0 + kRows - 1 of the V tile number g of this block (one warp).  Value rows behind the sequence get
     // weight 0 but may hold anything, and 0 x NaN is NaN: they are cleared.  A node's row that is not finite is
     // cleared too and noted in `poison`; the rows that see it get it added at the end.
+    template <int kRows>
     __device__ __forceinline__ void clean_values(const TreeSegment &s, int j, int g, int row0, unsigned *poison, bool &fine) const
     {
         const int start = j * kTreeTile + row0;
-        if (start + 31 < s.prefix()) return;                          // uniform
+        if (start + kRows - 1 < s.prefix()) return;                          // uniform
         unsigned char *rows[Ring::kItems];
 #pragma unroll
         for (int item = 0; item < Ring::kItems; ++item) {
             const int n = g * Ring::kItems + item, slot = n % Ring::kVSlots;
-            if (fine) fine = mbarrier_poll_bounded(misc + kTreeBarVFull + slot * 8, (n / Ring::kVSlots) & 1);
+            if (fine) fine = tree_poll(misc + kTreeBarVFull + slot * 8, (n / Ring::kVSlots) & 1);
             rows[item] = smem + Ring::kVOffset + slot * Ring::kItemBytes + row0 * 128;
         }
         __syncwarp();
         unsigned bad_rows = 0;
 #pragma unroll 1
-        for (int r0 = 0; r0 < 32; r0 += 4) {                          // four rows at a time, 8 lanes a row
+        for (int r0 = 0; r0 < kRows; r0 += 4) {                       // four rows at a time, 8 lanes a row
             const int pos = start + r0 + (lane >> 3);
             bool bad = false;
 #pragma unroll
@@ -493,6 +592,7 @@ struct TreeCopies {
 __device__ __forceinline__ float tree_stray_weight(const AttnParams &a, const TreeSegment &s, int64_t out_row, int64_t kv_row, int D, float lse2)
 {
     float dot = 0.f;
+    #pragma unroll 1
     for (int c = 0; c < D; ++c) dot = fmaf(__half2float(a.q[out_row * D + c]), __half2float(a.k[kv_row * D + c]), dot);
     return fast_exp2(dot * a.scale_log2e - lse2);
 }
@@ -503,6 +603,7 @@ static __device__ __noinline__ void tree_add_poisoned(const AttnParams &a, const
         if (!(poison[n >> 5] >> (n & 31) & 1u) || !row.sees(n)) continue;
         const int64_t kv_row = tree_cache_row(a, s.b, s.hk, s.prefix() + n);
         const float weight = tree_stray_weight(a, s, out_row, kv_row, D, lse2);
+#pragma unroll 1
         for (int c = 0; c < 32; ++c) o[c] += weight * __half2float(a.v[kv_row * D + d0 + c]);
     }
 }
@@ -522,8 +623,9 @@ static __device__ __noinline__ float tree_poisoned_value(const TreeParams &p, co
     return value;
 }
 
-// The barriers that the kernels have in common, and the poison words (one thread).
-__device__ __forceinline__ void tree_init_barriers(unsigned misc, unsigned char *misc_ptr, int softmax_warps)
+// The barriers that the kernels have in common, and the poison words (one thread); softmax_warps: how many work on
+// one unit of logits.
+__device__ __forceinline__ void tree_init_barriers(unsigned misc, unsigned char *misc_ptr, int softmax_warps, int all_softmax_warps)
 {
 #pragma unroll
     for (int s = 0; s < 6; ++s) {
@@ -539,13 +641,18 @@ __device__ __forceinline__ void tree_init_barriers(unsigned misc, unsigned char 
         mbarrier_init(misc + kTreeBarPvDone + s * 8, 1);
         mbarrier_init(misc + kTreeBarSFree + s * 8, softmax_warps);
     }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        mbarrier_init(misc + kTreeBarSegFull + s * 8, 1);
+        mbarrier_init(misc + kTreeBarSegEmpty + s * 8, all_softmax_warps + 3);     // V producer and the two MMA issuers too
+    }
     mbarrier_init(misc + kTreeBarQFull, 1);
     mbarrier_init(misc + kTreeBarQEmpty, 1);
     mbarrier_init_fence();
     for (int i = 0; i < 32; ++i) reinterpret_cast<unsigned *>(misc_ptr + kTreePoison)[i] = 0u;
 }
 
-// Joins the partial results of the items that more than one block worked on, and zeroes the rows of
+// Joins the partial results of the items that more than one piece has a part of, and zeroes the rows of
 // sequences without work; one thread block per item and kTreeMergeRows rows, one warp per row.
 constexpr int kTreeMergeThreads = 128;
 constexpr int kTreeMergeRows = 16;
@@ -555,7 +662,7 @@ __global__ void __launch_bounds__(kTreeMergeThreads)
 tree_merge_kernel(const TreeParams p, int blocks, int row_parts)
 {
     const AttnParams &a = p.a;
-    __shared__ int64_t sums[2][kTreeMergeThreads / 32];
+    __shared__ int sums[2][kTreeMergeThreads / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int part = blockIdx.x % row_parts;
     const int item = blockIdx.x / row_parts;                          // (sequence, KV head, row block)
@@ -570,11 +677,11 @@ tree_merge_kernel(const TreeParams p, int blocks, int row_parts)
     int c0 = 0, c1 = 0;
     if (n_tiles > 0) {
         // tiles before this sequence, and all of them
-        int64_t before = 0, all = 0;
+        int before = 0, all = 0;
         for (int i = threadIdx.x; i < p.batch; i += kTreeMergeThreads) {
             int n;
             const int other = checked_tree(p.tree, a.seq_lens, a.max_seq_len, nullptr, i, false, n);
-            const int64_t tiles = (int64_t)tree_tiles(other, n) * items;
+            const int tiles = tree_tiles(other, n) * items;
             if (i < b) before += tiles;
             all += tiles;
         }
@@ -593,16 +700,11 @@ tree_merge_kernel(const TreeParams p, int blocks, int row_parts)
             before += sums[0][w];
             all += sums[1][w];
         }
-        const int64_t first = before + (int64_t)in_seq * n_tiles, last = first + n_tiles - 1;
-        auto block_of = [&](int64_t tile) -> int {
-            int c = (int)(tile * min((int64_t)blocks, all) / all);
-            while (tree_first_tile(all, c + 1, blocks) <= tile) ++c;
-            while (tree_first_tile(all, c, blocks) > tile) --c;
-            return c;
-        };
-        c0 = block_of(first);
-        c1 = block_of(last);
-        if (c0 == c1) return;                                         // one block had it all: the result is written
+        const int first = before + in_seq * n_tiles, last = first + n_tiles - 1;
+        const TreePieces pieces(all, blocks, p.short_pieces);
+        c0 = pieces.piece_of(first);
+        c1 = pieces.piece_of(last);
+        if (c0 == c1) return;                                         // one piece has it all: the result is written
     }
     constexpr int kPer = D / 32;                                      // dims per lane
     for (int r = part * kTreeMergeRows + warp; r < min((part + 1) * kTreeMergeRows, p.item_rows); r += kTreeMergeThreads / 32) {

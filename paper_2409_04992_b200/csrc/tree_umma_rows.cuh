@@ -36,7 +36,7 @@ struct TreeRowsGeometry {
 
 template <int D, bool kPaged, int kStreams>
 __global__ void __launch_bounds__(TreeRowsGeometry<D, kStreams>::kThreads, 1)
-tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                       const __grid_constant__ CUtensorMap map_v)
 {
     using Geo = TreeRowsGeometry<D, kStreams>;
@@ -56,13 +56,13 @@ tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap ma
     const unsigned q_smem = base + Geo::kQOffset, misc = base + Geo::kMiscOffset;
     unsigned char *misc_ptr = smem + Geo::kMiscOffset;
 
-    tree_find_start(p, misc_ptr, Geo::kThreads);
+    tree_count_tiles(p, misc_ptr, Geo::kThreads);
     if (warp == kWarpLogits) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      :: "r"(misc + kTreeTmemPtr), "n"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     } else if (warp == kWarpK) {
-        if (lane == 0) tree_init_barriers(misc, misc_ptr, 4);
+        if (lane == 0) tree_init_barriers(misc, misc_ptr, 4, Geo::kSoftmaxWarps);
     } else if (warp < Geo::kSoftmaxWarps) {
         // rows of a block that do not exist are zeros for good: the copies fill only the others
         const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
@@ -74,9 +74,7 @@ tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap ma
     __syncthreads();
     tc_fence_after();
     const unsigned tmem = *reinterpret_cast<volatile unsigned *>(misc_ptr + kTreeTmemPtr);
-    TreeWalk walk;
-    walk.start(p, misc_ptr, lane);
-    TreeSegment seg;
+    const TreeQueue queue{misc, misc_ptr};
     const TreeCopies<D, kPaged, Ring> copies{p, smem, base, misc, lane};
 
     // The buffer of a unit (tile number g of this block, stream s) and how often it was used before.
@@ -84,22 +82,27 @@ tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap ma
     auto use_of = [](int g) -> int { return kStreams == 1 ? g >> 1 : g; };
 
     if (warp == kWarpK) {
-        copies.template produce_k<kStreams, kTreePanelBytes>(walk, &map_q, &map_k, q_smem);
+        copies.template produce_k<kStreams, kTreePanelBytes>(queue, &map_q, &map_k, q_smem);
     } else if (warp == kWarpV) {
-        copies.produce_v(walk, &map_v);
+        copies.produce_v(queue, &map_v);
     } else if (warp == kWarpLogits) {
         // ================================ logit MMAs ================================
         constexpr unsigned idesc = umma_idesc(128, 128, 0, 0);
         bool fine = true;
         int g = 0;
-        for (int k = 0; fine && walk.next(p, seg, lane); ++k) {
-            fine = __all_sync(0xffffffffu, mbarrier_wait_bounded(misc + kTreeBarQFull, k & 1));
+        for (int k = 0; fine; ++k) {
+            fine = queue.wait(k);
+            if (!fine) break;
+            const TreeSegment seg = queue.entry(k);
+            queue.done(k, lane);
+            if (seg.b < 0) break;
+            fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarQFull, k & 1));
             for (int j = seg.t0; j < seg.t1 && fine; ++j, ++g) {
 #pragma unroll
                 for (int item = 0; item < kItems; ++item) {
                     if (!fine) break;
                     const int n = g * kItems + item, slot = n % kKSlots;
-                    fine = __all_sync(0xffffffffu, mbarrier_wait_bounded(misc + kTreeBarKFull + slot * 8, (n / kKSlots) & 1));
+                    fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarKFull + slot * 8, (n / kKSlots) & 1));
                     if (!fine) break;
                     // rows of 128 bytes per 64-dim panel, 8-row groups 1024 bytes apart; a k-step of 16
                     // dims is 32 bytes along the row
@@ -108,7 +111,7 @@ tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap ma
                     for (int s = 0; s < kStreams; ++s) {
                         const int buf = buffer_of(g, s), use = use_of(g);
                         if (item == 0 && use >= 1)             // the weights that lie in the buffer have been used
-                            fine = fine && __all_sync(0xffffffffu, mbarrier_poll_bounded(misc + kTreeBarPvDone + buf * 8, (use - 1) & 1));
+                            fine = fine && __all_sync(0xffffffffu, tree_poll(misc + kTreeBarPvDone + buf * 8, (use - 1) & 1));
                         if (!fine) break;
                         tc_fence_after();
                         const uint64_t q_desc = umma_desc(q_smem + s * Geo::kQBytes, 16, 1024, 2);
@@ -136,17 +139,22 @@ tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap ma
         constexpr unsigned idesc = umma_idesc(128, kItemPanels * 64, 0, 1);       // weights K-major, V MN-major
         bool fine = true;
         int g = 0;
-        while (fine && walk.next(p, seg, lane)) {
+        for (int k = 0; fine; ++k) {
+            fine = queue.wait(k);
+            if (!fine) break;
+            const TreeSegment seg = queue.entry(k);
+            queue.done(k, lane);
+            if (seg.b < 0) break;
             for (int j = seg.t0; j < seg.t1 && fine; ++j, ++g) {
 #pragma unroll
                 for (int s = 0; s < kStreams; ++s) {
                     const int buf = buffer_of(g, s);
-                    fine = fine && __all_sync(0xffffffffu, mbarrier_poll_bounded(misc + kTreeBarPFull + buf * 8, use_of(g) & 1));
+                    fine = fine && __all_sync(0xffffffffu, tree_poll(misc + kTreeBarPFull + buf * 8, use_of(g) & 1));
 #pragma unroll
                     for (int item = 0; item < kItems; ++item) {
                         const int n = g * kItems + item, slot = n % kVSlots;
                         if (s == 0 && fine)
-                            fine = __all_sync(0xffffffffu, mbarrier_poll_bounded(misc + kTreeBarVFull + slot * 8, (n / kVSlots) & 1));
+                            fine = __all_sync(0xffffffffu, tree_poll(misc + kTreeBarVFull + slot * 8, (n / kVSlots) & 1));
                         if (!fine) break;
                         tc_fence_after();
                         // 64-dim panels kTreePanelBytes apart, 8-token groups 1024 bytes apart; a k-step is
@@ -181,7 +189,14 @@ tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap ma
         const bool used_row = node_in_block < p.nodes_per_block;
         bool fine = true;
         int g = 0;
-        for (int k = 0; walk.next(p, seg, lane); ++k) {
+        for (int k = 0;; ++k) {
+            if (!fine || !queue.wait(k)) {
+                fine = false;
+                break;
+            }
+            const TreeSegment seg = queue.entry(k);
+            queue.done(k, lane);
+            if (seg.b < 0) break;
             const int node = (seg.rb * kStreams + s) * p.nodes_per_block + node_in_block;
             const bool exists = used_row && node < p.tree.tokens, live = exists && node < seg.nodes;
             const int prefix = seg.prefix();
@@ -196,8 +211,8 @@ tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap ma
                 const unsigned logits = tmem + lanes + buf * 128;
                 const bool masked = start + kTreeTile > prefix;       // uniform
                 // (stream 0 cleans for both: the output MMAs of a tile start with it)
-                if (masked && s == 0) copies.clean_values(seg, j, g, (warp & 3) * 32, poison, fine);
-                if (fine) fine = mbarrier_poll_bounded(misc + kTreeBarSFull + buf * 8, use_of(g) & 1);
+                if (masked && s == 0) copies.template clean_values<32>(seg, j, g, (warp & 3) * 32, poison, fine);
+                if (fine) fine = tree_poll(misc + kTreeBarSFull + buf * 8, use_of(g) & 1);
                 fine = __all_sync(0xffffffffu, fine);
                 tc_fence_after();
                 // What the row sees of the tile, where that is not all of it; a negative scale takes the same way,
@@ -250,7 +265,7 @@ tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap ma
                     l *= alpha;
                     if (j > seg.t0) {
                         // the accumulator holds the tiles before this one once their MMAs are complete
-                        if (fine) fine = mbarrier_poll_bounded(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
+                        if (fine) fine = tree_poll(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
                         fine = __all_sync(0xffffffffu, fine);
                         tc_fence_after();
 #pragma unroll 1
@@ -303,15 +318,14 @@ tree_attn_rows_kernel(const TreeParams p, const __grid_constant__ CUtensorMap ma
                 if (lane == 0) mbarrier_arrive(misc + kTreeBarPFull + buf * 8);
             }
             // ---- the segment's end: the accumulator divided by the sum, to the output or the workspace ----
-            if (fine) fine = mbarrier_poll_bounded(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
+            if (fine) fine = tree_poll(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
             fine = __all_sync(0xffffffffu, fine);
             tc_fence_after();
             const bool empty = !live || l == 0.f;                     // (a NaN sum is not an empty row's)
             const float inverse = empty ? 0.f : 1.f / l;
             const float lse2 = empty ? kMinusHuge : m + log2f(l) - kGroupWeightLog2;
             const int64_t out_row = ((int64_t)seg.b * p.tree.tokens + node) * ((int64_t)a.heads * p.group) + (int64_t)seg.hk * p.group + head;
-            // the rows that a block starts inside go to its first slot, those it ends inside to its second
-            const int64_t slot_row = (int64_t)(2 * blockIdx.x + (seg.t0 == 0 ? 1 : 0)) * p.item_rows + s * p.nodes_per_block * p.group + t;
+            const int64_t slot_row = (int64_t)seg.slot * p.item_rows + s * p.nodes_per_block * p.group + t;
             const bool whole = seg.whole();
             const volatile unsigned *taken = poison;
             const bool stray = live && (taken[0] | taken[1] | taken[2] | taken[3]) != 0u;

@@ -3,14 +3,15 @@
 //
 // The TOKENS are the long side of the MMAs, the rows (N = 16, 32 or 64 of them) the short one:
 //   S^T[128 tokens x N]  = K_tile[128 x D] Q^T[D x N]
-//   O^T[128 dims x N]   += V_tile^T[128 x 128] P^T[128 x N]       (head size 256: two accumulators; 64: the
+//   O^T[128 dims x 2 N] += V_tile^T[128 x 128] P^T[128 x 2 N]     (head size 256: two accumulators; 64: the
 //                                                                  dims twice, the upper half is not read)
 // so that exponentials and MMAs are paid for the rows that there are: at 64 rows half of what the form
 // with the rows as the long side takes (there a tile costs 128 exponentials a thread whatever the rows
 // are, and the MMAs' power holds the clock at 1.45 GHz).  From 32 rows on two groups of four softmax warps
 // take half of the rows each, so that a scheduler has two warps whose waits and exponentials overlap.  Thread
 // t of a group owns token t: it reads its logits, masks them, and writes its weights to shared memory, each as an
-// fp16 high and low part (two MMAs; see tree_umma_rows.cuh for why).  The rows' references are alike in all
+// fp16 high and low part (2 N columns, added up at the end; see tree_umma_rows.cuh for why, and one MMA for both
+// because with so few columns the MMA's time is that of reading the V tile).  The rows' references are alike in all
 // threads of a group and follow the maximum lazily: a vote per tile says whether any logit exceeds its row's
 // by more than kGroupLag, and only then maxima are exchanged and the accumulator rescaled.  A thread keeps
 // its own share of the rows' sums.
@@ -29,7 +30,7 @@ struct TreeTokensGeometry {
     static constexpr int kGroups = N == 16 ? 1 : 2;                      // of four softmax warps
     static constexpr int kCols = N / kGroups;                            // rows of a group
     static constexpr int kThreads = (4 * kGroups + 4) * 32;
-    static constexpr int kExtraBytes = kTreeMiscBytes + N * 16;          // row maxima or sums by warp
+    static constexpr int kExtraBytes = kTreeMiscBytes + N * 20;          // row maxima or sums by warp, and references
     using Ring = TreeRing<D, 226 * 1024 - kQBytes - kPBytes - kExtraBytes>;
     static constexpr int kQOffset = Ring::kRingBytes;
     static constexpr int kPOffset = kQOffset + kQBytes;
@@ -37,8 +38,9 @@ struct TreeTokensGeometry {
     static constexpr int kSmemBytes = kMiscOffset + kExtraBytes + 1024;  // room to align to 1024 bytes
     static constexpr int kAccs = D == 256 ? 2 : 1;
     static constexpr int kOColumn = 2 * N;                               // tensor memory: two logit buffers, then the accumulators
-    static constexpr int kTmemCols = N == 64 ? 256 : N == 32 ? 128 : 64;
-    static_assert(kOColumn + kAccs * N <= kTmemCols, "tensor memory");
+    static constexpr int kTmemCols = (kOColumn + kAccs * 2 * N > 256) ? 512 : (kOColumn + kAccs * 2 * N > 128) ? 256 :
+                                     (kOColumn + kAccs * 2 * N > 64) ? 128 : 64;
+    static_assert(kOColumn + kAccs * 2 * N <= kTmemCols, "tensor memory");
     static_assert(kSmemBytes <= 227 * 1024, "one block per SM must fit");
 };
 
@@ -71,7 +73,7 @@ __device__ __forceinline__ void tc_loaded16(float *v)
 
 template <int D, bool kPaged, int N>
 __global__ void __launch_bounds__(TreeTokensGeometry<D, N>::kThreads, 1)
-tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                         const __grid_constant__ CUtensorMap map_v)
 {
     using Geo = TreeTokensGeometry<D, N>;
@@ -92,13 +94,13 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
     const unsigned q_smem = base + Geo::kQOffset, p_smem = base + Geo::kPOffset, misc = base + Geo::kMiscOffset;
     unsigned char *misc_ptr = smem + Geo::kMiscOffset;
 
-    tree_find_start(p, misc_ptr, Geo::kThreads);
+    tree_count_tiles(p, misc_ptr, Geo::kThreads);
     if (warp == kWarpLogits) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      :: "r"(misc + kTreeTmemPtr), "n"(Geo::kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     } else if (warp == kWarpK) {
-        if (lane == 0) tree_init_barriers(misc, misc_ptr, kSoftmaxWarps);
+        if (lane == 0) tree_init_barriers(misc, misc_ptr, kSoftmaxWarps, kSoftmaxWarps);
     } else if (warp < kSoftmaxWarps) {
         // rows that do not exist are zeros for good: the copies fill only the others
         const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
@@ -109,31 +111,34 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
     __syncthreads();
     tc_fence_after();
     const unsigned tmem = *reinterpret_cast<volatile unsigned *>(misc_ptr + kTreeTmemPtr);
-    TreeWalk walk;
-    walk.start(p, misc_ptr, lane);
-    TreeSegment seg;
+    const TreeQueue queue{misc, misc_ptr};
     const TreeCopies<D, kPaged, Ring> copies{p, smem, base, misc, lane};
 
     if (warp == kWarpK) {
-        copies.template produce_k<1, Geo::kQPanel>(walk, &map_q, &map_k, q_smem);
+        copies.template produce_k<1, Geo::kQPanel>(queue, &map_q, &map_k, q_smem);
     } else if (warp == kWarpV) {
-        copies.produce_v(walk, &map_v);
+        copies.produce_v(queue, &map_v);
     } else if (warp == kWarpLogits) {
         // ================================ logit MMAs ================================
         constexpr unsigned idesc = umma_idesc(128, N, 0, 0);           // K tile and query rows K-major
         const uint64_t q_desc = umma_desc(q_smem, 16, 1024, 2);
         bool fine = true;
         int g = 0;
-        for (int k = 0; fine && walk.next(p, seg, lane); ++k) {
-            fine = __all_sync(0xffffffffu, mbarrier_wait_bounded(misc + kTreeBarQFull, k & 1));
+        for (int k = 0; fine; ++k) {
+            fine = queue.wait(k);
+            if (!fine) break;
+            const TreeSegment seg = queue.entry(k);
+            queue.done(k, lane);
+            if (seg.b < 0) break;
+            fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarQFull, k & 1));
             for (int j = seg.t0; j < seg.t1 && fine; ++j, ++g) {
                 const int buf = g & 1;
-                if (g >= 2) fine = __all_sync(0xffffffffu, mbarrier_wait_bounded(misc + kTreeBarSFree + buf * 8, ((g >> 1) - 1) & 1));
+                if (g >= 2) fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarSFree + buf * 8, ((g >> 1) - 1) & 1));
 #pragma unroll
                 for (int item = 0; item < kItems; ++item) {
                     if (!fine) break;
                     const int n = g * kItems + item, slot = n % kKSlots;
-                    fine = __all_sync(0xffffffffu, mbarrier_wait_bounded(misc + kTreeBarKFull + slot * 8, (n / kKSlots) & 1));
+                    fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarKFull + slot * 8, (n / kKSlots) & 1));
                     if (!fine) break;
                     tc_fence_after();
                     // rows of 128 bytes per 64-dim panel, 8-row groups 1024 bytes apart; a k-step of 16
@@ -158,33 +163,36 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
         if (!fine && lane == 0 && a.status) atomicOr(a.status, kFlagCopyTimeout);
     } else if (warp == kWarpOutput) {
         // ================================ output MMAs ================================
-        constexpr unsigned idesc = umma_idesc(128, N, 1, 1);           // V tile and weights MN-major
+        constexpr unsigned idesc = umma_idesc(128, 2 * N, 1, 1);       // V tile and weights MN-major
         // Weights: 8-column blocks of [128 tokens][16 bytes], 2048 bytes apart; 8-token groups 128 bytes
         // apart; a k-step is 16 tokens = 256 bytes.  The low parts lie behind the high ones.
-        const uint64_t hi_desc = umma_desc(p_smem, 128, 2048, 0), lo_desc = umma_desc(p_smem + N * 256, 128, 2048, 0);
+        const uint64_t p_desc = umma_desc(p_smem, 128, 2048, 0);
         bool fine = true;
         int g = 0;
-        while (fine && walk.next(p, seg, lane)) {
+        for (int k = 0; fine; ++k) {
+            fine = queue.wait(k);
+            if (!fine) break;
+            const TreeSegment seg = queue.entry(k);
+            queue.done(k, lane);
+            if (seg.b < 0) break;
             for (int j = seg.t0; j < seg.t1 && fine; ++j, ++g) {
-                fine = __all_sync(0xffffffffu, mbarrier_poll_bounded(misc + kTreeBarPFull, g & 1));
+                fine = __all_sync(0xffffffffu, tree_poll(misc + kTreeBarPFull, g & 1));
 #pragma unroll
                 for (int item = 0; item < kItems; ++item) {
                     if (!fine) break;
                     const int n = g * kItems + item, slot = n % kVSlots;
-                    fine = __all_sync(0xffffffffu, mbarrier_poll_bounded(misc + kTreeBarVFull + slot * 8, (n / kVSlots) & 1));
+                    fine = __all_sync(0xffffffffu, tree_poll(misc + kTreeBarVFull + slot * 8, (n / kVSlots) & 1));
                     if (!fine) break;
                     tc_fence_after();
                     // V item read MN-major (M = 128 dims): its 64-dim panels kTreePanelBytes apart (the same panel
                     // twice at head size 64), 8-token groups 1024 bytes apart; a k-step is 16 tokens = 2048 bytes
                     const uint64_t v_desc = umma_desc(base + Ring::kVOffset + slot * kItemBytes, D == 64 ? 0 : kTreePanelBytes, 1024, 2);
                     if (elect_one()) {
-                        const unsigned acc = tmem + Geo::kOColumn + item * N;
+                        const unsigned acc = tmem + Geo::kOColumn + item * 2 * N;
 #pragma unroll
-                        for (int ks = 0; ks < 8; ++ks) {
-                            const uint64_t v_step = v_desc + (uint64_t)((ks * 2048) >> 4);
-                            tc_mma_f16(acc, v_step, hi_desc + (uint64_t)((ks * 256) >> 4), idesc, j > seg.t0 || ks > 0);
-                            tc_mma_f16(acc, v_step, lo_desc + (uint64_t)((ks * 256) >> 4), idesc, 1);
-                        }
+                        for (int ks = 0; ks < 8; ++ks)
+                            tc_mma_f16(acc, v_desc + (uint64_t)((ks * 2048) >> 4), p_desc + (uint64_t)((ks * 256) >> 4), idesc,
+                                       j > seg.t0 || ks > 0);
                         tc_commit(misc + kTreeBarVEmpty + slot * 8);
                         if (item + 1 == kItems) tc_commit(misc + kTreeBarPvDone);
                     }
@@ -200,17 +208,38 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
         const int t = threadIdx.x & 127;                              // token of the tile = lane of tensor memory
         const unsigned lanes = tmem + ((unsigned)((warp & 3) * 32) << 16);
         float *by_warp = reinterpret_cast<float *>(misc_ptr + kTreeMiscBytes);   // [N][4]: a row's maxima, or sums, by warp
+        float *offsets = by_warp + N * 4;                             // [N]: the rows' offsets as they were last moved
         const int rows_here = p.nodes_per_block * p.group;            // <= N
         const float scale = a.scale_log2e;
         constexpr float kTooLarge = kGroupLag + kGroupWeightLog2;
         bool fine = true;
+        float x[kCols];
+        // Waits for the logits of a tile and asks for this thread's.
+        auto request = [&](int tile) {
+            if (fine) fine = tree_poll(misc + kTreeBarSFull + (tile & 1) * 8, (tile >> 1) & 1);
+            fine = __all_sync(0xffffffffu, fine);
+            tc_fence_after();
+#pragma unroll
+            for (int r = 0; r < kCols; r += 16) tc_issue_load16(x + r, lanes + (tile & 1) * N + row0 + r);
+        };
         int g = 0;
-        for (int k = 0; walk.next(p, seg, lane); ++k) {
-            const int prefix = seg.prefix();
+        for (int k = 0;; ++k) {
+            // (one decision for the group: its barriers have to stay in step)
+            if (group_any(vote_id, !queue.wait(k) || !fine)) {
+                fine = false;
+                break;
+            }
+            const TreeSegment &seg = queue.entry(k);                  // read where it is needed: registers are scarce
+            if (seg.b < 0) break;
+            const int prefix = seg.prefix(), t0 = seg.t0, t1 = seg.t1;
             unsigned *poison = reinterpret_cast<unsigned *>(misc_ptr + kTreePoison) + (k & 7) * 4;
             // (the words of four segments ahead: no warp is more than two segments from another)
             if (threadIdx.x < 4) reinterpret_cast<volatile unsigned *>(misc_ptr + kTreePoison)[((k + 4) & 7) * 4 + threadIdx.x] = 0u;
             const int live_rows = min(rows_here, seg.nodes * p.group);
+            // What the group's rows see of the tree, lane r row row0 + r (asked for here, needed at the last tiles).
+            TreeRow mine = {0, 0, false};
+            if (t1 * kTreeTile > prefix && lane < kCols && row0 + lane < live_rows)
+                mine = tree_row(p.tree, seg.b, (row0 + lane) / p.group, seg.nodes);
             // Two rows at a time: the weight exponent's offset kGroupWeightLog2 - reference, and this thread's
             // sums; sums and accumulator carry kGroupWeightScale.
             float2 offset[kCols / 2], l[kCols / 2];
@@ -219,43 +248,39 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
                 offset[r] = make_float2(-kMinusHuge, -kMinusHuge);
                 l[r] = make_float2(0.f, 0.f);
             }
-            for (int j = seg.t0; j < seg.t1; ++j, ++g) {
+            for (int j = t0; j < t1; ++j, ++g) {
                 const int buf = g & 1, start = j * kTreeTile;
                 const unsigned logits = lanes + buf * N + row0;
                 const bool masked = start + kTreeTile > prefix;       // uniform
                 unsigned seen_by = ~0u;                               // the group's rows that see this thread's token
                 if (masked) {
-                    if (group == 0) copies.clean_values(seg, j, g, warp * 32, poison, fine);
-                    const int node = start + t - prefix;
-                    uint64_t rows = 0;
-                    if (node < 0) rows = live_rows >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << live_rows) - 1;
-                    if (node >= 0 && node < seg.nodes) {
-                        const uint64_t *words = p.tree.mask + (int64_t)seg.b * p.tree.tokens * p.tree.words + (node >> 6);
-                        const uint64_t heads = p.group < 64 ? ((uint64_t)1 << p.group) - 1 : ~(uint64_t)0;
-#pragma unroll 4
-                        for (int other = 0; other < seg.nodes; ++other)
-                            if (__ldg(words + (int64_t)other * p.tree.words) >> (node & 63) & 1u) rows |= heads << (other * p.group);
+                    copies.template clean_values<32 / Geo::kGroups>(seg, j, g, (warp & 3) * 32 + group * (32 / Geo::kGroups), poison, fine);
+                    // The 32 tokens of this warp are columns of the rows' bits: 32 votes transpose them.
+                    const int first = start + (warp & 3) * 32 - prefix;            // the node of lane 0's token
+                    const Bits128 bits = {mine.lo, mine.hi};
+                    unsigned window = mine.all ? ~0u : 0u;
+                    if (first >= 0) window = first < 128 ? bits.shifted_down(first).word(0) : 0u;
+                    else if (first > -32) window = bits.word(0) << -first | (mine.all ? (1u << -first) - 1u : 0u);
+#pragma unroll 8
+                    for (int i = 0; i < 32; ++i) {
+                        const unsigned rows = __ballot_sync(0xffffffffu, window >> i & 1u);
+                        if (lane == i) seen_by = rows;
                     }
-                    seen_by = (unsigned)(rows >> row0);
                 }
-                if (fine) fine = mbarrier_poll_bounded(misc + kTreeBarSFull + buf * 8, (g >> 1) & 1);
-                fine = __all_sync(0xffffffffu, fine);
-                tc_fence_after();
+                request(g);
                 // Exponents of the weights against the references; where one is too large the references move
                 // and they are computed again.
                 float e[kCols];
                 for (;;) {
 #pragma unroll
-                    for (int r = 0; r < kCols; r += 16) tc_issue_load16(e + r, logits + r);
-#pragma unroll
-                    for (int r = 0; r < kCols; r += 16) tc_loaded16(e + r);
+                    for (int r = 0; r < kCols; r += 16) tc_loaded16(x + r);
                     float most = -INFINITY, most_odd = -INFINITY;
 #pragma unroll
                     for (int r = 0; r < kCols / 2; ++r) {
                         // (not one fused operation: the scaled logit has to round as the maxima below do)
-                        const float2 x = add2(mul2(make_float2(e[2 * r], e[2 * r + 1]), make_float2(scale, scale)), offset[r]);
-                        e[2 * r] = x.x;
-                        e[2 * r + 1] = x.y;
+                        const float2 y = add2(mul2(make_float2(x[2 * r], x[2 * r + 1]), make_float2(scale, scale)), offset[r]);
+                        e[2 * r] = y.x;
+                        e[2 * r + 1] = y.y;
                     }
                     if (masked) {
 #pragma unroll
@@ -269,19 +294,19 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
                     }
                     if (!group_any(vote_id, fmaxf(most, most_odd) > kTooLarge)) break;
                     // ---- some row's reference moves (rare after a segment's first tile) ----
-                    if (j > seg.t0) {                                 // the accumulator holds the tiles before this one
-                        if (fine) fine = mbarrier_poll_bounded(misc + kTreeBarPvDone, (g - 1) & 1);
+                    if (j > t0) {                                 // the accumulator holds the tiles before this one
+                        if (fine) fine = tree_poll(misc + kTreeBarPvDone, (g - 1) & 1);
                         fine = __all_sync(0xffffffffu, fine);
                         tc_fence_after();
                     }
 #pragma unroll
                     for (int r0 = 0; r0 < kCols; r0 += 16) {
-                        float x[16];
-                        tc_issue_load16(x, logits + r0);
-                        tc_loaded16(x);
+                        float z[16];
+                        tc_issue_load16(z, logits + r0);
+                        tc_loaded16(z);
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) x[r] = seen_by >> (r0 + r) & 1u ? x[r] * scale : -INFINITY;
-                        const float top = warp_reduce16<true>(x, lane);
+                        for (int r = 0; r < 16; ++r) z[r] = seen_by >> (r0 + r) & 1u ? z[r] * scale : -INFINITY;
+                        const float top = warp_reduce16<true>(z, lane);
                         if ((lane & 1) == 0) by_warp[(row0 + r0 + warp_reduce16_row(lane)) * 4 + (warp & 3)] = top;
                     }
                     group_sync(sync_id);
@@ -298,22 +323,25 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
                             if (top + off > kTooLarge) {
                                 alpha[r] = fast_exp2(kGroupWeightLog2 - off - top);       // 2^(old - new reference)
                                 off = kGroupWeightLog2 - top;
+                                if (t == r0 + r) offsets[row0 + r0 + r] = off;
                             }
                             sum *= alpha[r];
                         }
-                        if (j > seg.t0) {
+                        if (j > t0) {
 #pragma unroll
-                            for (int acc = 0; acc < kAccs; ++acc) {
+                            for (int part = 0; part < 2 * kAccs; ++part) {        // high and low parts of each accumulator
                                 float o[16];
-                                tc_issue_load16(o, lanes + Geo::kOColumn + acc * N + row0 + r0);
+                                tc_issue_load16(o, lanes + Geo::kOColumn + part * N + row0 + r0);
                                 tc_loaded16(o);
 #pragma unroll
                                 for (int r = 0; r < 16; ++r) o[r] *= alpha[r];
-                                tc_store16(lanes + Geo::kOColumn + acc * N + row0 + r0, o);
+                                tc_store16(lanes + Geo::kOColumn + part * N + row0 + r0, o);
                             }
                         }
                     }
                     group_sync(sync_id);                              // the maxima have been read
+#pragma unroll
+                    for (int r = 0; r < kCols; r += 16) tc_issue_load16(x + r, logits + r);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -329,7 +357,7 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
                     lo[r] = pack_half2(rest.x, rest.y);
                 }
                 if (g > 0) {                                          // the previous tile's MMAs have read the weights
-                    if (fine) fine = mbarrier_poll_bounded(misc + kTreeBarPvDone, (g - 1) & 1);
+                    if (fine) fine = tree_poll(misc + kTreeBarPvDone, (g - 1) & 1);
                 }
                 unsigned char *weights = smem + Geo::kPOffset + row0 * 256 + t * 16;
 #pragma unroll
@@ -351,7 +379,7 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
                 const float sum = warp_reduce16<false>(x, lane);
                 if ((lane & 1) == 0) by_warp[(row0 + r0 + warp_reduce16_row(lane)) * 4 + (warp & 3)] = sum;
             }
-            if (fine) fine = mbarrier_poll_bounded(misc + kTreeBarPvDone, (g - 1) & 1);
+            if (fine) fine = tree_poll(misc + kTreeBarPvDone, (g - 1) & 1);
             fine = __all_sync(0xffffffffu, fine);
             tc_fence_after();
             group_sync(sync_id);
@@ -361,18 +389,13 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
                 const int r = row0 + t, node = r / p.group;
                 const float4 sums = *reinterpret_cast<const float4 *>(by_warp + r * 4);
                 const float total = (sums.x + sums.y) + (sums.z + sums.w);
-                float off = 0.f;
-#pragma unroll
-                for (int i = 0; i < kCols; ++i)
-                    if (i == t) off = (i & 1) ? offset[i / 2].y : offset[i / 2].x;
                 const bool empty = r >= live_rows || total == 0.f;    // (a NaN sum is not an empty row's)
-                const float lse2 = empty ? kMinusHuge : log2f(total) - off;
-                // (row numbers are below 2^31: checked by the host.)  The rows that a block starts inside go to
-                // its first slot, those it ends inside to its second.
+                const float lse2 = empty ? kMinusHuge : log2f(total) - offsets[r];
+                // (row numbers are below 2^31: checked by the host)
                 int to = -1;
                 if (r < rows_here && node < p.tree.tokens && fine) {
                     const int out_row = (seg.b * p.tree.tokens + node) * (a.heads * p.group) + seg.hk * p.group + (r - node * p.group);
-                    to = whole ? out_row : (2 * (int)blockIdx.x + (seg.t0 == 0 ? 1 : 0)) * p.item_rows + r;
+                    to = whole ? out_row : seg.slot * p.item_rows + r;
                     if (!whole) a.part_lse[to] = lse2;
                     else if (a.lse) a.lse[to] = empty ? -INFINITY : lse2 * kLn2;
                 }
@@ -382,30 +405,38 @@ tree_attn_tokens_kernel(const TreeParams p, const __grid_constant__ CUtensorMap 
             const volatile unsigned *taken = poison;
             const bool stray = (taken[0] | taken[1] | taken[2] | taken[3]) != 0u;
 #pragma unroll 1
-            for (int r0 = 0; r0 < kCols; r0 += 16) {
+            for (int block = 0; block < kCols / 16 * kAccs; ++block) {
+                const int first = row0 + block / kAccs * 16, acc = block % kAccs, d = acc * 128 + t;
+                float o[16], low[16];
+                tc_issue_load16(o, lanes + Geo::kOColumn + acc * 2 * N + first);
+                tc_issue_load16(low, lanes + Geo::kOColumn + (acc * 2 + 1) * N + first);
+                tc_loaded16(o);
+                tc_loaded16(low);
+                float more[16];
+                if (stray) {
 #pragma unroll 1
-                for (int acc = 0; acc < kAccs; ++acc) {
-                    float o[16];
-                    tc_issue_load16(o, lanes + Geo::kOColumn + acc * N + row0 + r0);
-                    tc_loaded16(o);
-                    const int d = acc * 128 + t;
-#pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float4 row = *reinterpret_cast<const float4 *>(by_warp + (row0 + r0 + i) * 4);
-                        const int to = __float_as_int(row.y);
-                        if (to >= 0 && (D >= 128 || t < D)) {
-                            // (an empty row's accumulator may hold anything)
-                            float value = row.x == 0.f ? 0.f : o[i] * row.x;
-                            if (stray) value += tree_poisoned_value(p, seg, poison, row0 + r0 + i, D, d, row.z);
-                            if (whole) a.out[(int64_t)to * D + d] = __float2half_rn(value);
-                            else a.part_o[(int64_t)to * D + d] = value;
-                        }
+                        const float4 row = *reinterpret_cast<const float4 *>(by_warp + (first + i) * 4);
+                        more[i] = __float_as_int(row.y) >= 0 && (D >= 128 || t < D) ? tree_poisoned_value(p, seg, poison, first + i, D, d, row.z) : 0.f;
                     }
-                    __syncwarp();
                 }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float2 row = *reinterpret_cast<const float2 *>(by_warp + (first + i) * 4);
+                    const int to = __float_as_int(row.y);
+                    // (an empty row's accumulator may hold anything)
+                    float value = row.x == 0.f ? 0.f : (o[i] + low[i]) * row.x;
+                    if (stray) value += more[i];
+                    if (to >= 0 && (D >= 128 || t < D)) {
+                        if (whole) a.out[(int64_t)to * D + d] = __float2half_rn(value);
+                        else a.part_o[(int64_t)to * D + d] = value;
+                    }
+                }
+                __syncwarp();
             }
             tc_fence_before();                                        // the accumulator has been read: the next tile may overwrite it
             group_sync(sync_id);                                      // so have the rows' numbers
+            queue.done(k, lane);
         }
         if (!fine && lane == 0 && a.status) atomicOr(a.status, kFlagCopyTimeout);
     }
