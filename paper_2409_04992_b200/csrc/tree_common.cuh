@@ -22,6 +22,15 @@ struct TreeShape {
 struct TreeRow {
     uint64_t lo, hi;               // nodes 0-63, 64-127
     bool all;                      // the row exists: it sees what lies before the tree
+    // without the bits of nodes that a tree of `nodes` nodes does not have
+    __device__ __forceinline__ TreeRow cut(int nodes) const
+    {
+        TreeRow row = *this;
+        if (nodes < 64) row.lo &= ((uint64_t)1 << nodes) - 1;
+        if (nodes <= 64) row.hi = 0;
+        else if (nodes < 128) row.hi &= ((uint64_t)1 << (nodes - 64)) - 1;
+        return row;
+    }
     // node < 0: a position before the tree
     __device__ __forceinline__ bool sees(int node) const
     {
@@ -39,11 +48,7 @@ __device__ __forceinline__ TreeRow tree_row(const TreeShape &tree, int b, int t,
     row.all = true;
     row.lo = words[0];
     if (tree.words > 1) row.hi = words[1];
-    // bits of nodes that the tree does not have count as 0
-    if (nodes < 64) row.lo &= ((uint64_t)1 << nodes) - 1;
-    if (nodes <= 64) row.hi = 0;
-    else if (nodes < 128) row.hi &= ((uint64_t)1 << (nodes - 64)) - 1;
-    return row;
+    return row.cut(nodes);
 }
 
 // Length of sequence b and its number of nodes as the kernels see them; what is out of range

@@ -28,19 +28,10 @@ namespace instinfer {
 constexpr int kTreeTile = 128;                         // tokens per tile
 constexpr int kTreePanelBytes = kTreeTile * 128;       // 64 dims of 128 rows
 
-// Bounded waits with the loop out of line (see mbarrier_wait_bounded and mbarrier_poll_bounded): the first test
-// succeeds more often than not, and some thirty of them are in each kernel.
+// A bounded wait with the loop out of line: the first test succeeds more often than not, and some thirty of these
+// are in each kernel.  (Polling instead of the parked wait made no difference here.)
 static __device__ __noinline__ bool tree_wait_more(unsigned bar, unsigned parity) { return mbarrier_wait_bounded(bar, parity); }
-static __device__ __noinline__ bool tree_poll_more(unsigned bar, unsigned parity)
-{
-    const long long start = clock64();
-    for (;;) {
-        if (mbarrier_test(bar, parity)) return true;
-        if (clock64() - start > kWaitCycles) return false;
-    }
-}
 __device__ __forceinline__ bool tree_wait(unsigned bar, unsigned parity) { return mbarrier_test(bar, parity) || tree_wait_more(bar, parity); }
-__device__ __forceinline__ bool tree_poll(unsigned bar, unsigned parity) { return mbarrier_test(bar, parity) || tree_poll_more(bar, parity); }
 
 // Ring geometry of a head size: an item is up to 128 dims of a tile (32 KiB; 16 KiB at head size 64).
 template <int D, int kBytes>
@@ -74,8 +65,9 @@ constexpr int kTreeBarSegFull = 288;   // [4] a segment is announced
 constexpr int kTreeBarSegEmpty = 320;  // [4] everyone is done with it
 constexpr int kTreePoison = 352;       // [8][4] words: nodes of a segment whose value row is not finite, by segment number
 constexpr int kTreeSegments = 480;     // [4] TreeSegment
+constexpr int kTreeEntryBytes = 56;
 constexpr int kTreeScan = 480;         // [16] ints: per-warp sums of the set-up's scan, before the first segment
-constexpr int kTreeMiscBytes = 480 + 4 * 48;
+constexpr int kTreeMiscBytes = 480 + 4 * kTreeEntryBytes;
 static_assert(kTreeScan + 16 * 4 <= kTreeMiscBytes && kTreeMiscBytes % 16 == 0, "misc region too small");
 
 struct TreeParams {
@@ -129,10 +121,14 @@ struct TreePieces {
 // inside an item goes to its piece's first slot, what ends inside one to its second.
 struct TreeSegment {
     int b, len, nodes, hk, rb, t0, t1, n_tiles, slot;
+    // Row 0 of the item's output and log-sum-exp: the caller's buffers, or the partial result's slot.  (Looked up by
+    // the producer: at a segment's end the others would wait for the parameters.)
+    void *out;
+    float *lse;
     __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == n_tiles; }
     __device__ __forceinline__ int prefix() const { return len - nodes; }
 };
-static_assert(sizeof(TreeSegment) <= 48, "queue entry");
+static_assert(sizeof(TreeSegment) == kTreeEntryBytes, "queue entry");
 
 // Draws this block's pieces and finds their segments (all 32 lanes of one warp together).  Out of line: the kernel's
 // loops should stay in the instruction cache.
@@ -161,6 +157,7 @@ struct TreeFinder {
         end = pieces.first(piece + 1);
         if (lane == 0 && pieces.step > 0) drawn = pieces.blocks + atomicAdd(p.ticket, 1u);
     }
+    template <int D>
     __device__ __noinline__ TreeSegment next(const TreeParams &p, int lane)
     {
         TreeSegment s;
@@ -203,6 +200,9 @@ struct TreeFinder {
         s.t1 = min(s.n_tiles, s.t0 + (end - tile));
         s.slot = 2 * piece + (s.t0 == 0 ? 1 : 0);
         tile += s.t1 - s.t0;
+        const int64_t row = (int64_t)b * p.tree.tokens * (p.a.heads * p.group) + s.hk * p.group, slot_row = (int64_t)s.slot * p.item_rows;
+        s.out = s.whole() ? static_cast<void *>(p.a.out + row * D) : static_cast<void *>(p.a.part_o + slot_row * D);
+        s.lse = !s.whole() ? p.a.part_lse + slot_row : p.a.lse ? p.a.lse + row : nullptr;
         return s;
     }
 };
@@ -211,7 +211,7 @@ struct TreeFinder {
 struct TreeQueue {
     unsigned misc;
     unsigned char *misc_ptr;
-    __device__ __forceinline__ TreeSegment &entry(int k) const { return reinterpret_cast<TreeSegment *>(misc_ptr + kTreeSegments + (k & 3) * 48)[0]; }
+    __device__ __forceinline__ TreeSegment &entry(int k) const { return reinterpret_cast<TreeSegment *>(misc_ptr + kTreeSegments)[k & 3]; }
     // Waits for segment k (all lanes); false if the wait ran out.
     __device__ __forceinline__ bool wait(int k) const
     {
@@ -432,7 +432,7 @@ struct TreeCopies {
     {
         constexpr int slots = kIsV ? Ring::kVSlots : Ring::kKSlots, bar_full = kIsV ? kTreeBarVFull : kTreeBarKFull;
         for (int i = max(count - slots, 0); i < count; ++i)
-            (void)tree_poll(misc + bar_full + (i % slots) * 8, (i / slots) & 1);
+            (void)tree_wait(misc + bar_full + (i % slots) * 8, (i / slots) & 1);
     }
     // The K producer's whole job: draws the pieces, announces their segments, copies the K tiles, and behind the
     // first tile of every segment its query rows, kBlocks row blocks (64 dims of one per kQPanel bytes) at q_smem.
@@ -443,7 +443,7 @@ struct TreeCopies {
         finder.start(p, *reinterpret_cast<const int *>(queue.misc_ptr + kTreeTotal), lane);
         int count = 0, k = 0;
         bool fine = true;
-        // Segments are found one ahead, while the copies of the one before wait for their slots: lengths, block ids
+        // Segments are found two ahead, while the copies of the one before wait for their slots: lengths, block ids
         // and the ticket's answer come from a busy memory system, some 2000 cycles each.
         auto announce = [&](const TreeSegment &s, int n) -> bool {
             if (n >= 4 && !__all_sync(0xffffffffu, tree_wait(misc + kTreeBarSegEmpty + (n & 3) * 8, ((n >> 2) - 1) & 1))) return false;
@@ -453,11 +453,16 @@ struct TreeCopies {
             }
             return true;
         };
-        TreeSegment seg = finder.next(p, lane);
+        TreeSegment seg = finder.template next<D>(p, lane);
         (void)announce(seg, 0);
         int ids = seg.b >= 0 ? fetch_ids(seg, seg.t0) : -1;
+        TreeSegment after = seg;
+        if (seg.b >= 0) {
+            after = finder.template next<D>(p, lane);
+            (void)announce(after, 1);
+        }
         for (; fine && seg.b >= 0; ++k) {
-            TreeSegment after;
+            TreeSegment later = after;                // segment k + 2
             int ids_after = -1;
             for (int j = seg.t0; j < seg.t1 && fine; ++j) {
                 const int now = ids;
@@ -483,18 +488,21 @@ struct TreeCopies {
                     }
                 }
                 __syncwarp();
-                after = finder.next(p, lane);
-                fine = fine && announce(after, k + 1);
-                if (after.b >= 0) ids_after = fetch_ids(after, after.t0);
+                if (after.b >= 0) {
+                    ids_after = fetch_ids(after, after.t0);
+                    later = finder.template next<D>(p, lane);
+                    fine = fine && announce(later, k + 2);
+                }
             }
             if (!fine) break;
             seg = after;
+            after = later;
             ids = ids_after;
         }
         if (!fine) {
             if (lane == 0 && p.a.status) atomicOr(p.a.status, kFlagCopyTimeout);
             drain<false>(count);
-            (void)tree_poll(misc + kTreeBarQFull, k & 1);     // (the query rows of this segment, if they were asked for)
+            (void)tree_wait(misc + kTreeBarQFull, k & 1);     // (the query rows of this segment, if they were asked for)
         }
     }
     __device__ __forceinline__ void produce_v(const TreeQueue &queue, const CUtensorMap *map_v) const
@@ -551,7 +559,7 @@ struct TreeCopies {
 #pragma unroll
         for (int item = 0; item < Ring::kItems; ++item) {
             const int n = g * Ring::kItems + item, slot = n % Ring::kVSlots;
-            if (fine) fine = tree_poll(misc + kTreeBarVFull + slot * 8, (n / Ring::kVSlots) & 1);
+            if (fine) fine = tree_wait(misc + kTreeBarVFull + slot * 8, (n / Ring::kVSlots) & 1);
             rows[item] = smem + Ring::kVOffset + slot * Ring::kItemBytes + row0 * 128;
         }
         __syncwarp();

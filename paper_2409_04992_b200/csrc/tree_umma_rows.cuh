@@ -111,7 +111,7 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                     for (int s = 0; s < kStreams; ++s) {
                         const int buf = buffer_of(g, s), use = use_of(g);
                         if (item == 0 && use >= 1)             // the weights that lie in the buffer have been used
-                            fine = fine && __all_sync(0xffffffffu, tree_poll(misc + kTreeBarPvDone + buf * 8, (use - 1) & 1));
+                            fine = fine && __all_sync(0xffffffffu, tree_wait(misc + kTreeBarPvDone + buf * 8, (use - 1) & 1));
                         if (!fine) break;
                         tc_fence_after();
                         const uint64_t q_desc = umma_desc(q_smem + s * Geo::kQBytes, 16, 1024, 2);
@@ -149,12 +149,12 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
 #pragma unroll
                 for (int s = 0; s < kStreams; ++s) {
                     const int buf = buffer_of(g, s);
-                    fine = fine && __all_sync(0xffffffffu, tree_poll(misc + kTreeBarPFull + buf * 8, use_of(g) & 1));
+                    fine = fine && __all_sync(0xffffffffu, tree_wait(misc + kTreeBarPFull + buf * 8, use_of(g) & 1));
 #pragma unroll
                     for (int item = 0; item < kItems; ++item) {
                         const int n = g * kItems + item, slot = n % kVSlots;
                         if (s == 0 && fine)
-                            fine = __all_sync(0xffffffffu, tree_poll(misc + kTreeBarVFull + slot * 8, (n / kVSlots) & 1));
+                            fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarVFull + slot * 8, (n / kVSlots) & 1));
                         if (!fine) break;
                         tc_fence_after();
                         // 64-dim panels kTreePanelBytes apart, 8-token groups 1024 bytes apart; a k-step is
@@ -212,7 +212,7 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                 const bool masked = start + kTreeTile > prefix;       // uniform
                 // (stream 0 cleans for both: the output MMAs of a tile start with it)
                 if (masked && s == 0) copies.template clean_values<32>(seg, j, g, (warp & 3) * 32, poison, fine);
-                if (fine) fine = tree_poll(misc + kTreeBarSFull + buf * 8, use_of(g) & 1);
+                if (fine) fine = tree_wait(misc + kTreeBarSFull + buf * 8, use_of(g) & 1);
                 fine = __all_sync(0xffffffffu, fine);
                 tc_fence_after();
                 // What the row sees of the tile, where that is not all of it; a negative scale takes the same way,
@@ -265,7 +265,7 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                     l *= alpha;
                     if (j > seg.t0) {
                         // the accumulator holds the tiles before this one once their MMAs are complete
-                        if (fine) fine = tree_poll(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
+                        if (fine) fine = tree_wait(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
                         fine = __all_sync(0xffffffffu, fine);
                         tc_fence_after();
 #pragma unroll 1
@@ -318,7 +318,7 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                 if (lane == 0) mbarrier_arrive(misc + kTreeBarPFull + buf * 8);
             }
             // ---- the segment's end: the accumulator divided by the sum, to the output or the workspace ----
-            if (fine) fine = tree_poll(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
+            if (fine) fine = tree_wait(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
             fine = __all_sync(0xffffffffu, fine);
             tc_fence_after();
             const bool empty = !live || l == 0.f;                     // (a NaN sum is not an empty row's)

@@ -176,12 +176,12 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
             queue.done(k, lane);
             if (seg.b < 0) break;
             for (int j = seg.t0; j < seg.t1 && fine; ++j, ++g) {
-                fine = __all_sync(0xffffffffu, tree_poll(misc + kTreeBarPFull, g & 1));
+                fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarPFull, g & 1));
 #pragma unroll
                 for (int item = 0; item < kItems; ++item) {
                     if (!fine) break;
                     const int n = g * kItems + item, slot = n % kVSlots;
-                    fine = __all_sync(0xffffffffu, tree_poll(misc + kTreeBarVFull + slot * 8, (n / kVSlots) & 1));
+                    fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarVFull + slot * 8, (n / kVSlots) & 1));
                     if (!fine) break;
                     tc_fence_after();
                     // V item read MN-major (M = 128 dims): its 64-dim panels kTreePanelBytes apart (the same panel
@@ -209,14 +209,17 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
         const unsigned lanes = tmem + ((unsigned)((warp & 3) * 32) << 16);
         float *by_warp = reinterpret_cast<float *>(misc_ptr + kTreeMiscBytes);   // [N][4]: a row's maxima, or sums, by warp
         float *offsets = by_warp + N * 4;                             // [N]: the rows' offsets as they were last moved
-        const int rows_here = p.nodes_per_block * p.group;            // <= N
+        const int rows_here = p.nodes_per_block * p.group;            // <= N: all the tree's rows
+        const int group_inverse = 65536 / p.group + 1;
+        auto node_of = [&](int r) -> int { return r * group_inverse >> 16; };      // r / p.group (exact for r < 64)
+        const int q_heads = a.heads * p.group;
         const float scale = a.scale_log2e;
         constexpr float kTooLarge = kGroupLag + kGroupWeightLog2;
         bool fine = true;
         float x[kCols];
         // Waits for the logits of a tile and asks for this thread's.
         auto request = [&](int tile) {
-            if (fine) fine = tree_poll(misc + kTreeBarSFull + (tile & 1) * 8, (tile >> 1) & 1);
+            if (fine) fine = tree_wait(misc + kTreeBarSFull + (tile & 1) * 8, (tile >> 1) & 1);
             fine = __all_sync(0xffffffffu, fine);
             tc_fence_after();
 #pragma unroll
@@ -236,10 +239,15 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
             // (the words of four segments ahead: no warp is more than two segments from another)
             if (threadIdx.x < 4) reinterpret_cast<volatile unsigned *>(misc_ptr + kTreePoison)[((k + 4) & 7) * 4 + threadIdx.x] = 0u;
             const int live_rows = min(rows_here, seg.nodes * p.group);
-            // What the group's rows see of the tree, lane r row row0 + r (asked for here, needed at the last tiles).
-            TreeRow mine = {0, 0, false};
-            if (t1 * kTreeTile > prefix && lane < kCols && row0 + lane < live_rows)
-                mine = tree_row(p.tree, seg.b, (row0 + lane) / p.group, seg.nodes);
+            // What the group's rows see of the tree, lane r row row0 + r: asked for here, looked at in the last tiles
+            // (by loads that the compiler does not move, nor waits for before they are used).
+            const bool my_row = t1 * kTreeTile > prefix && lane < kCols && row0 + lane < live_rows;
+            uint64_t my_lo = 0, my_hi = 0;
+            if (my_row) {
+                const uint64_t *words = p.tree.mask + ((int64_t)seg.b * p.tree.tokens + node_of(row0 + lane)) * p.tree.words;
+                asm volatile("ld.global.b64 %0, [%1];" : "=l"(my_lo) : "l"(words) : "memory");
+                if (p.tree.words > 1) asm volatile("ld.global.b64 %0, [%1];" : "=l"(my_hi) : "l"(words + 1) : "memory");
+            }
             // Two rows at a time: the weight exponent's offset kGroupWeightLog2 - reference, and this thread's
             // sums; sums and accumulator carry kGroupWeightScale.
             float2 offset[kCols / 2], l[kCols / 2];
@@ -254,13 +262,13 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                 const bool masked = start + kTreeTile > prefix;       // uniform
                 unsigned seen_by = ~0u;                               // the group's rows that see this thread's token
                 if (masked) {
-                    copies.template clean_values<32 / Geo::kGroups>(seg, j, g, (warp & 3) * 32 + group * (32 / Geo::kGroups), poison, fine);
                     // The 32 tokens of this warp are columns of the rows' bits: 32 votes transpose them.
                     const int first = start + (warp & 3) * 32 - prefix;            // the node of lane 0's token
+                    const TreeRow mine = TreeRow{my_lo, my_hi, my_row}.cut(seg.nodes);
                     const Bits128 bits = {mine.lo, mine.hi};
-                    unsigned window = mine.all ? ~0u : 0u;
+                    unsigned window = my_row ? ~0u : 0u;
                     if (first >= 0) window = first < 128 ? bits.shifted_down(first).word(0) : 0u;
-                    else if (first > -32) window = bits.word(0) << -first | (mine.all ? (1u << -first) - 1u : 0u);
+                    else if (first > -32) window = bits.word(0) << -first | (my_row ? (1u << -first) - 1u : 0u);
 #pragma unroll 8
                     for (int i = 0; i < 32; ++i) {
                         const unsigned rows = __ballot_sync(0xffffffffu, window >> i & 1u);
@@ -295,7 +303,7 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                     if (!group_any(vote_id, fmaxf(most, most_odd) > kTooLarge)) break;
                     // ---- some row's reference moves (rare after a segment's first tile) ----
                     if (j > t0) {                                 // the accumulator holds the tiles before this one
-                        if (fine) fine = tree_poll(misc + kTreeBarPvDone, (g - 1) & 1);
+                        if (fine) fine = tree_wait(misc + kTreeBarPvDone, (g - 1) & 1);
                         fine = __all_sync(0xffffffffu, fine);
                         tc_fence_after();
                     }
@@ -357,8 +365,10 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                     lo[r] = pack_half2(rest.x, rest.y);
                 }
                 if (g > 0) {                                          // the previous tile's MMAs have read the weights
-                    if (fine) fine = tree_poll(misc + kTreeBarPvDone, (g - 1) & 1);
+                    if (fine) fine = tree_wait(misc + kTreeBarPvDone, (g - 1) & 1);
                 }
+                // (late, so that the value tile has had time to land)
+                if (masked) copies.template clean_values<32 / Geo::kGroups>(seg, j, g, (warp & 3) * 32 + group * (32 / Geo::kGroups), poison, fine);
                 unsigned char *weights = smem + Geo::kPOffset + row0 * 256 + t * 16;
 #pragma unroll
                 for (int r = 0; r < kCols / 2; r += 4) {
@@ -379,28 +389,25 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                 const float sum = warp_reduce16<false>(x, lane);
                 if ((lane & 1) == 0) by_warp[(row0 + r0 + warp_reduce16_row(lane)) * 4 + (warp & 3)] = sum;
             }
-            if (fine) fine = tree_poll(misc + kTreeBarPvDone, (g - 1) & 1);
-            fine = __all_sync(0xffffffffu, fine);
-            tc_fence_after();
             group_sync(sync_id);
             const bool whole = seg.whole();
             if (t < kCols) {
-                // one thread per row: its sum's inverse, and the row it goes to (-1: none)
-                const int r = row0 + t, node = r / p.group;
+                // one thread per row: its sum's inverse (0: a row of zeros) and its log-sum-exp
+                const int r = row0 + t;
                 const float4 sums = *reinterpret_cast<const float4 *>(by_warp + r * 4);
                 const float total = (sums.x + sums.y) + (sums.z + sums.w);
                 const bool empty = r >= live_rows || total == 0.f;    // (a NaN sum is not an empty row's)
                 const float lse2 = empty ? kMinusHuge : log2f(total) - offsets[r];
-                // (row numbers are below 2^31: checked by the host)
-                int to = -1;
-                if (r < rows_here && node < p.tree.tokens && fine) {
-                    const int out_row = (seg.b * p.tree.tokens + node) * (a.heads * p.group) + seg.hk * p.group + (r - node * p.group);
-                    to = whole ? out_row : seg.slot * p.item_rows + r;
-                    if (!whole) a.part_lse[to] = lse2;
-                    else if (a.lse) a.lse[to] = empty ? -INFINITY : lse2 * kLn2;
+                if (r < rows_here && fine) {
+                    const int node = node_of(r);
+                    if (!whole) seg.lse[r] = lse2;
+                    else if (seg.lse) seg.lse[node * q_heads + (r - node * p.group)] = empty ? -INFINITY : lse2 * kLn2;
                 }
-                *reinterpret_cast<float4 *>(by_warp + r * 4) = make_float4(empty ? 0.f : 1.f / total, __int_as_float(to), lse2, 0.f);
+                *reinterpret_cast<float2 *>(by_warp + r * 4) = make_float2(empty ? 0.f : __fdividef(1.f, total), lse2);
             }
+            if (fine) fine = tree_wait(misc + kTreeBarPvDone, (g - 1) & 1);
+            fine = __all_sync(0xffffffffu, fine);
+            tc_fence_after();
             group_sync(sync_id);
             const volatile unsigned *taken = poison;
             const bool stray = (taken[0] | taken[1] | taken[2] | taken[3]) != 0u;
@@ -412,25 +419,33 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                 tc_issue_load16(low, lanes + Geo::kOColumn + (acc * 2 + 1) * N + first);
                 tc_loaded16(o);
                 tc_loaded16(low);
-                float more[16];
-                if (stray) {
-#pragma unroll 1
-                    for (int i = 0; i < 16; ++i) {
-                        const float4 row = *reinterpret_cast<const float4 *>(by_warp + (first + i) * 4);
-                        more[i] = __float_as_int(row.y) >= 0 && (D >= 128 || t < D) ? tree_poisoned_value(p, seg, poison, first + i, D, d, row.z) : 0.f;
-                    }
-                }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float2 row = *reinterpret_cast<const float2 *>(by_warp + (first + i) * 4);
-                    const int to = __float_as_int(row.y);
-                    // (an empty row's accumulator may hold anything)
-                    float value = row.x == 0.f ? 0.f : (o[i] + low[i]) * row.x;
-                    if (stray) value += more[i];
-                    if (to >= 0 && (D >= 128 || t < D)) {
-                        if (whole) a.out[(int64_t)to * D + d] = __float2half_rn(value);
-                        else a.part_o[(int64_t)to * D + d] = value;
+                    const float inverse = by_warp[(first + i) * 4];
+                    o[i] = inverse == 0.f ? 0.f : (o[i] + low[i]) * inverse;      // (an empty row's accumulator may hold anything)
+                }
+                const bool writes = fine && (D >= 128 || t < D);
+                if (stray) {
+                    float more[16];
+#pragma unroll 1
+                    for (int i = 0; i < 16; ++i)
+                        more[i] = writes && first + i < rows_here ? tree_poisoned_value(p, seg, poison, first + i, D, d, by_warp[(first + i) * 4 + 1]) : 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] += more[i];
+                }
+                const int rows = writes ? rows_here - first : 0;
+                if (whole) {
+                    __half *out = static_cast<__half *>(seg.out) + d;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int node = node_of(first + i);
+                        if (i < rows) out[(node * q_heads + (first + i - node * p.group)) * D] = __float2half_rn(o[i]);
                     }
+                } else {
+                    float *out = static_cast<float *>(seg.out) + first * D + d;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (i < rows) out[i * D] = o[i];
                 }
                 __syncwarp();
             }
