@@ -55,10 +55,18 @@ template <typename E>
 int launch_verify(const VerifyParams &p, int32_t batch, cudaStream_t stream)
 {
     // Blocks per sequence: as many as leave every thread at least one 16-byte group of a row.
-    const int64_t groups = ceil_div(p.vocab, RowReader<E>::kVec);
+    const int64_t groups = ceil_div(p.vocab, RowReader<E>::kVec) + 1;       // (a row that starts between boundaries has one more)
     unsigned ctas = 1;
     while (ctas < (unsigned)kVerifyMaxCtas && groups >= (int64_t)ctas * 2 * kVerifyThreads) ctas *= 2;
-    return launched(launch_clustered(verify_tree_kernel<E>, (unsigned)batch * ctas, ctas, kVerifyThreads, 0, stream, p));
+    // The largest share of a warp, in groups per thread: what the instances hold, 32 elements at most (16 of 64 bits
+    // and 16 of 32 would leave room for more threads, but a second wave costs less than a second pass over memory).
+    constexpr int kVec = RowReader<E>::kVec;
+    const int64_t held = ceil_div(ceil_div(groups, (int64_t)ctas * kVerifyWarps), 32);
+    if (held <= 8 / kVec) return launched(launch_clustered(verify_tree_kernel<E, 8 / kVec, 256>, (unsigned)batch * ctas, ctas, 256, 0, stream, p));
+    if (held <= 16 / kVec) return launched(launch_clustered(verify_tree_kernel<E, 16 / kVec, 256>, (unsigned)batch * ctas, ctas, 256, 0, stream, p));
+    if (held <= 32 / kVec) return launched(launch_clustered(verify_tree_kernel<E, 32 / kVec, 256>, (unsigned)batch * ctas, ctas, 256, 0, stream, p));
+    if (held <= 64 / kVec) return launched(launch_clustered(verify_tree_kernel<E, 32 / kVec, 512>, (unsigned)batch * ctas, ctas, 512, 0, stream, p));
+    return launched(launch_clustered(verify_tree_streamed_kernel<E>, (unsigned)batch * ctas, ctas, kVerifyThreads, 0, stream, p));
 }
 
 // Moving pages is bound by HBM: enough blocks to fill the GPU, fewer where the list cannot be long.
