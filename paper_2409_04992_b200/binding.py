@@ -6,6 +6,7 @@ library's kernels.  There is no fallback: if the library has not been built, loa
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from pathlib import Path
@@ -146,8 +147,10 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream or None
+    if stream is not None:
+        return stream.cuda_stream or None
+    # (the raw handle: a Stream object per call costs as much as a short kernel)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
 
 
 def _check(status: int) -> None:
@@ -397,13 +400,15 @@ def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.T
 
 def _layers(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor]):
     """The two HOST pointer arrays of the calls that work on all layers at once."""
-    if len(k_caches) != len(v_caches) or not k_caches:
+    n = len(k_caches)
+    caches = [*k_caches, *v_caches]
+    # (whole passes in C: a model has some hundred caches, and a Python loop over them outlasts the kernel)
+    if n == 0 or len(caches) != 2 * n or not all(map(torch.Tensor.is_contiguous, caches)) or \
+            len(set(map(torch.Tensor.numel, caches))) != 1:
         raise InstInferError(ERR_INVALID_ARG)
-    shape = k_caches[0].shape
-    if any(c.shape != shape or not c.is_contiguous() for c in (*k_caches, *v_caches)):
-        raise InstInferError(ERR_INVALID_ARG)
-    array = ctypes.c_void_p * len(k_caches)
-    return array(*(c.data_ptr() for c in k_caches)), array(*(c.data_ptr() for c in v_caches)), len(k_caches)
+    addresses = array.array("Q", map(torch.Tensor.data_ptr, caches))
+    at, _ = addresses.buffer_info()
+    return at, at + 8 * n, n, addresses          # the caller keeps `addresses` alive during the call
 
 
 def kv_keep_path(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor], path: torch.Tensor,
@@ -414,7 +419,7 @@ def kv_keep_path(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tens
     """instinfer_kv_keep_path: one cache per layer ([B,H,s_max,D], or pools [P,H,T,D] with
     block_table); path [B, tree_tokens]."""
     batch, tree_tokens = path.shape
-    k, v, n_layers = _layers(k_caches, v_caches)
+    k, v, n_layers, keep = _layers(k_caches, v_caches)
     _, heads, rows, head_dim = k_caches[0].shape
     if block_table is None:
         max_blocks, block_tokens, phys, s_max = 0, 0, 0, rows
@@ -446,7 +451,7 @@ def kv_resize(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tensor], 
               stream: Optional[torch.cuda.Stream] = None) -> None:
     """instinfer_kv_resize: one pool [P,H,T,D] per layer; new_lens may be seq_lens."""
     batch, max_blocks = block_table.shape
-    k, v, n_layers = _layers(k_pools, v_pools)
+    k, v, n_layers, keep = _layers(k_pools, v_pools)
     phys, heads, block_tokens, head_dim = k_pools[0].shape
     _check(load().instinfer_kv_resize(
         k, v, n_layers, _ptr(block_table), _ptr(block_refs), _ptr(seq_lens), _ptr(want_lens), _ptr(new_lens),
@@ -466,7 +471,7 @@ def kv_defragment(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tenso
     """instinfer_kv_defragment: one pool [P,H,T,D] per layer; the new table and counts may be the
     old ones; blocks_used int32 [1]."""
     batch, max_blocks = block_table.shape
-    k, v, n_layers = _layers(k_pools, v_pools)
+    k, v, n_layers, keep = _layers(k_pools, v_pools)
     phys, heads, block_tokens, head_dim = k_pools[0].shape
     _check(load().instinfer_kv_defragment(
         k, v, n_layers, _ptr(block_table), _ptr(new_block_table), _ptr(block_refs), _ptr(new_block_refs),
