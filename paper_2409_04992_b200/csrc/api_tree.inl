@@ -20,14 +20,19 @@ int tree_attention_shape(int32_t batch, int32_t tree_tokens, int32_t q_heads, in
 
 // ---- the tcgen05 form ----
 
-// Rows of the partial results: two slots per piece, at most 1 + short_pieces pieces per block and one more; the
-// ticket counter lies behind them.
+// Rows of the partial results: two slots per piece, at most 1 + short_pieces pieces per block and one more.  Behind
+// them lie the items' pieces and the ticket counter.
 size_t tree_slot_rows(const TreeRows &r) { return (size_t)2 * (sm_count() * (1 + r.short_pieces) + 1) * r.item_rows; }
 
-size_t tree_umma_workspace(int32_t tree_tokens, int32_t group, int32_t head_dim)
+size_t tree_partials_bytes(const TreeRows &r, int32_t head_dim)
+{
+    return (tree_slot_rows(r) * (head_dim + 1) * sizeof(float) + 255) / 256 * 256;
+}
+size_t tree_umma_workspace(int64_t pairs, int32_t tree_tokens, int32_t group, int32_t head_dim)
 {
     if (group > kTreeTile) return 0;
-    return (tree_slot_rows(tree_rows(tree_tokens, group, head_dim)) * (head_dim + 1) * sizeof(float) + 255) / 256 * 256 + 256;
+    const TreeRows r = tree_rows(tree_tokens, group, head_dim);
+    return tree_partials_bytes(r, head_dim) + ((size_t)pairs * r.row_blocks * sizeof(int2) + 255) / 256 * 256 + 256;
 }
 
 // Blocks of 16, 32 or 64 tokens, or of a multiple of 128: no tile straddles blocks of another kind.
@@ -112,22 +117,24 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
         const int row_parts = (rows.item_rows + kTreeMergeRows - 1) / kTreeMergeRows;
         const int32_t box = paged && block_tokens < kTreeTile ? block_tokens : kTreeTile;
         TreeLaunch t = {};
-        if (items * row_parts < (int64_t)1 << 31 && items * ceil_div(max_seq_len, kTreeTile) < (int64_t)1 << 31 &&
+        if (items * row_parts < (int64_t)1 << 31 && items * (ceil_div(max_seq_len, kTreeTile) + kTreeItemCost) < (int64_t)1 << 31 &&
             make_query_map(&t.map_q, q, batch, tree_tokens, q_heads, p.group, head_dim, rows.nodes_per_block) &&
             make_cache_map(&t.map_k, k_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box) &&
             make_cache_map(&t.map_v, v_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box)) {
             t.p.a = p.a;
             t.p.a.part_lse = p.a.part_o + tree_slot_rows(rows) * head_dim;
             t.p.short_pieces = rows.short_pieces;
+            unsigned char *behind = static_cast<unsigned char *>(workspace) + tree_partials_bytes(rows, head_dim);
+            t.p.item_pieces = reinterpret_cast<int2 *>(behind);
             t.p.ticket = reinterpret_cast<unsigned *>(static_cast<unsigned char *>(workspace) +
-                                                      tree_umma_workspace(tree_tokens, p.group, head_dim) - 256);
+                                                      tree_umma_workspace(pairs, tree_tokens, p.group, head_dim) - 256);
             t.p.tree = p.tree;
             t.p.batch = batch;
             t.p.group = p.group;
             t.p.nodes_per_block = rows.nodes_per_block;
             t.p.row_blocks = rows.row_blocks;
             t.p.item_rows = rows.item_rows;
-            const int64_t most_tiles = items * ceil_div(max_seq_len, kTreeTile);
+            const int64_t most_tiles = items * (ceil_div(max_seq_len, kTreeTile) + kTreeItemCost);
             t.grid = (unsigned)(most_tiles < sm_count() ? most_tiles : sm_count());
             t.merge_grid = (unsigned)(items * row_parts);
             t.row_parts = row_parts;
@@ -156,7 +163,7 @@ size_t instinfer_tree_workspace_bytes(int32_t batch, int32_t tree_tokens, int32_
     const int32_t rows = q_heads / kv_heads * tree_tokens, groups = (rows + kGroupRows - 1) / kGroupRows;
     // enough for either implementation: which one runs also depends on the cache layout
     const size_t warp_level = grouped_workspace_for(pairs, rows, head_dim, make_plan(pairs * groups, max_seq_len, grouped_rules(head_dim)));
-    const size_t umma = tree_umma_workspace(tree_tokens, q_heads / kv_heads, head_dim);
+    const size_t umma = tree_umma_workspace(pairs, tree_tokens, q_heads / kv_heads, head_dim);
     return warp_level > umma ? warp_level : umma;
 }
 

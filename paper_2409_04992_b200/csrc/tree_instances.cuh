@@ -28,7 +28,7 @@ int launch_tree_umma(const TreeLaunch &t)
     }
     cudaError_t err = launch_overlapped(kKernel, t.grid, kThreadsOf, kSmem, t.stream, t.p, t.map_q, t.map_k, t.map_v);
     if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) return INSTINFER_ERR_CUDA;
-    err = launch_overlapped(tree_merge_kernel<D>, t.merge_grid, kTreeMergeThreads, 0, t.stream, t.p, (int)t.grid, t.row_parts);
+    err = launch_overlapped(tree_merge_kernel<D>, t.merge_grid, kTreeMergeThreads, 0, t.stream, t.p, t.row_parts);
     return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? INSTINFER_OK : INSTINFER_ERR_CUDA;
 }
 template <int D, bool kPaged, int kStreams>

@@ -7,7 +7,10 @@
 // piece starts or ends inside leave partial results, two per piece at most (with the fixed chunks of the
 // other kernels the partials of 64 rows are 8 % of the traffic).  Why not equal shares alone: the SMs do not reach
 // memory equally fast, with equal shares of 207 tiles the first was done after 312 us and the last after 399.
-// Few tiles are cut into equal shares, one per block.  The cuts follow from the lengths alone, so a result
+// (An item that is short next to the long pieces stays whole with the long piece that it starts in.)
+// Few tiles are cut into equal shares, one per block.  A segment's set-up and end cost as much as some tiles, so an
+// item counts that many more (in front of its first): a block full of short sequences gets fewer of
+// them (104 -> 70 us at 35 items of 1 to 157 tiles).  The cuts follow from the lengths alone, so a result
 // depends neither on which block draws a piece nor on the placement of the cache's blocks.
 //
 // A block has softmax warps and four single-purpose warps, which hand tiles over through mbarriers:
@@ -53,21 +56,21 @@ constexpr int kTreeBarKFull = 0;       // [6]
 constexpr int kTreeBarKEmpty = 48;     // [6]
 constexpr int kTreeBarVFull = 96;      // [6]
 constexpr int kTreeBarVEmpty = 144;    // [6]
-constexpr int kTreeBarSFull = 192;     // [2] logits of a unit are in tensor memory
-constexpr int kTreeBarPFull = 208;     // [2] its weights are where the output MMAs read them
-constexpr int kTreeBarPvDone = 224;    // [2] its output MMAs are complete
-constexpr int kTreeBarQFull = 240;
-constexpr int kTreeBarQEmpty = 248;
-constexpr int kTreeBarSFree = 256;     // [2] the logits have been read
-constexpr int kTreeTmemPtr = 272;
-constexpr int kTreeTotal = 280;        // number of tiles
-constexpr int kTreeBarSegFull = 288;   // [4] a segment is announced
-constexpr int kTreeBarSegEmpty = 320;  // [4] everyone is done with it
-constexpr int kTreePoison = 352;       // [8][4] words: nodes of a segment whose value row is not finite, by segment number
-constexpr int kTreeSegments = 480;     // [4] TreeSegment
+constexpr int kTreeBarSFull = 192;     // [4] logits of a unit are in tensor memory
+constexpr int kTreeBarPFull = 224;     // [4] its weights are where the output MMAs read them
+constexpr int kTreeBarPvDone = 256;    // [4] its output MMAs are complete
+constexpr int kTreeBarQFull = 288;
+constexpr int kTreeBarQEmpty = 296;
+constexpr int kTreeBarSFree = 304;     // [2] the logits have been read
+constexpr int kTreeTmemPtr = 320;
+constexpr int kTreeTotal = 328;        // number of tiles
+constexpr int kTreeBarSegFull = 336;   // [4] a segment is announced
+constexpr int kTreeBarSegEmpty = 368;  // [4] everyone is done with it
+constexpr int kTreePoison = 400;       // [8][4] words: nodes of a segment whose value row is not finite, by segment number
+constexpr int kTreeSegments = 528;     // [4] TreeSegment
 constexpr int kTreeEntryBytes = 56;
-constexpr int kTreeScan = 480;         // [16] ints: per-warp sums of the set-up's scan, before the first segment
-constexpr int kTreeMiscBytes = 480 + 4 * kTreeEntryBytes;
+constexpr int kTreeScan = 528;         // [16] ints: per-warp sums of the set-up's scan, before the first segment
+constexpr int kTreeMiscBytes = 528 + 4 * kTreeEntryBytes;
 static_assert(kTreeScan + 16 * 4 <= kTreeMiscBytes && kTreeMiscBytes % 16 == 0, "misc region too small");
 
 struct TreeParams {
@@ -79,14 +82,20 @@ struct TreeParams {
     int32_t row_blocks;        // items per (sequence, KV head), of one or two row blocks each
     int32_t item_rows;         // rows of an item: all its row blocks'
     int32_t short_pieces;      // drawn pieces per block
+    int2 *item_pieces;         // [items] the pieces with the item's first and its last tile, for the merge
     unsigned *ticket;          // zero before the launch where W can reach kTreeDrawnTiles per block
 };
+
+constexpr int kTreeItemCost = 4;
 
 // Number of tiles of a sequence's items.
 __device__ __forceinline__ int tree_tiles(int len, int nodes)
 {
     return nodes > 0 ? (int)(((unsigned)len + kTreeTile - 1) / kTreeTile) : 0;
 }
+
+// What an item counts in the row of tiles.
+__device__ __forceinline__ int tree_weight(int tiles) { return tiles > 0 ? tiles + kTreeItemCost : 0; }
 
 // The cut of the row of tiles (see above); piece c is [first(c), first(c + 1)), count() pieces in all.
 constexpr int kTreeDrawnTiles = 24;    // tiles per block from which on pieces are drawn
@@ -162,44 +171,58 @@ struct TreeFinder {
     {
         TreeSegment s;
         s.b = -1;
-        if (tile >= end && piece < n_pieces) {
-            const unsigned got = __shfl_sync(0xffffffffu, drawn, 0);
-            begin(p, got < (unsigned)n_pieces ? (int)got : n_pieces, lane);
-        }
-        if (piece >= n_pieces) return s;
         const int items = p.a.heads * p.row_blocks;
-        while (tile >= limit) {    // (tile < W: some sequence has it)
-            const int from = b + 1;
-            if (from >= p.batch) return s;
-            int n = 0, l = 0;
-            if (from + lane < p.batch) l = checked_tree(p.tree, p.a.seq_lens, p.a.max_seq_len, nullptr, from + lane, false, n);
-            const int mine = tree_tiles(l, n) * items;
-            int sum = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int up = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += up;
+        do {
+            if (tile >= end && piece < n_pieces) {
+                const unsigned got = __shfl_sync(0xffffffffu, drawn, 0);
+                begin(p, got < (unsigned)n_pieces ? (int)got : n_pieces, lane);
             }
-            const unsigned reached = __ballot_sync(0xffffffffu, limit + sum > tile);
-            const int at = reached ? __ffs(reached) - 1 : 31;
-            len = __shfl_sync(0xffffffffu, l, at);
-            nodes = __shfl_sync(0xffffffffu, n, at);
-            base = limit + __shfl_sync(0xffffffffu, sum - mine, at);
-            limit = limit + __shfl_sync(0xffffffffu, sum, at);
-            b = from + at;
-        }
+            if (piece >= n_pieces) return s;
+            while (tile >= limit) {    // (tile < W: some sequence has it)
+                const int from = b + 1;
+                if (from >= p.batch) return s;
+                int n = 0, l = 0;
+                if (from + lane < p.batch) l = checked_tree(p.tree, p.a.seq_lens, p.a.max_seq_len, nullptr, from + lane, false, n);
+                const int mine = tree_weight(tree_tiles(l, n)) * items;
+                int sum = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int up = __shfl_up_sync(0xffffffffu, sum, o);
+                    if (lane >= o) sum += up;
+                }
+                const unsigned reached = __ballot_sync(0xffffffffu, limit + sum > tile);
+                const int at = reached ? __ffs(reached) - 1 : 31;
+                len = __shfl_sync(0xffffffffu, l, at);
+                nodes = __shfl_sync(0xffffffffu, n, at);
+                base = limit + __shfl_sync(0xffffffffu, sum - mine, at);
+                limit = limit + __shfl_sync(0xffffffffu, sum, at);
+                b = from + at;
+            }
+            s.n_tiles = tree_tiles(len, nodes);
+            if (b >= p.batch || s.n_tiles == 0) return s;     // (lengths that change under the kernel's hands)
+            const int weight = tree_weight(s.n_tiles), inside = tile - base, item = inside / weight;
+            const int from = inside - item * weight;
+            int to = min(weight, from + (end - tile));
+            s.hk = item / p.row_blocks;
+            s.rb = item - s.hk * p.row_blocks;
+            s.t0 = max(0, from - kTreeItemCost);
+            // An item that is short next to the long pieces and starts in one stays whole, with the piece that has its start.
+            if (pieces.step > 0 && 2 * weight <= pieces.length && tile - from < pieces.drawn) {
+                to = weight;
+                if (from > 0) s.t0 = weight;                  // another piece has it
+            }
+            s.t1 = to - kTreeItemCost;
+            tile += to - from;
+        } while (s.t1 <= s.t0);                               // only of the item's extra weight
+        s.b = b;
         s.len = len;
         s.nodes = nodes;
-        s.n_tiles = tree_tiles(len, nodes);
-        if (b >= p.batch || s.n_tiles == 0) return s;         // (lengths that change under the kernel's hands)
-        s.b = b;
-        const int inside = tile - base, item = inside / s.n_tiles;
-        s.hk = item / p.row_blocks;
-        s.rb = item - s.hk * p.row_blocks;
-        s.t0 = inside - item * s.n_tiles;
-        s.t1 = min(s.n_tiles, s.t0 + (end - tile));
+        if (lane == 0) {
+            int2 *of_item = p.item_pieces + (int64_t)b * items + s.hk * p.row_blocks + s.rb;
+            if (s.t0 == 0) of_item->x = piece;
+            if (s.t1 == s.n_tiles) of_item->y = piece;
+        }
         s.slot = 2 * piece + (s.t0 == 0 ? 1 : 0);
-        tile += s.t1 - s.t0;
         const int64_t row = (int64_t)b * p.tree.tokens * (p.a.heads * p.group) + s.hk * p.group, slot_row = (int64_t)s.slot * p.item_rows;
         s.out = s.whole() ? static_cast<void *>(p.a.out + row * D) : static_cast<void *>(p.a.part_o + slot_row * D);
         s.lse = !s.whole() ? p.a.part_lse + slot_row : p.a.lse ? p.a.lse + row : nullptr;
@@ -232,7 +255,7 @@ __device__ __forceinline__ void tree_count_tiles(const TreeParams &p, unsigned c
     for (int b = threadIdx.x; b < p.batch; b += threads) {
         int nodes;
         const int len = checked_tree(p.tree, p.a.seq_lens, p.a.max_seq_len, p.a.status, b, blockIdx.x == 0, nodes);
-        mine += tree_tiles(len, nodes);
+        mine += tree_weight(tree_tiles(len, nodes));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
@@ -285,6 +308,13 @@ __device__ __forceinline__ void tc_mma_f16_ts(unsigned d_tmem, unsigned a_tmem, 
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                  :: "r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// 32 bytes to a 32-byte boundary.
+__device__ __forceinline__ void store_32b(void *to, const unsigned (&v)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 :: "l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
 // Two 32-bit operations in one instruction.
@@ -643,11 +673,11 @@ __device__ __forceinline__ void tree_init_barriers(unsigned misc, unsigned char 
         mbarrier_init(misc + kTreeBarVEmpty + s * 8, 1);
     }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < 4; ++s) {
         mbarrier_init(misc + kTreeBarSFull + s * 8, 1);
         mbarrier_init(misc + kTreeBarPFull + s * 8, softmax_warps);
         mbarrier_init(misc + kTreeBarPvDone + s * 8, 1);
-        mbarrier_init(misc + kTreeBarSFree + s * 8, softmax_warps);
+        if (s < 2) mbarrier_init(misc + kTreeBarSFree + s * 8, softmax_warps);
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -661,88 +691,85 @@ __device__ __forceinline__ void tree_init_barriers(unsigned misc, unsigned char 
 }
 
 // Joins the partial results of the items that more than one piece has a part of, and zeroes the rows of
-// sequences without work; one thread block per item and kTreeMergeRows rows, one warp per row.
-constexpr int kTreeMergeThreads = 128;
-constexpr int kTreeMergeRows = 16;
+// sequences without work; a block takes kTreeMergeRows rows of an item, a warp one after the other of them.  The work is a chain of short loads (the item's pieces, their
+// log-sum-exps, the partials), so each link is one round of loads: a lane per piece, then eight partials at a time.
+constexpr int kTreeMergeThreads = 256;
+constexpr int kTreeMergeRows = 32;
 
 template <int D>
 __global__ void __launch_bounds__(kTreeMergeThreads)
-tree_merge_kernel(const TreeParams p, int blocks, int row_parts)
+tree_merge_kernel(const TreeParams p, int row_parts)
 {
     const AttnParams &a = p.a;
-    __shared__ int sums[2][kTreeMergeThreads / 32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int part = blockIdx.x % row_parts;
-    const int item = blockIdx.x / row_parts;                          // (sequence, KV head, row block)
+    const int lane = threadIdx.x & 31;
+    const int part = blockIdx.x % row_parts, item = blockIdx.x / row_parts;           // (sequence, KV head, row block)
     const int items = a.heads * p.row_blocks;
     const int b = item / items, in_seq = item - b * items;
     const int hk = in_seq / p.row_blocks, rb = in_seq - hk * p.row_blocks;
     allow_next_kernel();
     wait_for_previous_kernels();
     int nodes;
+    const int2 pieces = p.item_pieces[item];
     const int len = checked_tree(p.tree, a.seq_lens, a.max_seq_len, nullptr, b, false, nodes);
-    const int n_tiles = tree_tiles(len, nodes);
-    int c0 = 0, c1 = 0;
-    if (n_tiles > 0) {
-        // tiles before this sequence, and all of them
-        int before = 0, all = 0;
-        for (int i = threadIdx.x; i < p.batch; i += kTreeMergeThreads) {
-            int n;
-            const int other = checked_tree(p.tree, a.seq_lens, a.max_seq_len, nullptr, i, false, n);
-            const int tiles = tree_tiles(other, n) * items;
-            if (i < b) before += tiles;
-            all += tiles;
+    const int c0 = pieces.x, n = tree_tiles(len, nodes) > 0 ? pieces.y - c0 + 1 : 0;
+    if (n == 1) return;                                               // one piece had it all: the result is written
+#pragma unroll 1
+    for (int in_part = threadIdx.x >> 5; in_part < kTreeMergeRows; in_part += kTreeMergeThreads / 32) {
+        const int r = part * kTreeMergeRows + in_part;
+        const int node = rb * (p.item_rows / p.group) + r / p.group, head = r % p.group;
+        if (r >= p.item_rows || node >= p.tree.tokens) break;
+        const int64_t out_row = ((int64_t)b * p.tree.tokens + node) * ((int64_t)a.heads * p.group) + (int64_t)hk * p.group + head;
+        // (the item's start went to its piece's second slot, all else to the first one)
+        auto slot_row = [&](int i) -> int64_t { return (int64_t)(2 * (c0 + i) + (i == 0 ? 1 : 0)) * p.item_rows + r; };
+        float top = kMinusHuge, total = 0.f;
+        bool any_nan = false;
+        for (int i = lane; i < n; i += 32) {
+            const float lse = a.part_lse[slot_row(i)];
+            top = fmaxf(top, lse);
+            any_nan = any_nan || lse != lse;
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            before += __shfl_xor_sync(0xffffffffu, before, o);
-            all += __shfl_xor_sync(0xffffffffu, all, o);
-        }
-        if (lane == 0) {
-            sums[0][warp] = before;
-            sums[1][warp] = all;
-        }
-        __syncthreads();
-        before = all = 0;
-        for (int w = 0; w < kTreeMergeThreads / 32; ++w) {
-            before += sums[0][w];
-            all += sums[1][w];
-        }
-        const int first = before + in_seq * n_tiles, last = first + n_tiles - 1;
-        const TreePieces pieces(all, blocks, p.short_pieces);
-        c0 = pieces.piece_of(first);
-        c1 = pieces.piece_of(last);
-        if (c0 == c1) return;                                         // one piece has it all: the result is written
-    }
-    constexpr int kPer = D / 32;                                      // dims per lane
-    for (int r = part * kTreeMergeRows + warp; r < min((part + 1) * kTreeMergeRows, p.item_rows); r += kTreeMergeThreads / 32) {
-        const int node = rb * (p.item_rows / p.group) + r / p.group, head = r % p.group;
-        if (node >= p.tree.tokens) continue;
-        const int64_t out_row = ((int64_t)b * p.tree.tokens + node) * ((int64_t)a.heads * p.group) + (int64_t)hk * p.group + head;
-        float top = kMinusHuge, total = 0.f, acc[kPer];
-        bool any_nan = false;
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const bool empty = !(top > kMinusHuge) && !__any_sync(0xffffffffu, any_nan);
+        // A lane's dims: kVecs runs of kWidth.
+        constexpr int kPer = D / 32, kVecs = kPer >= 4 ? kPer / 4 : 1, kWidth = kPer / kVecs, kDeep = 8 / kVecs;
+        float acc[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
-        auto slot_row = [&](int c) -> int64_t { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * p.item_rows + r; };
-        if (n_tiles > 0) {
-            for (int c = c0; c <= c1; ++c) {
-                const float lse = a.part_lse[slot_row(c)];
-                top = fmaxf(top, lse);
-                any_nan = any_nan || lse != lse;
-            }
-            if (top > kMinusHuge || any_nan) {
-                for (int c = c0; c <= c1; ++c) {
-                    const float w = fast_exp2(a.part_lse[slot_row(c)] - top);
-                    total += w;
-                    const float *from = a.part_o + slot_row(c) * D + lane * kPer;
+        for (int i0 = 0; i0 < n && !empty; i0 += 32) {
+            const float mine = i0 + lane < n ? fast_exp2(a.part_lse[slot_row(i0 + lane)] - top) : 0.f;
+            const int here = min(32, n - i0);
+            for (int i = 0; i < here; i += kDeep) {
+                float x[kDeep][kPer];
 #pragma unroll
-                    for (int i = 0; i < kPer; ++i) acc[i] = fmaf(w, from[i], acc[i]);
+                for (int u = 0; u < kDeep; ++u) {
+                    if (i + u < here) {
+                        const float *from = a.part_o + slot_row(i0 + i + u) * D + lane * kWidth;
+#pragma unroll
+                        for (int v = 0; v < kVecs; ++v) {
+                            if constexpr (kWidth == 4) *reinterpret_cast<float4 *>(&x[u][4 * v]) = *reinterpret_cast<const float4 *>(from + v * 128);
+                            else *reinterpret_cast<float2 *>(&x[u][0]) = *reinterpret_cast<const float2 *>(from);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kDeep; ++u) {
+                    const float w = __shfl_sync(0xffffffffu, mine, (i + u) & 31);
+                    if (i + u < here) {
+                        total += w;
+#pragma unroll
+                        for (int d = 0; d < kPer; ++d) acc[d] = fmaf(w, x[u][d], acc[d]);
+                    }
                 }
             }
         }
-        const bool empty = !(top > kMinusHuge) && !any_nan;
+        const float inverse = empty ? 0.f : 1.f / total;
+        unsigned *to = reinterpret_cast<unsigned *>(a.out + out_row * D);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) a.out[out_row * D + lane * kPer + i] = __float2half_rn(empty ? 0.f : acc[i] / total);
+        for (int i = 0; i < kPer; i += 2) {
+            const int d = lane * kWidth + i / 4 * 128 + i % 4;            // (kWidth 2: i is 0)
+            to[d / 2] = empty ? 0u : pack_half2(acc[i] * inverse, acc[i + 1] * inverse);
+        }
         if (a.lse && lane == 0) a.lse[out_row] = empty ? -INFINITY : (top + log2f(total)) * kLn2;
     }
 }

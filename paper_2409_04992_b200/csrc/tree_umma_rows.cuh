@@ -12,8 +12,10 @@
 //
 // kStreams = 1 (at most 128 rows, or head size 256): two logit buffers, so that S of the next tile is
 // computed while the softmax warps work on this one.  kStreams = 2: two row blocks share every K and V
-// tile; each has its own softmax warps, logit buffer and accumulator (tensor memory is full then), and
-// the tensor cores serve them in turn.
+// tile; each has its own softmax warps and accumulator, and as tensor memory is full then, its two logit
+// buffers hold half a tile each (64 tokens): with one buffer of a whole tile per row block the softmax
+// waited for the MMAs that use the weights and for those of the next logits, 2700 of 6100 cycles a tile.
+// (Leaving the low parts out in this form gave another 11 % and 1.4 times the error.)
 #pragma once
 
 #include "tree_umma_common.cuh"
@@ -29,10 +31,28 @@ struct TreeRowsGeometry {
     static constexpr int kSmemBytes = kMiscOffset + kTreeMiscBytes + 1024;     // room to align to 1024 bytes
     static constexpr int kSoftmaxWarps = 4 * kStreams;
     static constexpr int kThreads = (kSoftmaxWarps + 4) * 32;
+    static constexpr int kUnit = kStreams == 1 ? 128 : 64;               // tokens whose logits and weights go through a buffer at once
+    static constexpr int kUnits = 128 / kUnit;                           // per tile
     static constexpr int kOColumn = 256;                                 // tensor memory: two logit buffers, then the accumulators
     static_assert(kOColumn + kStreams * D <= 512, "tensor memory");
     static_assert(kSmemBytes <= 227 * 1024, "one block per SM must fit");
 };
+
+template <int kWords>
+__device__ __forceinline__ void store_row(void *to, const unsigned (&w)[kWords])
+{
+    if ((reinterpret_cast<uintptr_t>(to) & 31) == 0) {
+#pragma unroll
+        for (int c = 0; c < kWords; c += 8) {
+            const unsigned v[8] = {w[c], w[c + 1], w[c + 2], w[c + 3], w[c + 4], w[c + 5], w[c + 6], w[c + 7]};
+            store_32b(static_cast<unsigned char *>(to) + 4 * c, v);
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < kWords; c += 4)
+            *reinterpret_cast<uint4 *>(static_cast<unsigned char *>(to) + 4 * c) = make_uint4(w[c], w[c + 1], w[c + 2], w[c + 3]);
+    }
+}
 
 template <int D, bool kPaged, int kStreams>
 __global__ void __launch_bounds__(TreeRowsGeometry<D, kStreams>::kThreads, 1)
@@ -77,8 +97,9 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
     const TreeQueue queue{misc, misc_ptr};
     const TreeCopies<D, kPaged, Ring> copies{p, smem, base, misc, lane};
 
-    // The buffer of a unit (tile number g of this block, stream s) and how often it was used before.
-    auto buffer_of = [](int g, int s) -> int { return kStreams == 1 ? g & 1 : s; };
+    constexpr int kUnit = Geo::kUnit, kUnits = Geo::kUnits;
+    // The buffer of a unit (tile number g of this block, stream s, part h of the tile) and how often it was used before.
+    auto buffer_of = [](int g, int s, int h) -> int { return kStreams == 1 ? g & 1 : 2 * s + h; };
     auto use_of = [](int g) -> int { return kStreams == 1 ? g >> 1 : g; };
 
     if (warp == kWarpK) {
@@ -87,7 +108,7 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
         copies.produce_v(queue, &map_v);
     } else if (warp == kWarpLogits) {
         // ================================ logit MMAs ================================
-        constexpr unsigned idesc = umma_idesc(128, 128, 0, 0);
+        constexpr unsigned idesc = umma_idesc(128, kUnit, 0, 0);
         bool fine = true;
         int g = 0;
         for (int k = 0; fine; ++k) {
@@ -108,8 +129,8 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                     // dims is 32 bytes along the row
                     const uint64_t k_desc = umma_desc(base + slot * kItemBytes, 16, 1024, 2);
 #pragma unroll
-                    for (int s = 0; s < kStreams; ++s) {
-                        const int buf = buffer_of(g, s), use = use_of(g);
+                    for (int u = 0; u < kUnits * kStreams; ++u) {
+                        const int h = u / kStreams, s = u % kStreams, buf = buffer_of(g, s, h), use = use_of(g);
                         if (item == 0 && use >= 1)             // the weights that lie in the buffer have been used
                             fine = fine && __all_sync(0xffffffffu, tree_wait(misc + kTreeBarPvDone + buf * 8, (use - 1) & 1));
                         if (!fine) break;
@@ -118,12 +139,12 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                         if (elect_one()) {
 #pragma unroll
                             for (int ks = 0; ks < 4 * kItemPanels; ++ks)
-                                tc_mma_f16(tmem + buf * 128,
+                                tc_mma_f16(tmem + buf * kUnit,
                                            q_desc + (uint64_t)(((item * kItemPanels + (ks >> 2)) * kTreePanelBytes + (ks & 3) * 32) >> 4),
-                                           k_desc + (uint64_t)(((ks >> 2) * kTreePanelBytes + (ks & 3) * 32) >> 4), idesc,
+                                           k_desc + (uint64_t)(((ks >> 2) * kTreePanelBytes + h * kUnit * 128 + (ks & 3) * 32) >> 4), idesc,
                                            item > 0 || ks > 0);
                             if (item + 1 == kItems) tc_commit(misc + kTreeBarSFull + buf * 8);
-                            if (s + 1 == kStreams) {
+                            if (u + 1 == kUnits * kStreams) {
                                 tc_commit(misc + kTreeBarKEmpty + slot * 8);
                                 if (item + 1 == kItems && j + 1 == seg.t1) tc_commit(misc + kTreeBarQEmpty);
                             }
@@ -147,13 +168,13 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
             if (seg.b < 0) break;
             for (int j = seg.t0; j < seg.t1 && fine; ++j, ++g) {
 #pragma unroll
-                for (int s = 0; s < kStreams; ++s) {
-                    const int buf = buffer_of(g, s);
+                for (int u = 0; u < kUnits * kStreams; ++u) {
+                    const int h = u / kStreams, s = u % kStreams, buf = buffer_of(g, s, h);
                     fine = fine && __all_sync(0xffffffffu, tree_wait(misc + kTreeBarPFull + buf * 8, use_of(g) & 1));
 #pragma unroll
                     for (int item = 0; item < kItems; ++item) {
                         const int n = g * kItems + item, slot = n % kVSlots;
-                        if (s == 0 && fine)
+                        if (u == 0 && fine)
                             fine = __all_sync(0xffffffffu, tree_wait(misc + kTreeBarVFull + slot * 8, (n / kVSlots) & 1));
                         if (!fine) break;
                         tc_fence_after();
@@ -161,15 +182,15 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                         // 16 tokens = 2048 bytes.  Weights of 32 tokens: 16 columns of high, 16 of low parts.
                         const uint64_t v_desc = umma_desc(base + Ring::kVOffset + slot * kItemBytes, kTreePanelBytes, 1024, 2);
                         if (elect_one()) {
-                            const unsigned acc = tmem + Geo::kOColumn + s * D + item * 128, weights = tmem + buf * 128;
+                            const unsigned acc = tmem + Geo::kOColumn + s * D + item * 128, weights = tmem + buf * kUnit;
 #pragma unroll
-                            for (int ks = 0; ks < 8; ++ks) {
+                            for (int ks = 0; ks < kUnit / 16; ++ks) {
                                 const unsigned at = weights + (ks >> 1) * 32 + (ks & 1) * 8;
-                                const uint64_t v_step = v_desc + (uint64_t)((ks * 2048) >> 4);
-                                tc_mma_f16_ts(acc, at, v_step, idesc, j > seg.t0 || ks > 0);
+                                const uint64_t v_step = v_desc + (uint64_t)(((h * (kUnit / 16) + ks) * 2048) >> 4);
+                                tc_mma_f16_ts(acc, at, v_step, idesc, j > seg.t0 || h > 0 || ks > 0);
                                 tc_mma_f16_ts(acc, at + 16, v_step, idesc, 1);
                             }
-                            if (s + 1 == kStreams) tc_commit(misc + kTreeBarVEmpty + slot * 8);
+                            if (u + 1 == kUnits * kStreams) tc_commit(misc + kTreeBarVEmpty + slot * 8);
                             if (item + 1 == kItems) tc_commit(misc + kTreeBarPvDone + buf * 8);
                         }
                         __syncwarp();
@@ -207,14 +228,10 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
             if (live && seg.t1 * kTreeTile > prefix) row = tree_row(p.tree, seg.b, node, seg.nodes);
             float m = kMinusHuge, l = 0.f;                            // l and the accumulator carry kGroupWeightScale
             for (int j = seg.t0; j < seg.t1; ++j, ++g) {
-                const int buf = buffer_of(g, s), start = j * kTreeTile;
-                const unsigned logits = tmem + lanes + buf * 128;
+                const int start = j * kTreeTile;
                 const bool masked = start + kTreeTile > prefix;       // uniform
                 // (stream 0 cleans for both: the output MMAs of a tile start with it)
                 if (masked && s == 0) copies.template clean_values<32>(seg, j, g, (warp & 3) * 32, poison, fine);
-                if (fine) fine = tree_wait(misc + kTreeBarSFull + buf * 8, use_of(g) & 1);
-                fine = __all_sync(0xffffffffu, fine);
-                tc_fence_after();
                 // What the row sees of the tile, where that is not all of it; a negative scale takes the same way,
                 // as it would turn the maximum around.
                 const bool special = masked || a.scale_log2e < 0.f;   // uniform
@@ -238,87 +255,111 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
 #pragma unroll
                     for (int c = 0; c < 32; ++c) x[c] = word >> c & 1u ? x[c] * a.scale_log2e : -INFINITY;
                 };
-                // The row is read twice, 32 columns at a time in short loops, the next columns on their way while these
-                // are worked on: holding all 128 logits unrolls the softmax into some 1500 instructions, and one
-                // warp per scheduler then waits for their fetch half of the time (2000 cycles for the weights of a
-                // tile, where the exponentials alone take 1024).
-                float x[32], y[32];
-                float top = -INFINITY;
-                tc_issue_load32(x, logits);
 #pragma unroll 1
-                for (int i = 0; i < 4; i += 2) {
-                    tc_loaded32(x);
-                    tc_issue_load32(y, logits + i * 32 + 32);
-                    if (special) adjust(x, i);
-                    top = max32(x, top);
-                    tc_loaded32(y);
-                    tc_issue_load32(x, logits + (i * 32 + 64) % 128);      // (the last one is the second pass's first)
-                    if (special) adjust(y, i + 1);
-                    top = max32(y, top);
-                }
-                top *= factor;
-                // The reference follows the maximum lazily: weights stay below 2^kGroupLag.
-                const bool moved = top > m + kGroupLag;
-                if (__any_sync(0xffffffffu, moved)) {
-                    const float alpha = moved ? fast_exp2(m - top) : 1.f;
-                    if (moved) m = top;
-                    l *= alpha;
-                    if (j > seg.t0) {
-                        // the accumulator holds the tiles before this one once their MMAs are complete
-                        if (fine) fine = tree_wait(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
-                        fine = __all_sync(0xffffffffu, fine);
-                        tc_fence_after();
+                for (int h = 0; h < kUnits; ++h) {
+                    const int buf = buffer_of(g, s, h);
+                    const unsigned logits = tmem + lanes + buf * kUnit;
+                    if (fine) fine = tree_wait(misc + kTreeBarSFull + buf * 8, use_of(g) & 1);
+                    fine = __all_sync(0xffffffffu, fine);
+                    tc_fence_after();
+                    float x[32], y[32];
+                    float top = -INFINITY;
+                    if constexpr (kUnit == 64) {
+                        tc_issue_load32(x, logits);
+                        tc_issue_load32(y, logits + 32);
+                        tc_loaded32(x);
+                        tc_loaded32(y);
+                        if (special) {
+                            adjust(x, 2 * h);
+                            adjust(y, 2 * h + 1);
+                        }
+                        top = max32(y, max32(x, top));
+                    } else {
+                        // The row is read twice, 32 columns at a time in short loops, the next columns on their way while
+                        // these are worked on: all 128 logits held at once leave no registers for anything else.
+                        tc_issue_load32(x, logits);
 #pragma unroll 1
-                        for (int c0 = 0; c0 < D; c0 += 32) {
-                            float o[32];
-                            unsigned back[32];
-                            tc_issue_load32(o, acc + c0);
-                            tc_loaded32(o);
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) back[c] = __float_as_uint(o[c] * alpha);
-                            tc_store32(acc + c0, back);
+                        for (int i = 0; i < 4; i += 2) {
+                            tc_loaded32(x);
+                            tc_issue_load32(y, logits + i * 32 + 32);
+                            if (special) adjust(x, i);
+                            top = max32(x, top);
+                            tc_loaded32(y);
+                            tc_issue_load32(x, logits + (i * 32 + 64) % 128);      // (the last one is the second pass's first)
+                            if (special) adjust(y, i + 1);
+                            top = max32(y, top);
                         }
                     }
-                }
-                // Weights (scaled by kGroupWeightScale inside the exponent), their sum, and their fp16 high and
-                // low parts over the logits: 16 + 16 columns per 32 tokens.
-                const float2 minus_ref = make_float2(kGroupWeightLog2 - m, kGroupWeightLog2 - m), factors = make_float2(factor, factor);
-                float2 sum = make_float2(0.f, 0.f), sum_odd = make_float2(0.f, 0.f);
-                auto weigh = [&](const float (&z)[32], int i) {
-                    unsigned parts[32];
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        // (not one fused operation: the scaled logit has to round as the maximum did)
-                        const float2 e = add2(mul2(make_float2(z[2 * c], z[2 * c + 1]), factors), minus_ref);
-                        const float2 w = make_float2(fast_exp2(e.x), fast_exp2(e.y));
-                        float2 &total = c & 1 ? sum_odd : sum;
-                        total = add2(total, w);
-                        parts[c] = pack_half2(w.x, w.y);
-                        const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&parts[c]));
-                        const float2 rest = fma2(back, make_float2(-1.f, -1.f), w);
-                        parts[16 + c] = pack_half2(rest.x, rest.y);
-                    }
-                    tc_store32(logits + i * 32, parts);
-                };
+                    top *= factor;
+                    // The reference follows the maximum lazily: weights stay below 2^kGroupLag.
+                    const bool moved = top > m + kGroupLag;
+                    if (__any_sync(0xffffffffu, moved)) {
+                        const float alpha = moved ? fast_exp2(m - top) : 1.f;
+                        if (moved) m = top;
+                        l *= alpha;
+                        if (j > seg.t0 || h > 0) {
+                            // the accumulator holds the units before this one once their MMAs are complete
+                            const int before = h > 0 ? g : g - 1;
+                            if (fine) fine = tree_wait(misc + kTreeBarPvDone + buffer_of(before, s, h > 0 ? h - 1 : kUnits - 1) * 8, use_of(before) & 1);
+                            fine = __all_sync(0xffffffffu, fine);
+                            tc_fence_after();
 #pragma unroll 1
-                for (int i = 0; i < 4; i += 2) {
-                    tc_loaded32(x);
-                    tc_issue_load32(y, logits + i * 32 + 32);
-                    if (special) adjust(x, i);
-                    weigh(x, i);
-                    tc_loaded32(y);
-                    if (i == 0) tc_issue_load32(x, logits + 64);
-                    if (special) adjust(y, i + 1);
-                    weigh(y, i + 1);
+                            for (int c0 = 0; c0 < D; c0 += 32) {
+                                float o[32];
+                                unsigned back[32];
+                                tc_issue_load32(o, acc + c0);
+                                tc_loaded32(o);
+#pragma unroll
+                                for (int c = 0; c < 32; ++c) back[c] = __float_as_uint(o[c] * alpha);
+                                tc_store32(acc + c0, back);
+                            }
+                        }
+                    }
+                    // Weights (scaled by kGroupWeightScale inside the exponent), their sum, and their fp16 high and
+                    // low parts over the logits: 16 + 16 columns per 32 tokens.
+                    const float2 minus_ref = make_float2(kGroupWeightLog2 - m, kGroupWeightLog2 - m), factors = make_float2(factor, factor);
+                    float2 sum = make_float2(0.f, 0.f), sum_odd = make_float2(0.f, 0.f);
+                    auto weigh = [&](const float (&z)[32], int i) {
+                        unsigned parts[32];
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) {
+                            // (not one fused operation: the scaled logit has to round as the maximum did)
+                            const float2 e = add2(mul2(make_float2(z[2 * c], z[2 * c + 1]), factors), minus_ref);
+                            const float2 w = make_float2(fast_exp2(e.x), fast_exp2(e.y));
+                            float2 &total = c & 1 ? sum_odd : sum;
+                            total = add2(total, w);
+                            parts[c] = pack_half2(w.x, w.y);
+                            const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&parts[c]));
+                            const float2 rest = fma2(back, make_float2(-1.f, -1.f), w);
+                            parts[16 + c] = pack_half2(rest.x, rest.y);
+                        }
+                        tc_store32(logits + i * 32, parts);
+                    };
+                    if constexpr (kUnit == 64) {
+                        weigh(x, 0);
+                        weigh(y, 1);
+                    } else {
+#pragma unroll 1
+                        for (int i = 0; i < 4; i += 2) {
+                            tc_loaded32(x);
+                            tc_issue_load32(y, logits + i * 32 + 32);
+                            if (special) adjust(x, i);
+                            weigh(x, i);
+                            tc_loaded32(y);
+                            if (i == 0) tc_issue_load32(x, logits + 64);
+                            if (special) adjust(y, i + 1);
+                            weigh(y, i + 1);
+                        }
+                    }
+                    l += (sum.x + sum.y) + (sum_odd.x + sum_odd.y);
+                    tc_stored();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbarrier_arrive(misc + kTreeBarPFull + buf * 8);
                 }
-                l += (sum.x + sum.y) + (sum_odd.x + sum_odd.y);
-                tc_stored();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbarrier_arrive(misc + kTreeBarPFull + buf * 8);
             }
             // ---- the segment's end: the accumulator divided by the sum, to the output or the workspace ----
-            if (fine) fine = tree_wait(misc + kTreeBarPvDone + buffer_of(g - 1, s) * 8, use_of(g - 1) & 1);
+            if (fine) fine = tree_wait(misc + kTreeBarPvDone + buffer_of(g - 1, s, kUnits - 1) * 8, use_of(g - 1) & 1);
             fine = __all_sync(0xffffffffu, fine);
             tc_fence_after();
             const bool empty = !live || l == 0.f;                     // (a NaN sum is not an empty row's)
@@ -344,16 +385,17 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
 #pragma unroll
                         for (int c = 0; c < 32; ++c) o[c] += more[c];
                     }
+                    // (a thread's stores are a row apart: 32 bytes each where the buffer allows it)
                     if (whole) {
-                        uint4 *to = reinterpret_cast<uint4 *>(a.out + out_row * D + c0);
+                        unsigned h[16];
 #pragma unroll
-                        for (int c = 0; c < 32; c += 8)
-                            to[c / 8] = make_uint4(pack_half2(o[c], o[c + 1]), pack_half2(o[c + 2], o[c + 3]),
-                                                   pack_half2(o[c + 4], o[c + 5]), pack_half2(o[c + 6], o[c + 7]));
+                        for (int c = 0; c < 16; ++c) h[c] = pack_half2(o[2 * c], o[2 * c + 1]);
+                        store_row<16>(a.out + out_row * D + c0, h);
                     } else {
-                        float4 *to = reinterpret_cast<float4 *>(a.part_o + slot_row * D + c0);
+                        unsigned w[32];
 #pragma unroll
-                        for (int c = 0; c < 32; c += 4) to[c / 4] = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+                        for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(o[c]);
+                        store_row<32>(a.part_o + slot_row * D + c0, w);
                     }
                 }
                 __syncwarp();
