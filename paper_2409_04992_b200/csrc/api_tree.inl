@@ -18,6 +18,15 @@ int tree_attention_shape(int32_t batch, int32_t tree_tokens, int32_t q_heads, in
     return INSTINFER_OK;
 }
 
+// Plan of the warp-level form: the grouped kernel's rules without the search for the best number of chunks (some
+// 300 divisions on the host, which every call would pay for the workspace's size).
+PlanRules tree_rules(int32_t head_dim)
+{
+    PlanRules rules = grouped_rules(head_dim);
+    rules.block_overhead_tokens = 0;
+    return rules;
+}
+
 // ---- the tcgen05 form ----
 
 // Rows of the partial results: two slots per piece, at most 1 + short_pieces pieces per block and one more.  Behind
@@ -81,7 +90,7 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
     p.tree.words = (tree_tokens + 63) / 64;
     if (!usable(workspace) || workspace_bytes < instinfer_tree_workspace_bytes(batch, tree_tokens, q_heads, kv_heads, head_dim, max_seq_len))
         return INSTINFER_ERR_WORKSPACE;
-    const SplitPlan plan = make_plan(pairs * p.row_groups, max_seq_len, grouped_rules(head_dim));
+    const SplitPlan plan = make_plan(pairs * p.row_groups, max_seq_len, tree_rules(head_dim));
     const int64_t grid = pairs * plan.n_splits * p.row_groups;
     if (grid >= (int64_t)1 << 31 || pairs * p.rows >= (int64_t)1 << 31) return INSTINFER_ERR_INVALID_ARG;
     p.a.q = static_cast<const __half *>(q);
@@ -162,7 +171,7 @@ size_t instinfer_tree_workspace_bytes(int32_t batch, int32_t tree_tokens, int32_
     if (pairs == 0) return 256;
     const int32_t rows = q_heads / kv_heads * tree_tokens, groups = (rows + kGroupRows - 1) / kGroupRows;
     // enough for either implementation: which one runs also depends on the cache layout
-    const size_t warp_level = grouped_workspace_for(pairs, rows, head_dim, make_plan(pairs * groups, max_seq_len, grouped_rules(head_dim)));
+    const size_t warp_level = grouped_workspace_for(pairs, rows, head_dim, make_plan(pairs * groups, max_seq_len, tree_rules(head_dim)));
     const size_t umma = tree_umma_workspace(pairs, tree_tokens, q_heads / kv_heads, head_dim);
     return warp_level > umma ? warp_level : umma;
 }

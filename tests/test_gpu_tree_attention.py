@@ -322,3 +322,61 @@ def test_offsets_beyond_32_bits():
     torch.cuda.synchronize()
     compare(out.cpu().numpy(), lse.cpu().numpy(),
             od.tree_attention(small.q, small.k, small.v, small.table, small.lens, small.trees, small.see, small.scale), "far blocks")
+
+
+@pytest.mark.parametrize("layout,tokens,dim,q_heads,kv_heads,nodes,lens", [
+    ("paged", 32, 128, 40, 40, 64, [9000, 5003, 7777, 130, 64]),      # many items, each shorter than a long piece
+    ("paged", 64, 128, 32, 4, 32, [60000, 33001, 40]),                # few items, longer than the pieces; two row blocks
+    ("contiguous", 0, 64, 24, 24, 20, [30011, 17000]),
+    ("paged", 128, 256, 12, 6, 40, [40000, 200, 33333]),
+    ("paged", 16, 128, 16, 16, 7, [70001, 12345]),
+    ("paged", 32, 64, 20, 2, 13, [60011, 50000, 1000])])
+def test_large_batches_whose_pieces_are_drawn(path, layout, tokens, dim, q_heads, kv_heads, nodes, lens):
+    """Enough tiles for pieces drawn from the ticket counter: every row against 64-bit attention on the
+    GPU, one (sequence, KV head) at a time; twice, with the same bits."""
+    if path == 1:
+        pytest.skip("the cut into pieces belongs to the tcgen05 form")
+    B, group = len(lens), q_heads // kv_heads
+    g = torch.Generator(device="cuda").manual_seed(sum(lens))
+    draw = lambda *s: torch.randn(*s, generator=g, device="cuda").half()  # noqa: E731
+    rng = np.random.default_rng(3)
+    trees = [nodes, max(1, nodes - 3), nodes, nodes, nodes][:B]
+    see = np.stack([od.ancestor_mask(random_tree(rng, t, nodes), t, nodes) for t in trees])
+    if layout == "paged":
+        per = max(od.blocks_for(n, tokens) for n in lens)
+        ids = rng.permutation(B * per)[:B * per].reshape(B, per).astype(np.int32)
+        table = torch.from_numpy(ids).cuda()
+        k, v = draw(B * per, kv_heads, tokens, dim), draw(B * per, kv_heads, tokens, dim)
+    else:
+        table, k, v = None, draw(B, kv_heads, max(lens), dim), draw(B, kv_heads, max(lens), dim)
+    q = draw(B, nodes, q_heads, dim)
+    put = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    scale, flags = dim ** -0.5, torch.zeros(1, dtype=torch.int32, device="cuda")
+    need = binding.tree_workspace_bytes(B, nodes, q_heads, kv_heads, dim, max(lens))
+    outs = []
+    for _ in range(2):
+        out, lse, ws = gu.Guarded(tuple(q.shape), torch.float16), gu.Guarded(tuple(q.shape[:3]), torch.float32), gu.Guarded((need,), torch.uint8)
+        binding.decode_attention_tree(out.view, lse.view, q, k, v, table, put(lens), put(trees),
+                                      torch.from_numpy(od.pack_mask(see)).cuda(), max(lens), scale, ws.view, flags)
+        torch.cuda.synchronize()
+        assert out.intact() and lse.intact() and ws.intact() and int(flags.item()) == 0
+        outs.append((out.view.clone(), lse.view.clone()))
+    assert torch.equal(outs[0][0].view(torch.int16), outs[1][0].view(torch.int16)) and torch.equal(outs[0][1], outs[1][1])
+    got, got_lse = outs[0]
+    for b, (n, t) in enumerate(zip(lens, trees)):
+        hide = torch.zeros(t, n, dtype=torch.float64, device="cuda")
+        hide[:, n - t:] = torch.where(torch.from_numpy(see[b, :t, :t]).cuda(), 0.0, -float("inf"))
+        for h in range(kv_heads):
+            if table is None:
+                ks, vs = k[b, h, :n].double(), v[b, h, :n].double()
+            else:
+                pages = table[b, :od.blocks_for(n, tokens)].long()
+                ks, vs = k[pages, h].flatten(0, 1)[:n].double(), v[pages, h].flatten(0, 1)[:n].double()
+            rows = q[b, :t, h * group:(h + 1) * group].double()
+            s = torch.einsum("tgd,nd->tgn", rows, ks) * scale
+            spread = (torch.einsum("tgd,nd->tgn", rows.abs(), ks.abs()) * scale).amax(-1)
+            s += hide[:, None]
+            w = torch.softmax(s, -1)
+            compare(got[b, :t, h * group:(h + 1) * group].cpu().numpy(), got_lse[b, :t, h * group:(h + 1) * group].cpu().numpy(),
+                    [x.cpu().numpy() for x in (w @ vs, torch.logsumexp(s, -1), w @ vs.abs(), spread)], f"sequence {b} head {h}", n)
+        assert (got[b, t:] == 0).all() and torch.isneginf(got_lse[b, t:]).all()
