@@ -126,7 +126,7 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
         const int row_parts = (rows.item_rows + kTreeMergeRows - 1) / kTreeMergeRows;
         const int32_t box = paged && block_tokens < kTreeTile ? block_tokens : kTreeTile;
         TreeLaunch t = {};
-        if (items * row_parts < (int64_t)1 << 31 && items * (ceil_div(max_seq_len, kTreeTile) + kTreeItemCost) < (int64_t)1 << 31 &&
+        if (items * row_parts < (int64_t)1 << 31 && (int64_t)tree_tokens * q_heads * head_dim < (int64_t)1 << 31 && items * (ceil_div(max_seq_len, kTreeTile) + kTreeItemCost) < (int64_t)1 << 31 &&
             make_query_map(&t.map_q, q, batch, tree_tokens, q_heads, p.group, head_dim, rows.nodes_per_block) &&
             make_cache_map(&t.map_k, k_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box) &&
             make_cache_map(&t.map_v, v_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box)) {
