@@ -642,7 +642,9 @@ int instinfer_set_sparse_path(int32_t path);
  * instinfer_set_grouped_path forces the choice for later calls of this process: 0 automatic,
  * 1 warp-level, 2 tcgen05 where the shape allows (a tuning and test aid; returns INSTINFER_OK
  * or INSTINFER_ERR_INVALID_ARG; not thread-safe against concurrent calls).  Both meet the
- * entry point's tolerances; their results are not bit-identical to each other.
+ * entry point's tolerances; their results are not bit-identical to each other.  The setting also
+ * holds for instinfer_decode_attention_tree, whose tcgen05 form takes these block sizes and every
+ * head size (head size 64 from 17 rows per KV head on).
  */
 int instinfer_set_grouped_path(int32_t path);
 

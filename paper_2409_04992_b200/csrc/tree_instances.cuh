@@ -45,7 +45,9 @@ int launch_tree_tokens(const TreeLaunch &t)
 template <int D, bool kPaged>
 int launch_tree(const TreeRows &rows, const TreeLaunch &t)
 {
-    if (rows.columns == 16) return launch_tree_tokens<D, kPaged, 16>(t);
+    if constexpr (D != 64) {                       // (head size 64: the warp-level form)
+        if (rows.columns == 16) return launch_tree_tokens<D, kPaged, 16>(t);
+    }
     if (rows.columns == 32) return launch_tree_tokens<D, kPaged, 32>(t);
     if (rows.columns == 64) return launch_tree_tokens<D, kPaged, 64>(t);
     if constexpr (D != 256) {
