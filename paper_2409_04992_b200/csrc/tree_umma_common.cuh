@@ -340,16 +340,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     return r;
 }
 
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    uint64_t x, y, d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
-    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(x), "l"(y));
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
-    return r;
-}
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float d;

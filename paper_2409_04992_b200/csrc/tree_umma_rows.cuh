@@ -208,6 +208,7 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
         const unsigned acc = tmem + lanes + Geo::kOColumn + s * D;
         const int node_in_block = t / p.group, head = t - node_in_block * p.group;
         const bool used_row = node_in_block < p.nodes_per_block;
+        const float factor = fabsf(a.scale_log2e), sign = copysignf(1.f, a.scale_log2e);
         bool fine = true;
         int g = 0;
         for (int k = 0;; ++k) {
@@ -226,16 +227,17 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
             if (threadIdx.x < 4) reinterpret_cast<volatile unsigned *>(misc_ptr + kTreePoison)[((k + 4) & 7) * 4 + threadIdx.x] = 0u;
             TreeRow row = {0, 0, live};
             if (live && seg.t1 * kTreeTile > prefix) row = tree_row(p.tree, seg.b, node, seg.nodes);
-            float m = kMinusHuge, l = 0.f;                            // l and the accumulator carry kGroupWeightScale
+            // The reference is a logit before it is scaled, taken off before the scale comes in: the largest logit's
+            // weight is exactly kGroupWeightScale then, however large it is.  l and the accumulator carry that scale.
+            float m = kMinusHuge, l = 0.f;
             for (int j = seg.t0; j < seg.t1; ++j, ++g) {
                 const int start = j * kTreeTile;
                 const bool masked = start + kTreeTile > prefix;       // uniform
                 // (stream 0 cleans for both: the output MMAs of a tile start with it)
                 if (masked && s == 0) copies.template clean_values<32>(seg, j, g, (warp & 3) * 32, poison, fine);
-                // What the row sees of the tile, where that is not all of it; a negative scale takes the same way,
-                // as it would turn the maximum around.
+                // What the row sees of the tile, where that is not all of it; a negative scale takes the same way:
+                // its sign goes to the logits, so that the maximum is the maximum.
                 const bool special = masked || a.scale_log2e < 0.f;   // uniform
-                const float factor = special ? 1.f : a.scale_log2e;
                 Bits128 sees = {~(uint64_t)0, ~(uint64_t)0};
                 if (masked) {
                     sees = {row.lo, row.hi};
@@ -253,7 +255,7 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                 auto adjust = [&](float (&x)[32], int i) {
                     const unsigned word = sees.word(i);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) x[c] = word >> c & 1u ? x[c] * a.scale_log2e : -INFINITY;
+                    for (int c = 0; c < 32; ++c) x[c] = word >> c & 1u ? x[c] * sign : -INFINITY;
                 };
 #pragma unroll 1
                 for (int h = 0; h < kUnits; ++h) {
@@ -290,11 +292,11 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                             top = max32(y, top);
                         }
                     }
-                    top *= factor;
                     // The reference follows the maximum lazily: weights stay below 2^kGroupLag.
-                    const bool moved = top > m + kGroupLag;
+                    const float rise = (top - m) * factor;
+                    const bool moved = rise > kGroupLag;
                     if (__any_sync(0xffffffffu, moved)) {
-                        const float alpha = moved ? fast_exp2(m - top) : 1.f;
+                        const float alpha = moved ? fast_exp2(-rise) : 1.f;
                         if (moved) m = top;
                         l *= alpha;
                         if (j > seg.t0 || h > 0) {
@@ -317,14 +319,14 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                     }
                     // Weights (scaled by kGroupWeightScale inside the exponent), their sum, and their fp16 high and
                     // low parts over the logits: 16 + 16 columns per 32 tokens.
-                    const float2 minus_ref = make_float2(kGroupWeightLog2 - m, kGroupWeightLog2 - m), factors = make_float2(factor, factor);
+                    const float2 minus_ref = make_float2(-m, -m), factors = make_float2(factor, factor);
+                    const float2 extra = make_float2(kGroupWeightLog2, kGroupWeightLog2);
                     float2 sum = make_float2(0.f, 0.f), sum_odd = make_float2(0.f, 0.f);
                     auto weigh = [&](const float (&z)[32], int i) {
                         unsigned parts[32];
 #pragma unroll
                         for (int c = 0; c < 16; ++c) {
-                            // (not one fused operation: the scaled logit has to round as the maximum did)
-                            const float2 e = add2(mul2(make_float2(z[2 * c], z[2 * c + 1]), factors), minus_ref);
+                            const float2 e = fma2(add2(make_float2(z[2 * c], z[2 * c + 1]), minus_ref), factors, extra);
                             const float2 w = make_float2(fast_exp2(e.x), fast_exp2(e.y));
                             float2 &total = c & 1 ? sum_odd : sum;
                             total = add2(total, w);
@@ -364,7 +366,7 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
             tc_fence_after();
             const bool empty = !live || l == 0.f;                     // (a NaN sum is not an empty row's)
             const float inverse = empty ? 0.f : 1.f / l;
-            const float lse2 = empty ? kMinusHuge : m + log2f(l) - kGroupWeightLog2;
+            const float lse2 = empty ? kMinusHuge : log2f(l) + fmaf(m, factor, -kGroupWeightLog2);
             const int64_t out_row = ((int64_t)seg.b * p.tree.tokens + node) * ((int64_t)a.heads * p.group) + (int64_t)seg.hk * p.group + head;
             const int64_t slot_row = (int64_t)seg.slot * p.item_rows + s * p.nodes_per_block * p.group + t;
             const bool whole = seg.whole();

@@ -208,12 +208,12 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
         const int t = threadIdx.x & 127;                              // token of the tile = lane of tensor memory
         const unsigned lanes = tmem + ((unsigned)((warp & 3) * 32) << 16);
         float *by_warp = reinterpret_cast<float *>(misc_ptr + kTreeMiscBytes);   // [N][4]: a row's maxima, or sums, by warp
-        float *offsets = by_warp + N * 4;                             // [N]: the rows' offsets as they were last moved
+        float *offsets = by_warp + N * 4;                             // [N]: the rows' references (negated) as they were last moved
         const int rows_here = p.nodes_per_block * p.group;            // <= N: all the tree's rows
         const int group_inverse = 65536 / p.group + 1;
         auto node_of = [&](int r) -> int { return r * group_inverse >> 16; };      // r / p.group (exact for r < 64)
         const int q_heads = a.heads * p.group;
-        const float scale = a.scale_log2e;
+        const float scale = a.scale_log2e, sign = copysignf(1.f, scale);
         constexpr float kTooLarge = kGroupLag + kGroupWeightLog2;
         bool fine = true;
         float x[kCols];
@@ -248,12 +248,13 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                 asm volatile("ld.global.b64 %0, [%1];" : "=l"(my_lo) : "l"(words) : "memory");
                 if (p.tree.words > 1) asm volatile("ld.global.b64 %0, [%1];" : "=l"(my_hi) : "l"(words + 1) : "memory");
             }
-            // Two rows at a time: the weight exponent's offset kGroupWeightLog2 - reference, and this thread's
-            // sums; sums and accumulator carry kGroupWeightScale.
+            // Two rows at a time: the negated reference, and this thread's sums; sums and accumulator carry
+            // kGroupWeightScale.  The reference is a logit before it is scaled, taken off before the scale comes in:
+            // the largest logit's weight is exactly kGroupWeightScale then, however large it is.
             float2 offset[kCols / 2], l[kCols / 2];
 #pragma unroll
             for (int r = 0; r < kCols / 2; ++r) {
-                offset[r] = make_float2(-kMinusHuge, -kMinusHuge);
+                offset[r] = make_float2(-kMinusHuge * sign, -kMinusHuge * sign);
                 l[r] = make_float2(0.f, 0.f);
             }
             for (int j = t0; j < t1; ++j, ++g) {
@@ -279,14 +280,14 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                 // Exponents of the weights against the references; where one is too large the references move
                 // and they are computed again.
                 float e[kCols];
-                for (;;) {
+                for (int attempt = 0;; ++attempt) {
 #pragma unroll
                     for (int r = 0; r < kCols; r += 16) tc_loaded16(x + r);
                     float most = -INFINITY, most_odd = -INFINITY;
 #pragma unroll
                     for (int r = 0; r < kCols / 2; ++r) {
-                        // (not one fused operation: the scaled logit has to round as the maxima below do)
-                        const float2 y = add2(mul2(make_float2(x[2 * r], x[2 * r + 1]), make_float2(scale, scale)), offset[r]);
+                        const float2 y = fma2(add2(make_float2(x[2 * r], x[2 * r + 1]), offset[r]), make_float2(scale, scale),
+                                              make_float2(kGroupWeightLog2, kGroupWeightLog2));
                         e[2 * r] = y.x;
                         e[2 * r + 1] = y.y;
                     }
@@ -300,7 +301,7 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                         most = max3(most, e[r], e[r + 1]);
                         most_odd = max3(most_odd, e[r + 2], e[r + 3]);
                     }
-                    if (!group_any(vote_id, fmaxf(most, most_odd) > kTooLarge)) break;
+                    if (attempt > 0 || !group_any(vote_id, fmaxf(most, most_odd) > kTooLarge)) break;
                     // ---- some row's reference moves (rare after a segment's first tile) ----
                     if (j > t0) {                                 // the accumulator holds the tiles before this one
                         if (fine) fine = tree_wait(misc + kTreeBarPvDone, (g - 1) & 1);
@@ -313,7 +314,7 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                         tc_issue_load16(z, logits + r0);
                         tc_loaded16(z);
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) z[r] = seen_by >> (r0 + r) & 1u ? z[r] * scale : -INFINITY;
+                        for (int r = 0; r < 16; ++r) z[r] = seen_by >> (r0 + r) & 1u ? z[r] * sign : -INFINITY;
                         const float top = warp_reduce16<true>(z, lane);
                         if ((lane & 1) == 0) by_warp[(row0 + r0 + warp_reduce16_row(lane)) * 4 + (warp & 3)] = top;
                     }
@@ -328,9 +329,10 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                             float &off = (r & 1) ? offset[(r0 + r) / 2].y : offset[(r0 + r) / 2].x;
                             float &sum = (r & 1) ? l[(r0 + r) / 2].y : l[(r0 + r) / 2].x;
                             alpha[r] = 1.f;
-                            if (top + off > kTooLarge) {
-                                alpha[r] = fast_exp2(kGroupWeightLog2 - off - top);       // 2^(old - new reference)
-                                off = kGroupWeightLog2 - top;
+                            const float moved = -top * sign, rise = (off - moved) * scale;
+                            if (rise > kGroupLag) {
+                                alpha[r] = fast_exp2(-rise);                              // 2^(old - new reference)
+                                off = moved;
                                 if (t == r0 + r) offsets[row0 + r0 + r] = off;
                             }
                             sum *= alpha[r];
@@ -397,7 +399,7 @@ tree_attn_tokens_kernel(const __grid_constant__ TreeParams p, const __grid_const
                 const float4 sums = *reinterpret_cast<const float4 *>(by_warp + r * 4);
                 const float total = (sums.x + sums.y) + (sums.z + sums.w);
                 const bool empty = r >= live_rows || total == 0.f;    // (a NaN sum is not an empty row's)
-                const float lse2 = empty ? kMinusHuge : log2f(total) - offsets[r];
+                const float lse2 = empty ? kMinusHuge : log2f(total) - fmaf(offsets[r], scale, kGroupWeightLog2);
                 if (r < rows_here && fine) {
                     const int node = node_of(r);
                     if (!whole) seg.lse[r] = lse2;

@@ -220,6 +220,50 @@ def test_peaked_and_moving_logits(dim):
         check(c, f"scale {scale}")
 
 
+@pytest.mark.parametrize("dim,nodes,group", [(128, 8, 1), (128, 40, 1), (128, 60, 2), (128, 60, 4), (64, 30, 1), (64, 90, 2), (256, 20, 1), (256, 90, 1)])
+def test_huge_logits(path, dim, nodes, group):
+    """Logits of 2^20 to 2^35, past where a reference and the weights' scale can be added exactly: the kernels
+    end, and as the largest logit of a row is apart from the others by far more than their rounding, its
+    value row is the result."""
+    if path == 1:
+        pytest.skip("the warp-level form's weights overflow there, as the grouped entry point's do")
+    c = Case("contiguous", 0, group, 1, dim, nodes, [300, 140], seed=15)
+    for b, n in enumerate(c.lens):
+        sizes = 2.0 ** np.random.default_rng(b).uniform(-1, 13, n)
+        c.k[b, 0, :n] = np.sign(c.k[b, 0, :n].astype(np.float32)) * 4 * sizes[:, None]
+    c.q = (np.sign(c.q.astype(np.float32)) * 2.0 ** np.random.default_rng(5).uniform(4, 14, c.q.shape[:3])[..., None]).astype(np.float16)
+    want = od.tree_attention(c.q, c.k, c.v, c.table, c.lens, c.trees, c.see, c.scale)
+    got, lse, flags = run(c)
+    assert flags == 0 and np.isfinite(got).all() and np.isfinite(lse).all()
+    assert want[3].max() > 2.0 ** 30
+    assert (np.abs(lse - want[1]) <= dim * 2.0 ** -22 * want[3] + 16).all()
+    # rows whose second largest logit is far below the largest one, in units of the logits' rounding
+    clear = 0
+    for b, n in enumerate(c.lens):
+        for t in range(c.trees[b]):
+            seen = [*range(n - c.trees[b]), *(n - c.trees[b] + j for j in range(c.trees[b]) if c.see[b, t, j])]
+            for h in range(group):
+                s = np.sort(c.k[b, 0, seen].astype(np.float64) @ c.q[b, t, h].astype(np.float64) * c.scale)
+                if s[-1] - s[-2] > 2 * dim * 2.0 ** -22 * want[3][b, t, h] + 40:
+                    clear += 1
+                    assert np.abs(got[b, t, h] - want[0][b, t, h]).max() <= 2.0 ** -10 * np.abs(want[0][b, t, h]).max()
+    assert clear > 0
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-30, -1e-30, -0.09, 2.0, -2.0])
+@pytest.mark.parametrize("dim,nodes,group", [(128, 6, 1), (128, 40, 2), (128, 50, 3), (64, 70, 1), (256, 40, 1), (256, 80, 1)])
+def test_other_scales(scale, dim, nodes, group):
+    c = Case("contiguous", 0, group, 1, dim, nodes, [300, 131, 20], seed=18)
+    c.scale = scale
+    check(c, f"scale {scale}")
+
+
+def test_a_cache_smaller_than_one_tile():
+    for dim, nodes, group in ((128, 2, 1), (128, 2, 40), (64, 2, 20), (256, 1, 70), (128, 1, 128)):
+        check(Case("contiguous", 0, group, 1, dim, nodes, [3], seed=16), f"three tokens, {group} heads")
+        check(Case("paged", 16, 2 * group, 2, dim, nodes, [2, 3], seed=17), f"three tokens, {group} heads, paged")
+
+
 def test_a_chain_agrees_with_the_grouped_entry_point():
     c = Case("paged", 32, 8, 2, 128, 4, [300, 64, 1000], seed=9)
     c.see[:] = np.tril(np.ones((4, 4), dtype=bool))
