@@ -153,6 +153,14 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
 
 
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """Refuses tensors of another device than the current one (whose stream the call goes to)."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise InstInferError(ERR_INVALID_ARG)
+
+
 def _check(status: int) -> None:
     if status != OK:
         raise InstInferError(status)
@@ -339,6 +347,7 @@ def tree_mask(mask: torch.Tensor, parents: torch.Tensor, tree_lens: Optional[tor
     """instinfer_tree_mask: mask int64 [B, T, ceil(T / 64)] (the bits of the header's uint64 words),
     parents int32 [B, T], tree_lens int32 [B] (None: T nodes each)."""
     batch, tree_tokens = parents.shape
+    _here(mask, parents)
     _check(load().instinfer_tree_mask(_ptr(mask), _ptr(parents), _ptr(tree_lens), batch, tree_tokens,
                                       _ptr(status_flags), _stream(stream)))
 
@@ -359,6 +368,7 @@ def decode_attention_tree(out: torch.Tensor, lse: Optional[torch.Tensor], q: tor
     with Hkv heads ([B,Hkv,s_max,D], or pools [P,Hkv,T,D] with block_table)."""
     batch, tree_tokens, q_heads, head_dim = q.shape
     kv_heads = k_cache.shape[1]
+    _here(out, q, k_cache, workspace)
     if block_table is None:
         s_max, block_tokens, max_blocks, phys = k_cache.shape[2], 0, 0, 0
     else:
@@ -390,6 +400,7 @@ def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.T
                 (vocab > 1 and probs.stride(2) != 1) or (tree_tokens > 1 and probs.stride(1) != stride) or
                 (batch > 1 and probs.stride(0) != tree_tokens * stride)):
             raise InstInferError(ERR_INVALID_ARG)
+    _here(path, target_probs, tokens)
     if target_probs.dtype not in _PROBS_TYPES:
         raise InstInferError(ERR_UNSUPPORTED)
     _check(load().instinfer_verify_tree(
@@ -419,6 +430,7 @@ def kv_keep_path(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tens
     """instinfer_kv_keep_path: one cache per layer ([B,H,s_max,D], or pools [P,H,T,D] with
     block_table); path [B, tree_tokens]."""
     batch, tree_tokens = path.shape
+    _here(path, k_caches[0] if len(k_caches) else None)
     k, v, n_layers, keep = _layers(k_caches, v_caches)
     _, heads, rows, head_dim = k_caches[0].shape
     if block_table is None:
@@ -436,6 +448,7 @@ def kv_fork(block_table: torch.Tensor, block_refs: torch.Tensor, seq_lens: torch
             stream: Optional[torch.cuda.Stream] = None) -> None:
     """instinfer_kv_fork: block_table [B, M], block_refs [P], seq_lens [B], src and dst [n]."""
     batch, max_blocks = block_table.shape
+    _here(block_table, src)
     _check(load().instinfer_kv_fork(_ptr(block_table), _ptr(block_refs), _ptr(seq_lens), _ptr(src), _ptr(dst),
                                     src.numel(), max_blocks, int(block_tokens), block_refs.numel(), batch,
                                     _ptr(status_flags), _stream(stream)))
@@ -451,6 +464,7 @@ def kv_resize(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tensor], 
               stream: Optional[torch.cuda.Stream] = None) -> None:
     """instinfer_kv_resize: one pool [P,H,T,D] per layer; new_lens may be seq_lens."""
     batch, max_blocks = block_table.shape
+    _here(block_table, workspace, k_pools[0] if len(k_pools) else None)
     k, v, n_layers, keep = _layers(k_pools, v_pools)
     phys, heads, block_tokens, head_dim = k_pools[0].shape
     _check(load().instinfer_kv_resize(
@@ -471,6 +485,7 @@ def kv_defragment(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tenso
     """instinfer_kv_defragment: one pool [P,H,T,D] per layer; the new table and counts may be the
     old ones; blocks_used int32 [1]."""
     batch, max_blocks = block_table.shape
+    _here(block_table, workspace, k_pools[0] if len(k_pools) else None)
     k, v, n_layers, keep = _layers(k_pools, v_pools)
     phys, heads, block_tokens, head_dim = k_pools[0].shape
     _check(load().instinfer_kv_defragment(

@@ -58,7 +58,7 @@ def check(target, draft, tokens, parents, tree_lens, uniforms):
 @pytest.mark.parametrize("dtype", DTYPES, ids=str)
 @pytest.mark.parametrize("batch,nodes,vocab,shape", [
     (3, 1, 1, "mixed"), (5, 2, 2, "chain"), (4, 7, 31, "mixed"), (3, 33, 257, "pairs"), (2, 64, 1000, "mixed"),
-    (2, 65, 4099, "star"), (2, 128, 515, "mixed"), (1, 8, 32000, "mixed"), (2, 5, 50257, "star"), (1, 4, 131073, "pairs")])
+    (2, 65, 4099, "star"), (2, 128, 515, "mixed"), (1, 8, 32000, "mixed"), (2, 5, 50257, "star"), (2, 3, 100003, "star"), (1, 4, 131073, "pairs")])
 def test_trees(dtype, batch, nodes, vocab, shape):
     for seed in range(3):
         target, draft, tokens, parents, uniforms = make(seed, batch, nodes, vocab, dtype, shape)
@@ -180,6 +180,8 @@ def test_other_streams_graphs_and_refusals():
         torch.cuda.synchronize()
         want = od.verify(target.double().numpy(), draft.double().numpy(), tokens, parents, [10] * 3, fresh)
         assert all(np.array_equal(g.cpu().numpy(), w) for g, w in zip(out, want))
+    with pytest.raises(binding.InstInferError):
+        binding.verify_tree(*out, dev[0].cpu(), dev[1].cpu(), dev[2], dev[3], None, u)       # not on this device
     for bad in (dict(a=dev[0].double()), dict(b=dev[1].float()), dict(b=dev[1][:, :, :3000]), dict(a=dev[0].transpose(0, 1))):
         with pytest.raises(binding.InstInferError):
             binding.verify_tree(*out, bad.get("a", dev[0]), bad.get("b", dev[1]), dev[2], dev[3], None, u)
