@@ -220,6 +220,21 @@ def test_a_captured_step_replays():
     assert grown.cpu().tolist() == [40, 60, 60, 0]
 
 
+def test_new_lengths_may_be_the_wanted_ones_and_flags_may_be_left_out():
+    pool = Pool(1, 12, 2, 8, 64, 4, 4)
+    pool.resize([20, 9, 0, 0])
+    pool.fork([0], [2])
+    pool.lens, flags = od.resize(pool.caches, pool.table, pool.refs, pool.lens, [24, 33, 21, 5], 8)
+    assert flags == od.FLAG_SEQ_LEN_RANGE            # 33 is too long
+    want = ints([24, 33, 21, 5])
+    binding.kv_resize(pool.k, pool.v, pool.gpu_table, pool.gpu_refs, pool.gpu_lens, want, want, pool.ws.view)
+    pool.gpu_lens = want
+    pool.check(0, "no flags asked for")
+    od.fork(pool.table, pool.refs, pool.lens, [1, 1], [3, 3], 8)
+    binding.kv_fork(pool.gpu_table, pool.gpu_refs, pool.gpu_lens, ints([1, 1]), ints([3, 3]), 8)
+    pool.check(0, "no flags asked for")
+
+
 # ---------------------------------------------------------------- keeping a path
 def keep_case(layout, tokens, layers, batch, heads, dim, nodes, lens, seed):
     rng = np.random.default_rng(seed)

@@ -424,3 +424,37 @@ def test_large_batches_whose_pieces_are_drawn(path, layout, tokens, dim, q_heads
             compare(got[b, :t, h * group:(h + 1) * group].cpu().numpy(), got_lse[b, :t, h * group:(h + 1) * group].cpu().numpy(),
                     [x.cpu().numpy() for x in (w @ vs, torch.logsumexp(s, -1), w @ vs.abs(), spread)], f"sequence {b} head {h}", n)
         assert (got[b, t:] == 0).all() and torch.isneginf(got_lse[b, t:]).all()
+
+
+@pytest.mark.parametrize("layout,tokens,dim,q_heads,kv_heads,nodes", [
+    ("contiguous", 0, 128, 128, 1, 32),       # 4096 rows: 32 blocks of rows of one node each
+    ("paged", 16, 128, 100, 1, 8),            # a node's heads leave 28 rows of a block empty
+    ("paged", 32, 256, 65, 1, 5), ("contiguous", 0, 256, 64, 1, 64), ("paged", 128, 64, 96, 1, 7),
+    ("contiguous", 0, 128, 400, 2, 3),        # more heads than a block of rows: the warp-level form
+    ("paged", 16, 64, 33, 1, 124)])
+def test_many_rows(layout, tokens, dim, q_heads, kv_heads, nodes):
+    lens = [300, 5, 129, 0]
+    check(Case(layout, tokens, q_heads, kv_heads, dim, nodes, lens, [min(nodes, n) for n in lens], seed=nodes), f"{q_heads} heads, {nodes} nodes")
+
+
+@pytest.mark.parametrize("layout,tokens", [("contiguous", 0), ("paged", 16)])
+@pytest.mark.parametrize("dim,nodes,group", [(128, 3, 1), (128, 20, 2), (128, 30, 3), (64, 5, 4), (256, 5, 2)])
+def test_large_batches_of_short_and_empty_sequences(layout, tokens, dim, nodes, group):
+    lens = np.random.default_rng(nodes).choice([0, 0, 1, 2, 5, 40, 140, 270], 700)
+    trees = [min(nodes, int(n)) for n in lens]
+    trees[5:50:3] = [0] * 15
+    check(Case(layout, tokens, group, 1, dim, nodes, lens.tolist(), trees, seed=19), f"700 sequences D={dim}")
+    check(Case(layout, tokens, group, 1, dim, nodes, [0] * 699 + [300], seed=20), f"one of 700 D={dim}")
+
+
+@pytest.mark.parametrize("dim,nodes,group", [(128, 3, 1), (128, 20, 2), (128, 30, 3), (64, 30, 1), (256, 5, 2)])
+def test_without_log_sum_exps_and_flags(dim, nodes, group):
+    c = Case("paged", 32, group, 1, dim, nodes, [300, 40, 0, 2000], [nodes, nodes, 0, 1], seed=21)
+    want, want_lse, _ = run(c)
+    put = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    out = gu.Guarded(c.q.shape, torch.float16)
+    ws = torch.empty(binding.tree_workspace_bytes(4, nodes, group, 1, dim, 2000), dtype=torch.uint8, device="cuda")
+    binding.decode_attention_tree(out.view, None, put(c.q), put(c.k), put(c.v), put(c.table), put(c.lens), put(c.trees),
+                                  put(od.pack_mask(c.see)), 2000, c.scale, ws)
+    torch.cuda.synchronize()
+    assert out.intact() and np.array_equal(gu.bits(out.view), want.view(np.uint16))

@@ -208,3 +208,17 @@ def test_masks(nodes, shape):
     want = od.pack_mask(np.stack([od.ancestor_mask(parents[b], lens[b], nodes) for b in range(5)]))
     torch.cuda.synchronize()
     assert int(flags.item()) == od.FLAG_TREE_RANGE and np.array_equal(mask.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("vocab", [2047, 2048, 2049, 4095, 4097, 8191, 16385, 32767, 32769, 65535, 65537, 131071, 131072, 140001])
+def test_vocabularies_at_the_borders_of_the_forms(dtype, vocab):
+    target, draft, tokens, parents, uniforms = make(vocab, 2, 4, vocab, dtype, "star")
+    uniforms[1] = np.float32(1 - 2.0 ** -24)         # the last tokens of the rows too
+    check(target, draft, tokens, parents, None, uniforms)
+
+
+def test_more_sequences_than_clusters_fit():
+    target, draft, tokens, parents, uniforms = make(7, 200, 6, 9001, torch.float16, "mixed")
+    lens = np.random.default_rng(1).integers(0, 7, 200).astype(np.int32)
+    check(target, draft, tokens, parents, lens, uniforms)
