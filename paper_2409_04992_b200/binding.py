@@ -155,7 +155,8 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
 
 def _here(*tensors: Optional[torch.Tensor]) -> None:
     """Refuses tensors of another device than the current one (whose stream the call goes to)."""
-    device = torch.cuda.current_device()
+    # (the raw query, as in _stream: a microsecond less per call; -1 for tensors of the host)
+    device = torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != device:
             raise InstInferError(ERR_INVALID_ARG)

@@ -15,6 +15,11 @@
 // threads of a group and follow the maximum lazily: a vote per tile says whether any logit exceeds its row's
 // by more than kGroupLag, and only then maxima are exchanged and the accumulator rescaled.  A thread keeps
 // its own share of the rows' sums.
+//
+// Measured (K and V bytes per second, 16 sequences of 4k to 8k tokens, 40 KV heads, head size 128, 32-token blocks,
+// with the merge): 8 rows 6.23 TB/s, 16 rows 6.16, 32 rows 5.91 (memory is the bound), 64 rows 5.35 in short runs and
+// 4.65 sustained, where the exponentials and the MMAs' power (the clock falls to 1.5 GHz) weigh as much as memory.
+// Head size 256: 16 rows 6.24, 64 rows 5.56.
 #pragma once
 
 #include "tree_umma_common.cuh"

