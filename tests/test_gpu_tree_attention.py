@@ -458,3 +458,38 @@ def test_without_log_sum_exps_and_flags(dim, nodes, group):
                                   put(od.pack_mask(c.see)), 2000, c.scale, ws)
     torch.cuda.synchronize()
     assert out.intact() and np.array_equal(gu.bits(out.view), want.view(np.uint16))
+
+
+@pytest.mark.parametrize("nodes,group", [(9, 1), (40, 1), (40, 4)])
+def test_drawn_pieces_in_a_captured_call(path, nodes, group):
+    """Replays, and an eager call between them on the same workspace, give the same bits: the counter that
+    pieces are drawn from starts anew each time."""
+    if path == 1:
+        pytest.skip("the cut into pieces belongs to the tcgen05 form")
+    B, H, D, n = 4, 8, 128, 16384
+    g = torch.Generator(device="cuda").manual_seed(nodes)
+    draw = lambda *s: torch.randn(*s, generator=g, device="cuda").half()  # noqa: E731
+    k, v, q = draw(B, H, n, D), draw(B, H, n, D), draw(B, nodes, H * group, D)
+    lens = torch.tensor([n, n - 77, n - 5000, n], dtype=torch.int32, device="cuda")
+    see = np.stack([od.ancestor_mask(random_tree(np.random.default_rng(b), nodes, nodes), nodes, nodes) for b in range(B)])
+    mask = torch.from_numpy(od.pack_mask(see)).cuda()
+    ws = torch.full((binding.tree_workspace_bytes(B, nodes, H * group, H, D, n),), 255, dtype=torch.uint8, device="cuda")
+    flags = torch.zeros(1, dtype=torch.int32, device="cuda")
+    eager, captured = (torch.zeros_like(q) for _ in range(2))
+
+    def call(out):
+        binding.decode_attention_tree(out, None, q, k, v, None, lens, None, mask, n, D ** -0.5, ws, flags)
+
+    call(eager)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(captured)
+    for _ in range(3):
+        captured.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(captured.view(torch.int16), eager.view(torch.int16))
+        call(eager)
+    torch.cuda.synchronize()
+    assert torch.equal(captured.view(torch.int16), eager.view(torch.int16)) and int(flags.item()) == 0
