@@ -17,7 +17,7 @@
 // waited for the MMAs that use the weights and for those of the next logits, 2700 of 6100 cycles a tile.
 // (Leaving the low parts out in this form gave another 11 % and 1.4 times the error.)
 //
-// Measured: 256 rows (32 nodes x 8 heads) over 8 x 32k tokens of 8 KV heads, head size 128: 457 us, 469 TFLOP/s of the
+// Measured: 256 rows (32 nodes x 8 heads) over 8 x 32k tokens of 8 KV heads, head size 128: 460 us, 466 TFLOP/s of the
 // two products counted once (the low parts' MMAs come on top: the tensor pipe is active 55 % of the time, the
 // exponentials' pipe 38 %); 512 rows 739 TFLOP/s.  What bounds it is the chain logits -> softmax -> weights of a unit,
 // of which a block has two (or four half) in flight.
