@@ -239,7 +239,17 @@ tree_attn_rows_kernel(const __grid_constant__ TreeParams p, const __grid_constan
                 const int start = j * kTreeTile;
                 const bool masked = start + kTreeTile > prefix;       // uniform
                 // (stream 0 cleans for both: the output MMAs of a tile start with it)
-                if (masked && s == 0) copies.template clean_values<32>(seg, j, g, (warp & 3) * 32, poison, fine);
+                if (masked && s == 0) {
+                    // Whether a value tile has landed is a parity of its slot's barrier: only once the slot's last tenant
+                    // has landed does it speak of this tile.  This warp has seen logits of the tile before, for whose
+                    // buffer the weights two tiles further back were used up; a tenant younger than that (head size 256:
+                    // three slots for two items a tile) is waited for through the output MMAs that read it.
+                    if constexpr (kVSlots < 3 * kItems) {
+                        if (g > 0 && fine) fine = tree_wait(misc + kTreeBarPvDone + buffer_of(g - 1, s, kUnits - 1) * 8, use_of(g - 1) & 1);
+                        fine = __all_sync(0xffffffffu, fine);
+                    }
+                    copies.template clean_values<32>(seg, j, g, (warp & 3) * 32, poison, fine);
+                }
                 // What the row sees of the tile, where that is not all of it; a negative scale takes the same way:
                 // its sign goes to the logits, so that the maximum is the maximum.
                 const bool special = masked || a.scale_log2e < 0.f;   // uniform

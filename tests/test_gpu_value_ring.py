@@ -1,0 +1,93 @@
+"""Value tiles that land late: other streams keep memory busy while sequences end inside a tile, where the
+softmax warps clear value rows that must not meet a weight of 0.  What they clear has to be this tile's rows and
+not those of the tile that the slot held before, so that every run gives the same bits, those of 64-bit attention."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import draft as od
+from paper_2409_04992_b200 import binding
+from tests.test_gpu_tree_attention import compare, random_tree
+
+pytestmark = pytest.mark.gpu
+
+
+class Busy:
+    """Copies on other streams, for as long as a call takes."""
+
+    def __init__(self):
+        self.streams = [torch.cuda.Stream() for _ in range(2)]
+        self.buffers = [torch.zeros(2, 1 << 27, dtype=torch.uint8, device="cuda") for _ in self.streams]
+
+    def start(self):
+        for stream, both in zip(self.streams, self.buffers):
+            with torch.cuda.stream(stream):
+                for _ in range(4):
+                    both[0].copy_(both[1])
+
+
+def pool_of(lens, kv_heads, tokens, dim, seed):
+    """(k, v, table): pages in a random order; what no sequence holds is not finite."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    per = max(od.blocks_for(n, tokens) for n in lens)
+    ids = np.random.default_rng(seed).permutation(len(lens) * per).reshape(len(lens), per).astype(np.int32)
+    table = torch.from_numpy(ids).cuda()
+    k, v = (torch.randn(len(lens) * per, kv_heads, tokens, dim, generator=g, device="cuda").half() for _ in range(2))
+    for b, n in enumerate(lens):
+        for e in range(per):
+            for cache in (k, v):
+                cache[int(ids[b, e]), :, max(0, min(tokens, n - e * tokens)):] = float("nan")
+    return k, v, table
+
+
+def rows(cache, table, b, h, n, tokens):
+    return cache[table[b, :od.blocks_for(n, tokens)].long(), h].flatten(0, 1)[:n].double()
+
+
+def repeat(call, outs, times=40):
+    """The first run's outputs; every other one has the same bits, with and without busy memory."""
+    busy, first = Busy(), None
+    for i in range(times):
+        for o in outs:
+            o.fill_(float("nan"))
+        if i % 2:
+            busy.start()
+        call()
+        torch.cuda.synchronize()
+        bits = [o.view(torch.int16).clone() for o in outs]
+        first = first or bits
+        assert all(torch.equal(x, y) for x, y in zip(first, bits)), f"run {i}"
+    return outs
+
+
+@pytest.mark.parametrize("dim,group,nodes,kv_heads,tokens", [
+    (256, 3, 25, 5, 16), (256, 1, 128, 4, 64), (128, 3, 25, 8, 16), (128, 8, 32, 4, 32), (64, 4, 33, 6, 16), (256, 1, 20, 5, 16), (128, 1, 40, 8, 32)])
+def test_trees(dim, group, nodes, kv_heads, tokens):
+    lens = [20011, 16682, 13351, 10001, 6691, 3363, 133, 1090, 517, 777, 2051]
+    B, q_heads = len(lens), kv_heads * group
+    k, v, table = pool_of(lens, kv_heads, tokens, dim, dim + nodes)
+    rng = np.random.default_rng(1)
+    trees = [max(1, nodes - (b % 3) * (nodes // 4)) for b in range(B)]
+    see = np.stack([od.ancestor_mask(random_tree(rng, t, nodes), t, nodes) for t in trees])
+    q = torch.randn(B, nodes, q_heads, dim, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").half()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], dtype=torch.float32, device="cuda")
+    ws = torch.empty(binding.tree_workspace_bytes(B, nodes, q_heads, kv_heads, dim, max(lens)), dtype=torch.uint8, device="cuda")
+    flags = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    lens_gpu, trees_gpu, mask = ints(lens), ints(trees), torch.from_numpy(od.pack_mask(see)).cuda()
+    repeat(lambda: binding.decode_attention_tree(out, lse, q, k, v, table, lens_gpu, trees_gpu, mask, max(lens), dim ** -0.5, ws, flags),
+           [out, lse])
+    assert int(flags.item()) == 0
+    for b, (n, t) in enumerate(zip(lens, trees)):
+        hide = torch.zeros(t, n, dtype=torch.float64, device="cuda")
+        hide[:, n - t:] = torch.where(torch.from_numpy(see[b, :t, :t]).cuda(), 0.0, -float("inf"))
+        for h in range(kv_heads):
+            ks, vs = rows(k, table, b, h, n, tokens), rows(v, table, b, h, n, tokens)
+            mine = slice(h * group, (h + 1) * group)
+            queries = q[b, :t, mine].double()
+            s = torch.einsum("tgd,nd->tgn", queries, ks) * dim ** -0.5
+            spread = (torch.einsum("tgd,nd->tgn", queries.abs(), ks.abs()) * dim ** -0.5).amax(-1)
+            s += hide[:, None]
+            w = torch.softmax(s, -1)
+            compare(out[b, :t, mine].cpu().numpy(), lse[b, :t, mine].cpu().numpy(),
+                    [x.cpu().numpy() for x in (w @ vs, torch.logsumexp(s, -1), w @ vs.abs(), spread)], f"sequence {b} head {h}", n)
