@@ -780,6 +780,10 @@ grouped_attn_umma_kernel(const GroupedParams p, unsigned *ticket, const __grid_c
                         // The value row of a position outside the chunk gets weight zero, but its bytes
                         // may be anything (the tail of a block, a slot not fetched): 0 x NaN must not
                         // reach the accumulator, so the row is cleared once the tile has landed.
+                        // Landed is a parity of the slot's barrier, which speaks of this tile once the slot's last tenant
+                        // has landed.  The tile before the last one has been used up (its weights' buffer was needed
+                        // again); a younger tenant (head size 256: three slots for two items a tile) is waited for.
+                        if (kSlots < 2 * kItems && g > 0) fine = mbarrier_poll_bounded(misc + kUmmaBarPvDone, (g - 1) & 1);
                         const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
                         for (int item = 0; item < kItems; ++item) {

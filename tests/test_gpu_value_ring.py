@@ -7,6 +7,7 @@ import torch
 
 from oracle import draft as od
 from paper_2409_04992_b200 import binding
+from tests import gpu_util as gu
 from tests.test_gpu_tree_attention import compare, random_tree
 
 pytestmark = pytest.mark.gpu
@@ -91,3 +92,28 @@ def test_trees(dim, group, nodes, kv_heads, tokens):
             w = torch.softmax(s, -1)
             compare(out[b, :t, mine].cpu().numpy(), lse[b, :t, mine].cpu().numpy(),
                     [x.cpu().numpy() for x in (w @ vs, torch.logsumexp(s, -1), w @ vs.abs(), spread)], f"sequence {b} head {h}", n)
+
+
+@pytest.mark.parametrize("dim,q_tokens,group,kv_heads,tokens", [(256, 1, 8, 5, 16), (256, 4, 2, 8, 64), (128, 2, 4, 8, 32)])
+def test_grouped_steps(dim, q_tokens, group, kv_heads, tokens):
+    """The same for the grouped entry point, whose tolerances are the library's (2e-3 on unit-variance values)."""
+    lens = [20011, 16682, 13351, 10001, 6691, 3363, 133, 1090, 517, 777, 2051]
+    B, q_heads = len(lens), kv_heads * group
+    k, v, table = pool_of(lens, kv_heads, tokens, dim, dim + q_tokens)
+    q = torch.randn(B, q_tokens, q_heads, dim, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").half()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], dtype=torch.float32, device="cuda")
+    ws = torch.empty(binding.grouped_workspace_bytes(B, q_tokens, q_heads, kv_heads, dim, max(lens)), dtype=torch.uint8, device="cuda")
+    flags = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lens_gpu = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    repeat(lambda: binding.decode_attention_grouped(out, lse, q, k, v, table, lens_gpu, max(lens), dim ** -0.5, ws, flags), [out, lse])
+    assert int(flags.item()) == 0
+    for b, n in enumerate(lens):
+        hide = torch.zeros(q_tokens, n, dtype=torch.float64, device="cuda")
+        for t in range(q_tokens):
+            hide[t, n - (q_tokens - 1 - t):] = -float("inf")
+        for h in range(kv_heads):
+            ks, vs = rows(k, table, b, h, n, tokens), rows(v, table, b, h, n, tokens)
+            mine = slice(h * group, (h + 1) * group)
+            s = torch.einsum("tgd,nd->tgn", q[b, :, mine].double(), ks) * dim ** -0.5 + hide[:, None]
+            assert (out[b, :, mine].double() - torch.softmax(s, -1) @ vs).abs().max() <= gu.MAX_ABS, (b, h)
+            assert (lse[b, :, mine].double() - torch.logsumexp(s, -1)).abs().max() <= gu.LSE_ATOL + 20 * gu.LSE_RTOL, (b, h)
