@@ -419,7 +419,8 @@ size_t instinfer_kv_resize_workspace_bytes(int32_t batch, int64_t num_phys_block
  * stay.  Tables and counts are written to new_block_table [batch, max_blocks_per_seq] and
  * new_block_refs [num_phys_blocks] (which may be block_table and block_refs themselves; entries
  * behind a sequence's last block are copied as they are), *blocks_used = U (device).  Blocks from U
- * on are free afterwards.
+ * on are free afterwards.  A listed block that counts as free is nobody's, and another one may be moved
+ * over it: its entries are copied as they are and flagged INSTINFER_FLAG_POOL.
  *   workspace  at least instinfer_kv_defragment_workspace_bytes(num_phys_blocks) bytes
  */
 int instinfer_kv_defragment(void *const *k_pools, void *const *v_pools, int32_t n_layers,

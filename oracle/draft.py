@@ -264,7 +264,7 @@ def defragment(caches, table, refs, seq_lens, tokens):
     used = int((refs > 0).sum())
     holes = [i for i in range(used) if refs[i] <= 0]
     movers = [i for i in range(used, len(refs)) if refs[i] > 0]
-    to = {i: i for i in range(used)}
+    to = {i: i for i in range(used) if refs[i] > 0}
     to.update(zip(movers, holes))
     new_refs = np.zeros_like(refs)
     for i in range(len(refs)):

@@ -489,7 +489,7 @@ kv_defragment_plan_kernel(const DefragmentParams p)
         const int2 sum = plan_scan(make_int2(is_hole, moves), warp_sums, &total);
         if (is_hole) p.list.pages[2 * (hole + sum.x - 1) + 1] = (int)id;
         if (moves) p.list.pages[2 * (mover + sum.y - 1)] = (int)id;
-        if (id < to) p.map[id] = id < used ? (int)id : -1;
+        if (id < to) p.map[id] = in_use && id < used ? (int)id : -1;      // (a hole is no one's, though a mover will lie there)
         hole += total.x;
         mover += total.y;
     }
