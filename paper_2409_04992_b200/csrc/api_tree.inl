@@ -116,6 +116,9 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
     p.a.max_seq_len = max_seq_len;
     p.a.kv_bytes = (paged ? num_phys_blocks * kv_heads * block_tokens : (int64_t)batch * kv_heads * s_max) * head_dim * 2;
     p.a.scale_log2e = scale * 1.44269504088896340736f;
+    // (the kernels start with a reference of -1e30, unscaled: what scale there is has to tell it from a logit.
+    // Logits of fp16 keys stay below 2^41, so that this scale and none give the same weights.)
+    if (fabsf(p.a.scale_log2e) < 1e-20f) p.a.scale_log2e = copysignf(1e-20f, p.a.scale_log2e);
     p.a.part_o = static_cast<float *>(workspace);
     p.a.part_lse = p.a.part_o + (size_t)pairs * plan.n_splits * p.rows * head_dim;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
@@ -133,9 +136,6 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
             make_cache_map(&t.map_k, k_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box) &&
             make_cache_map(&t.map_v, v_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box)) {
             t.p.a = p.a;
-            // (the kernels start with a reference of -1e30, unscaled: what scale there is has to tell it from a logit.
-            // Logits of fp16 keys stay below 2^41, so that this scale and none give the same weights.)
-            if (fabsf(p.a.scale_log2e) < 1e-20f) t.p.a.scale_log2e = copysignf(1e-20f, p.a.scale_log2e);
             t.p.a.part_lse = p.a.part_o + tree_slot_rows(rows) * head_dim;
             t.p.short_pieces = rows.short_pieces;
             unsigned char *behind = static_cast<unsigned char *>(workspace) + tree_partials_bytes(rows, head_dim);

@@ -101,6 +101,10 @@ __device__ __forceinline__ int64_t grouped_row_index(const GroupedParams &p, int
 // One 16-token tile against the 16 query rows: logits, online softmax, and O += P V.  `base`
 // is the stage's shared-memory address; the running state (references, sums, output fragments)
 // is updated in place.
+// Draft trees (kTree): references are logits before the scale (its sign apart), taken off before the scale comes in,
+// as in the tcgen05 forms.  The largest logit's weight is exactly kGroupWeightScale then, however large it is; with
+// scaled references, base-2 logits past 2^24 round reference and weight scale together, and from 2^27 on a weight
+// leaves the range of fp16.
 template <int D, bool kTree>
 __device__ __forceinline__ void grouped_tile(unsigned base, unsigned k_rd, unsigned v_rd, unsigned q_rd,
                                              const unsigned (&qa)[GroupedGeometry<D>::kQInSmem ? 1 : GroupedGeometry<D>::kKSteps][4],
@@ -133,7 +137,15 @@ __device__ __forceinline__ void grouped_tile(unsigned base, unsigned k_rd, unsig
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] = (s[n][e] + s_odd[n][e]) * scale_log2e;
+        for (int e = 0; e < 4; ++e) s[n][e] = kTree ? s[n][e] + s_odd[n][e] : (s[n][e] + s_odd[n][e]) * scale_log2e;
+    }
+    const float factor = kTree ? fabsf(scale_log2e) : 1.f;    // what is left to scale a difference of logits by
+    if (kTree && scale_log2e < 0.f) {                          // uniform
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = -s[n][e];
+        }
     }
     if (tok0 + kGroupTile > unmasked_end) {      // uniform: last tiles of the sequence only
 #pragma unroll
@@ -158,19 +170,21 @@ __device__ __forceinline__ void grouped_tile(unsigned base, unsigned k_rd, unsig
     // rescaling, a tight lag would rescale on most tiles of a short chunk.
     const float top_lo_here = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
     const float top_hi_here = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-    if (__any_sync(0xffffffffu, top_lo_here > m_lo + kGroupLag || top_hi_here > m_hi + kGroupLag)) {
+    auto rises = [&](float top, float m) -> bool { return kTree ? (top - m) * factor > kGroupLag : top > m + kGroupLag; };
+    auto fading = [&](float m, float top) -> float { return fast_exp2(kTree ? (m - top) * factor : m - top); };
+    if (__any_sync(0xffffffffu, rises(top_lo_here, m_lo) || rises(top_hi_here, m_hi))) {
         float top_lo = top_lo_here, top_hi = top_hi_here;
         top_lo = fmaxf(top_lo, __shfl_xor_sync(0xffffffffu, top_lo, 1));
         top_lo = fmaxf(top_lo, __shfl_xor_sync(0xffffffffu, top_lo, 2));
         top_hi = fmaxf(top_hi, __shfl_xor_sync(0xffffffffu, top_hi, 1));
         top_hi = fmaxf(top_hi, __shfl_xor_sync(0xffffffffu, top_hi, 2));
         float alpha_lo = 1.f, alpha_hi = 1.f;
-        if (top_lo > m_lo + kGroupLag) {
-            alpha_lo = fast_exp2(m_lo - top_lo);
+        if (rises(top_lo, m_lo)) {
+            alpha_lo = fading(m_lo, top_lo);
             m_lo = top_lo;
         }
-        if (top_hi > m_hi + kGroupLag) {
-            alpha_hi = fast_exp2(m_hi - top_hi);
+        if (rises(top_hi, m_hi)) {
+            alpha_hi = fading(m_hi, top_hi);
             m_hi = top_hi;
         }
         l_lo *= alpha_lo;
@@ -191,7 +205,8 @@ __device__ __forceinline__ void grouped_tile(unsigned base, unsigned k_rd, unsig
     for (int n = 0; n < 2; ++n) {
         float w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = fast_exp2(s[n][e] - (e < 2 ? e_lo : e_hi));
+        for (int e = 0; e < 4; ++e)
+            w[e] = fast_exp2(kTree ? fmaf(s[n][e] - (e < 2 ? m_lo : m_hi), factor, kGroupWeightLog2) : s[n][e] - (e < 2 ? e_lo : e_hi));
         l_lo += w[0] + w[1];
         l_hi += w[2] + w[3];
         p_hi[2 * n] = pack_half2(w[0], w[1]);
@@ -399,7 +414,7 @@ grouped_attn_split_kernel(const GroupedParams p)
     const unsigned k_rd = (mrow + (mat >> 1) * 8) * G::kRowStride + (mat & 1) * 16;
     const unsigned v_rd = G::kTileBytes + (mrow + (mat & 1) * 8) * G::kRowStride + (mat >> 1) * 16;
 
-    // Running state of rows gid (lo) and gid + 8 (hi): reference m (base-2 logits), this
+    // Running state of rows gid (lo) and gid + 8 (hi): reference m (base-2 logits; kTree: unscaled ones), this
     // lane's share of the sum l, and the output fragments; l and o carry kGroupWeightScale.
     float m_lo = kMinusHuge, m_hi = kMinusHuge, l_lo = 0.f, l_hi = 0.f;
     float o[D / 8][4];
@@ -466,6 +481,7 @@ grouped_attn_split_kernel(const GroupedParams p)
     }
     __syncthreads();
 
+    const float factor = kTree ? fabsf(a.scale_log2e) : 1.f;
     for (int i = threadIdx.x; i < rows_here * D; i += kThreads) {
         const int r = i / D, d = i - r * D;
         float top = kMinusHuge;
@@ -474,7 +490,7 @@ grouped_attn_split_kernel(const GroupedParams p)
         float total = 0.f, acc = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            const float weight = fast_exp2(sm_m[w * kGroupRows + r] - top);
+            const float weight = fast_exp2(kTree ? (sm_m[w * kGroupRows + r] - top) * factor : sm_m[w * kGroupRows + r] - top);
             total = fmaf(weight, sm_l[w * kGroupRows + r], total);
             acc = fmaf(weight, sm_o[(w * kGroupRows + r) * D + d], acc);
         }
@@ -483,7 +499,7 @@ grouped_attn_split_kernel(const GroupedParams p)
         // tree have met the tiles before it unmasked and end here.)
         const bool empty = kTree ? total == 0.f || (row0 + r) / p.group >= nodes : !(total > 0.f);
         float value = empty ? 0.f : acc / total;
-        const float lse2 = empty ? kMinusHuge : top + log2f(total) - kGroupWeightLog2;
+        const float lse2 = empty ? kMinusHuge : kTree ? fmaf(top, factor, log2f(total) - kGroupWeightLog2) : top + log2f(total) - kGroupWeightLog2;
         if (kTree && (poison[0] | poison[1] | poison[2] | poison[3]) != 0u) {
             const TreeRow seen = tree_row(p.tree, b, (row0 + r) / p.group, nodes);
             const __half *q_row = a.q + grouped_row_index(p, b, hk, row0 + r) * D;
