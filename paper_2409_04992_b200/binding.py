@@ -146,20 +146,20 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _stream(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
+def _stream(stream: Optional[torch.cuda.Stream], device: Optional[int] = None) -> Optional[int]:
     if stream is not None:
         return stream.cuda_stream or None
     # (the raw handle: a Stream object per call costs as much as a short kernel)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device) or None
 
 
-def _here(*tensors: Optional[torch.Tensor]) -> None:
-    """Refuses tensors of another device than the current one (whose stream the call goes to)."""
+def _here(*tensors: Optional[torch.Tensor]) -> int:
+    """The current device, whose stream the call goes to; refuses tensors of another one (None: not given)."""
     # (the raw query, as in _stream: a microsecond less per call; -1 for tensors of the host)
     device = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise InstInferError(ERR_INVALID_ARG)
+    if {t.get_device() for t in tensors if t is not None} != {device}:
+        raise InstInferError(ERR_INVALID_ARG)
+    return device
 
 
 def _check(status: int) -> None:
@@ -348,9 +348,9 @@ def tree_mask(mask: torch.Tensor, parents: torch.Tensor, tree_lens: Optional[tor
     """instinfer_tree_mask: mask int64 [B, T, ceil(T / 64)] (the bits of the header's uint64 words),
     parents int32 [B, T], tree_lens int32 [B] (None: T nodes each)."""
     batch, tree_tokens = parents.shape
-    _here(mask, parents)
-    _check(load().instinfer_tree_mask(_ptr(mask), _ptr(parents), _ptr(tree_lens), batch, tree_tokens,
-                                      _ptr(status_flags), _stream(stream)))
+    here = _here(mask, parents, tree_lens, status_flags)
+    _check(load().instinfer_tree_mask(mask.data_ptr(), parents.data_ptr(), _ptr(tree_lens), batch, tree_tokens,
+                                      _ptr(status_flags), _stream(stream, here)))
 
 
 def tree_workspace_bytes(batch: int, tree_tokens: int, q_heads: int, kv_heads: int, head_dim: int,
@@ -369,17 +369,17 @@ def decode_attention_tree(out: torch.Tensor, lse: Optional[torch.Tensor], q: tor
     with Hkv heads ([B,Hkv,s_max,D], or pools [P,Hkv,T,D] with block_table)."""
     batch, tree_tokens, q_heads, head_dim = q.shape
     kv_heads = k_cache.shape[1]
-    _here(out, q, k_cache, workspace)
+    here = _here(out, lse, q, k_cache, v_cache, block_table, seq_lens, tree_lens, mask, workspace, status_flags)
     if block_table is None:
         s_max, block_tokens, max_blocks, phys = k_cache.shape[2], 0, 0, 0
     else:
         s_max, block_tokens, max_blocks, phys = (0, k_cache.shape[2], block_table.shape[1],
                                                  k_cache.shape[0])
     _check(load().instinfer_decode_attention_tree(
-        _ptr(out), _ptr(lse), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens),
-        _ptr(tree_lens), _ptr(mask), batch, tree_tokens, q_heads, kv_heads, head_dim, s_max, block_tokens,
-        max_blocks, phys, int(max_seq_len), float(scale), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _ptr(status_flags), _stream(stream)))
+        out.data_ptr(), _ptr(lse), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(block_table), seq_lens.data_ptr(),
+        _ptr(tree_lens), mask.data_ptr(), batch, tree_tokens, q_heads, kv_heads, head_dim, s_max, block_tokens,
+        max_blocks, phys, int(max_seq_len), float(scale), workspace.data_ptr(),
+        workspace.nbytes, _ptr(status_flags), _stream(stream, here)))
 
 
 _PROBS_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -401,26 +401,28 @@ def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.T
                 (vocab > 1 and probs.stride(2) != 1) or (tree_tokens > 1 and probs.stride(1) != stride) or
                 (batch > 1 and probs.stride(0) != tree_tokens * stride)):
             raise InstInferError(ERR_INVALID_ARG)
-    _here(path, target_probs, tokens)
+    here = _here(path, path_lens, out_tokens, target_probs, draft_probs, tokens, parents, tree_lens, uniforms, status_flags)
     if target_probs.dtype not in _PROBS_TYPES:
         raise InstInferError(ERR_UNSUPPORTED)
     _check(load().instinfer_verify_tree(
-        _ptr(path), _ptr(path_lens), _ptr(out_tokens), _ptr(target_probs), _ptr(draft_probs),
-        _PROBS_TYPES[target_probs.dtype], stride, _ptr(tokens), _ptr(parents), _ptr(tree_lens),
-        _ptr(uniforms), batch, tree_tokens, vocab, _ptr(status_flags), _stream(stream)))
+        path.data_ptr(), path_lens.data_ptr(), out_tokens.data_ptr(), target_probs.data_ptr(), _ptr(draft_probs),
+        _PROBS_TYPES[target_probs.dtype], stride, tokens.data_ptr(), parents.data_ptr(), _ptr(tree_lens),
+        uniforms.data_ptr(), batch, tree_tokens, vocab, _ptr(status_flags), _stream(stream, here)))
 
 
-def _layers(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor]):
-    """The two HOST pointer arrays of the calls that work on all layers at once."""
+def _layers(here: int, k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor]):
+    """The two HOST pointer arrays of the calls that work on all layers at once, and the caches' shape: as many V as K
+    caches, contiguous, of one size, all on the device `here`."""
     n = len(k_caches)
     caches = [*k_caches, *v_caches]
-    # (whole passes in C: a model has some hundred caches, and a Python loop over them outlasts the kernel)
+    # (whole passes in C: a model has some hundred caches, and a Python loop over them outlasts the kernel.)
     if n == 0 or len(caches) != 2 * n or not all(map(torch.Tensor.is_contiguous, caches)) or \
-            len(set(map(torch.Tensor.numel, caches))) != 1:
+            len(set(map(torch.Tensor.numel, caches))) != 1 or set(map(torch.Tensor.get_device, caches)) != {here}:
         raise InstInferError(ERR_INVALID_ARG)
+    shape = k_caches[0].shape
     addresses = array.array("Q", map(torch.Tensor.data_ptr, caches))
     at, _ = addresses.buffer_info()
-    return at, at + 8 * n, n, addresses          # the caller keeps `addresses` alive during the call
+    return at, at + 8 * n, n, shape, addresses   # the caller keeps `addresses` alive during the call
 
 
 def kv_keep_path(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor], path: torch.Tensor,
@@ -431,17 +433,16 @@ def kv_keep_path(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tens
     """instinfer_kv_keep_path: one cache per layer ([B,H,s_max,D], or pools [P,H,T,D] with
     block_table); path [B, tree_tokens]."""
     batch, tree_tokens = path.shape
-    _here(path, k_caches[0] if len(k_caches) else None)
-    k, v, n_layers, keep = _layers(k_caches, v_caches)
-    _, heads, rows, head_dim = k_caches[0].shape
+    here = _here(path, path_lens, tree_lens, seq_lens, new_lens, block_table, status_flags)
+    k, v, n_layers, (blocks, heads, rows, head_dim), keep = _layers(here, k_caches, v_caches)
     if block_table is None:
         max_blocks, block_tokens, phys, s_max = 0, 0, 0, rows
     else:
-        max_blocks, block_tokens, phys, s_max = block_table.shape[1], rows, k_caches[0].shape[0], 0
+        max_blocks, block_tokens, phys, s_max = block_table.shape[1], rows, blocks, 0
     _check(load().instinfer_kv_keep_path(
-        k, v, n_layers, _ptr(path), _ptr(path_lens), _ptr(tree_lens), _ptr(seq_lens), _ptr(new_lens),
+        k, v, n_layers, path.data_ptr(), path_lens.data_ptr(), _ptr(tree_lens), seq_lens.data_ptr(), new_lens.data_ptr(),
         _ptr(block_table), max_blocks, block_tokens, phys, batch, tree_tokens, heads, head_dim, s_max,
-        _ptr(status_flags), _stream(stream)))
+        _ptr(status_flags), _stream(stream, here)))
 
 
 def kv_fork(block_table: torch.Tensor, block_refs: torch.Tensor, seq_lens: torch.Tensor, src: torch.Tensor,
@@ -449,10 +450,10 @@ def kv_fork(block_table: torch.Tensor, block_refs: torch.Tensor, seq_lens: torch
             stream: Optional[torch.cuda.Stream] = None) -> None:
     """instinfer_kv_fork: block_table [B, M], block_refs [P], seq_lens [B], src and dst [n]."""
     batch, max_blocks = block_table.shape
-    _here(block_table, src)
-    _check(load().instinfer_kv_fork(_ptr(block_table), _ptr(block_refs), _ptr(seq_lens), _ptr(src), _ptr(dst),
+    here = _here(block_table, block_refs, seq_lens, src, dst, status_flags)
+    _check(load().instinfer_kv_fork(block_table.data_ptr(), block_refs.data_ptr(), seq_lens.data_ptr(), src.data_ptr(), dst.data_ptr(),
                                     src.numel(), max_blocks, int(block_tokens), block_refs.numel(), batch,
-                                    _ptr(status_flags), _stream(stream)))
+                                    _ptr(status_flags), _stream(stream, here)))
 
 
 def kv_resize_workspace_bytes(batch: int, num_phys_blocks: int) -> int:
@@ -465,13 +466,12 @@ def kv_resize(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tensor], 
               stream: Optional[torch.cuda.Stream] = None) -> None:
     """instinfer_kv_resize: one pool [P,H,T,D] per layer; new_lens may be seq_lens."""
     batch, max_blocks = block_table.shape
-    _here(block_table, workspace, k_pools[0] if len(k_pools) else None)
-    k, v, n_layers, keep = _layers(k_pools, v_pools)
-    phys, heads, block_tokens, head_dim = k_pools[0].shape
+    here = _here(block_table, block_refs, seq_lens, want_lens, new_lens, workspace, status_flags)
+    k, v, n_layers, (phys, heads, block_tokens, head_dim), keep = _layers(here, k_pools, v_pools)
     _check(load().instinfer_kv_resize(
-        k, v, n_layers, _ptr(block_table), _ptr(block_refs), _ptr(seq_lens), _ptr(want_lens), _ptr(new_lens),
-        max_blocks, block_tokens, phys, batch, heads, head_dim, _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _ptr(status_flags), _stream(stream)))
+        k, v, n_layers, block_table.data_ptr(), block_refs.data_ptr(), seq_lens.data_ptr(), want_lens.data_ptr(), new_lens.data_ptr(),
+        max_blocks, block_tokens, phys, batch, heads, head_dim, workspace.data_ptr(),
+        workspace.nbytes, _ptr(status_flags), _stream(stream, here)))
 
 
 def kv_defragment_workspace_bytes(num_phys_blocks: int) -> int:
@@ -486,13 +486,12 @@ def kv_defragment(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tenso
     """instinfer_kv_defragment: one pool [P,H,T,D] per layer; the new table and counts may be the
     old ones; blocks_used int32 [1]."""
     batch, max_blocks = block_table.shape
-    _here(block_table, workspace, k_pools[0] if len(k_pools) else None)
-    k, v, n_layers, keep = _layers(k_pools, v_pools)
-    phys, heads, block_tokens, head_dim = k_pools[0].shape
+    here = _here(block_table, block_refs, seq_lens, new_block_table, new_block_refs, blocks_used, workspace, status_flags)
+    k, v, n_layers, (phys, heads, block_tokens, head_dim), keep = _layers(here, k_pools, v_pools)
     _check(load().instinfer_kv_defragment(
-        k, v, n_layers, _ptr(block_table), _ptr(new_block_table), _ptr(block_refs), _ptr(new_block_refs),
-        _ptr(seq_lens), _ptr(blocks_used), max_blocks, block_tokens, phys, batch, heads, head_dim,
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status_flags), _stream(stream)))
+        k, v, n_layers, block_table.data_ptr(), new_block_table.data_ptr(), block_refs.data_ptr(), new_block_refs.data_ptr(),
+        seq_lens.data_ptr(), blocks_used.data_ptr(), max_blocks, block_tokens, phys, batch, heads, head_dim,
+        workspace.data_ptr(), workspace.nbytes, _ptr(status_flags), _stream(stream, here)))
 
 
 def decode_step_host(out_host: torch.Tensor, qkv_host: torch.Tensor, qkv_dev: torch.Tensor,
