@@ -368,13 +368,16 @@ def decode_attention_tree(out: torch.Tensor, lse: Optional[torch.Tensor], q: tor
     """instinfer_decode_attention_tree: q, out [B, T, Hq, D]; mask as tree_mask writes it; caches
     with Hkv heads ([B,Hkv,s_max,D], or pools [P,Hkv,T,D] with block_table)."""
     batch, tree_tokens, q_heads, head_dim = q.shape
-    kv_heads = k_cache.shape[1]
+    shape = k_cache.shape
+    sequences, kv_heads = shape[0] if block_table is None else block_table.shape[0], shape[1]
     here = _here(out, lse, q, k_cache, v_cache, block_table, seq_lens, tree_lens, mask, workspace, status_flags)
+    if v_cache.shape != shape or shape[3] != head_dim or sequences < batch or \
+            mask.numel() < batch * tree_tokens * ((tree_tokens + 63) // 64):
+        raise InstInferError(ERR_INVALID_ARG)
     if block_table is None:
-        s_max, block_tokens, max_blocks, phys = k_cache.shape[2], 0, 0, 0
+        s_max, block_tokens, max_blocks, phys = shape[2], 0, 0, 0
     else:
-        s_max, block_tokens, max_blocks, phys = (0, k_cache.shape[2], block_table.shape[1],
-                                                 k_cache.shape[0])
+        s_max, block_tokens, max_blocks, phys = 0, shape[2], block_table.shape[1], shape[0]
     _check(load().instinfer_decode_attention_tree(
         out.data_ptr(), _ptr(lse), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(block_table), seq_lens.data_ptr(),
         _ptr(tree_lens), mask.data_ptr(), batch, tree_tokens, q_heads, kv_heads, head_dim, s_max, block_tokens,
@@ -410,16 +413,22 @@ def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.T
         uniforms.data_ptr(), batch, tree_tokens, vocab, _ptr(status_flags), _stream(stream, here)))
 
 
+_bytes_of = torch.Tensor.nbytes.__get__
+
+
 def _layers(here: int, k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor]):
     """The two HOST pointer arrays of the calls that work on all layers at once, and the caches' shape: as many V as K
-    caches, contiguous, of one size, all on the device `here`."""
+    caches, fp16, contiguous, of one size, all on the device `here`."""
     n = len(k_caches)
     caches = [*k_caches, *v_caches]
-    # (whole passes in C: a model has some hundred caches, and a Python loop over them outlasts the kernel.)
+    # (whole passes in C: a model has some hundred caches, and a Python loop over them outlasts the kernel.  One shape
+    # of another type has another number of bytes, so that the first cache's type speaks for all.)
     if n == 0 or len(caches) != 2 * n or not all(map(torch.Tensor.is_contiguous, caches)) or \
-            len(set(map(torch.Tensor.numel, caches))) != 1 or set(map(torch.Tensor.get_device, caches)) != {here}:
+            len(set(map(_bytes_of, caches))) != 1 or set(map(torch.Tensor.get_device, caches)) != {here}:
         raise InstInferError(ERR_INVALID_ARG)
     shape = k_caches[0].shape
+    if v_caches[0].shape != shape or k_caches[0].dtype is not torch.float16:
+        raise InstInferError(ERR_INVALID_ARG)
     addresses = array.array("Q", map(torch.Tensor.data_ptr, caches))
     at, _ = addresses.buffer_info()
     return at, at + 8 * n, n, shape, addresses   # the caller keeps `addresses` alive during the call
@@ -436,9 +445,12 @@ def kv_keep_path(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tens
     here = _here(path, path_lens, tree_lens, seq_lens, new_lens, block_table, status_flags)
     k, v, n_layers, (blocks, heads, rows, head_dim), keep = _layers(here, k_caches, v_caches)
     if block_table is None:
-        max_blocks, block_tokens, phys, s_max = 0, 0, 0, rows
+        sequences, max_blocks, block_tokens, phys, s_max = blocks, 0, 0, 0, rows
     else:
-        max_blocks, block_tokens, phys, s_max = block_table.shape[1], rows, blocks, 0
+        sequences, max_blocks = block_table.shape
+        block_tokens, phys, s_max = rows, blocks, 0
+    if sequences < batch:
+        raise InstInferError(ERR_INVALID_ARG)
     _check(load().instinfer_kv_keep_path(
         k, v, n_layers, path.data_ptr(), path_lens.data_ptr(), _ptr(tree_lens), seq_lens.data_ptr(), new_lens.data_ptr(),
         _ptr(block_table), max_blocks, block_tokens, phys, batch, tree_tokens, heads, head_dim, s_max,
@@ -451,6 +463,8 @@ def kv_fork(block_table: torch.Tensor, block_refs: torch.Tensor, seq_lens: torch
     """instinfer_kv_fork: block_table [B, M], block_refs [P], seq_lens [B], src and dst [n]."""
     batch, max_blocks = block_table.shape
     here = _here(block_table, block_refs, seq_lens, src, dst, status_flags)
+    if dst.numel() != src.numel():
+        raise InstInferError(ERR_INVALID_ARG)
     _check(load().instinfer_kv_fork(block_table.data_ptr(), block_refs.data_ptr(), seq_lens.data_ptr(), src.data_ptr(), dst.data_ptr(),
                                     src.numel(), max_blocks, int(block_tokens), block_refs.numel(), batch,
                                     _ptr(status_flags), _stream(stream, here)))
@@ -468,6 +482,8 @@ def kv_resize(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tensor], 
     batch, max_blocks = block_table.shape
     here = _here(block_table, block_refs, seq_lens, want_lens, new_lens, workspace, status_flags)
     k, v, n_layers, (phys, heads, block_tokens, head_dim), keep = _layers(here, k_pools, v_pools)
+    if block_refs.numel() < phys:
+        raise InstInferError(ERR_INVALID_ARG)
     _check(load().instinfer_kv_resize(
         k, v, n_layers, block_table.data_ptr(), block_refs.data_ptr(), seq_lens.data_ptr(), want_lens.data_ptr(), new_lens.data_ptr(),
         max_blocks, block_tokens, phys, batch, heads, head_dim, workspace.data_ptr(),
@@ -488,6 +504,8 @@ def kv_defragment(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tenso
     batch, max_blocks = block_table.shape
     here = _here(block_table, block_refs, seq_lens, new_block_table, new_block_refs, blocks_used, workspace, status_flags)
     k, v, n_layers, (phys, heads, block_tokens, head_dim), keep = _layers(here, k_pools, v_pools)
+    if block_refs.numel() < phys or new_block_refs.numel() < phys or new_block_table.shape != block_table.shape:
+        raise InstInferError(ERR_INVALID_ARG)
     _check(load().instinfer_kv_defragment(
         k, v, n_layers, block_table.data_ptr(), new_block_table.data_ptr(), block_refs.data_ptr(), new_block_refs.data_ptr(),
         seq_lens.data_ptr(), blocks_used.data_ptr(), max_blocks, block_tokens, phys, batch, heads, head_dim,

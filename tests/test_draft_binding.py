@@ -116,6 +116,53 @@ def test_a_layer_of_another_device_is_refused(lib, call, name, layer):
     refused(lib, call, args)
 
 
+@pytest.mark.parametrize("call,name", LAYERED)
+@pytest.mark.parametrize("layer", range(LAYERS))
+def test_a_layer_of_another_type_or_size_is_refused(lib, call, name, layer):
+    for bad in (torch.zeros(P, HKV, PAGE, D), torch.zeros(P, HKV, PAGE, D, dtype=torch.int64), halves(P - 1, HKV, PAGE, D),
+                halves(P, HKV, D, PAGE).transpose(2, 3)):
+        args = CALLS[call]()
+        args[name][layer] = bad
+        refused(lib, call, args)
+
+
+@pytest.mark.parametrize("call,name", LAYERED)
+def test_pools_of_another_type_or_number_are_refused(lib, call, name):
+    other = name.replace("k_", "v_") if name.startswith("k_") else name.replace("v_", "k_")
+    args = CALLS[call]()
+    args[name] = args[name][1:]
+    refused(lib, call, args)
+    args = CALLS[call]()
+    args[name], args[other] = ([x.float() for x in args[n]] for n in (name, other))
+    refused(lib, call, args)
+    args = CALLS[call]()
+    args[name] = [halves(P, PAGE, HKV, D) for _ in range(LAYERS)]        # as many elements, another layout
+    refused(lib, call, args)
+
+
+def test_what_belongs_together_has_to_fit(lib):
+    for call in ("kv_resize", "kv_defragment"):
+        refused(lib, call, dict(CALLS[call](), block_refs=ints(P - 1)))
+    refused(lib, "kv_defragment", dict(CALLS["kv_defragment"](), new_block_refs=ints(P - 1)))
+    for shape in ((B - 1, M), (B, M - 1), (B, M + 1)):
+        refused(lib, "kv_defragment", dict(CALLS["kv_defragment"](), new_block_table=ints(*shape)))
+    for src, dst in ((2, 1), (1, 2)):
+        refused(lib, "kv_fork", dict(CALLS["kv_fork"](), src=ints(src), dst=ints(dst)))
+    refused(lib, "decode_attention_tree", dict(CALLS["decode_attention_tree"](), v_cache=halves(P, PAGE, HKV, D)))
+    refused(lib, "decode_attention_tree", dict(CALLS["decode_attention_tree"](), v_cache=halves(P - 1, HKV, PAGE, D)))
+    # caches, tables and masks of fewer sequences than the call's, of other heads, or of fewer nodes
+    tree, keep = CALLS["decode_attention_tree"], CALLS["kv_keep_path"]
+    refused(lib, "decode_attention_tree", dict(tree(), block_table=ints(B - 1, M)))
+    refused(lib, "decode_attention_tree", dict(tree(), block_table=None, k_cache=halves(B - 1, HKV, 100, D), v_cache=halves(B - 1, HKV, 100, D)))
+    refused(lib, "decode_attention_tree", dict(tree(), k_cache=halves(P, HKV, PAGE, 2 * D), v_cache=halves(P, HKV, PAGE, 2 * D)))
+    refused(lib, "decode_attention_tree", dict(tree(), mask=torch.zeros(B - 1, T, 1, dtype=torch.int64)))
+    wide = dict(tree(), q=halves(B, 65, HQ, D), out=halves(B, 65, HQ, D), lse=torch.zeros(B, 65, HQ))
+    refused(lib, "decode_attention_tree", dict(wide, mask=torch.zeros(B, 65, 1, dtype=torch.int64)))
+    refused(lib, "kv_keep_path", dict(keep(), block_table=ints(B - 1, M)))
+    few = [halves(B - 1, HKV, 100, D) for _ in range(LAYERS)]
+    refused(lib, "kv_keep_path", dict(keep(), block_table=None, k_caches=few, v_caches=few))
+
+
 def test_buffers_may_be_larger_and_rows_further_apart(lib):
     binding.decode_attention_tree(**dict(CALLS["decode_attention_tree"](), seq_lens=ints(B + 5), status_flags=ints(4)), stream=STREAM)
     binding.kv_resize(**dict(CALLS["kv_resize"](), seq_lens=ints(B + 1), new_lens=ints(B + 3), block_refs=ints(P + 1)), stream=STREAM)
