@@ -29,19 +29,29 @@ PlanRules tree_rules(int32_t head_dim)
 
 // ---- the tcgen05 form ----
 
-// Rows of the partial results: two slots per piece, at most 1 + short_pieces pieces per block and one more.  Behind
-// them lie the items' pieces and the ticket counter.
-size_t tree_slot_rows(const TreeRows &r) { return (size_t)2 * (sm_count() * (1 + r.short_pieces) + 1) * r.item_rows; }
-
-size_t tree_partials_bytes(const TreeRows &r, int32_t head_dim)
+// The grid, and the workspace: partial results (two slots of an item's rows per piece), then the items' pieces and the
+// ticket counter.  One function for the size query and the launch, so that they cannot part: the pieces that the kernel
+// cuts (TreePieces) are one per block, and where the longest sequences allowed could give every block kTreeDrawnTiles
+// tiles, short_pieces more.
+struct TreeCut {
+    int64_t items, most_tiles;    // tiles (with the items' extra weight) if all sequences were max_seq_len long
+    unsigned grid;
+    bool draws;
+    size_t slot_rows, partials_bytes, ticket_offset, bytes;
+};
+TreeCut tree_cut(const TreeRows &r, int64_t pairs, int32_t max_seq_len, int32_t head_dim)
 {
-    return (tree_slot_rows(r) * (head_dim + 1) * sizeof(float) + 255) / 256 * 256;
-}
-size_t tree_umma_workspace(int64_t pairs, int32_t tree_tokens, int32_t group, int32_t head_dim)
-{
-    if (group > kTreeTile) return 0;
-    const TreeRows r = tree_rows(tree_tokens, group, head_dim);
-    return tree_partials_bytes(r, head_dim) + ((size_t)pairs * r.row_blocks * sizeof(int2) + 255) / 256 * 256 + 256;
+    TreeCut c;
+    c.items = pairs * r.row_blocks;
+    c.most_tiles = c.items * (ceil_div(max_seq_len, kTreeTile) + kTreeItemCost);
+    c.grid = (unsigned)(c.most_tiles < sm_count() ? c.most_tiles : sm_count());
+    c.draws = c.most_tiles >= (int64_t)kTreeDrawnTiles * c.grid;
+    const size_t pieces = (size_t)c.grid * (1 + (c.draws ? r.short_pieces : 0)) + 1;
+    c.slot_rows = 2 * pieces * r.item_rows;
+    c.partials_bytes = (c.slot_rows * (head_dim + 1) * sizeof(float) + 255) / 256 * 256;
+    c.ticket_offset = c.partials_bytes + ((size_t)c.items * sizeof(int2) + 255) / 256 * 256;
+    c.bytes = c.ticket_offset + 256;
+    return c;
 }
 
 // Blocks of 16, 32 or 64 tokens, or of a multiple of 128: no tile straddles blocks of another kind.  Head size 64 with at
@@ -127,32 +137,30 @@ int instinfer_decode_attention_tree(void *out, float *lse, const void *q, const 
     // driver without the encoder, takes the warp-level one).
     if (g_grouped_path != 1 && tree_umma_shape(head_dim, p.rows, p.group, paged, block_tokens)) {
         const TreeRows rows = tree_rows(tree_tokens, p.group, head_dim);
-        const int64_t items = pairs * rows.row_blocks;
+        const TreeCut cut = tree_cut(rows, pairs, max_seq_len, head_dim);
         const int row_parts = (rows.item_rows + kTreeMergeRows - 1) / kTreeMergeRows;
         const int32_t box = paged && block_tokens < kTreeTile ? block_tokens : kTreeTile;
         TreeLaunch t = {};
-        if (items * row_parts < (int64_t)1 << 31 && (int64_t)tree_tokens * q_heads * head_dim < (int64_t)1 << 31 && items * (ceil_div(max_seq_len, kTreeTile) + kTreeItemCost) < (int64_t)1 << 31 &&
+        if (cut.items * row_parts < (int64_t)1 << 31 && (int64_t)tree_tokens * q_heads * head_dim < (int64_t)1 << 31 && cut.most_tiles < (int64_t)1 << 31 &&
             make_query_map(&t.map_q, q, batch, tree_tokens, q_heads, p.group, head_dim, rows.nodes_per_block) &&
             make_cache_map(&t.map_k, k_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box) &&
             make_cache_map(&t.map_v, v_cache, p.a.kv_bytes / (2 * head_dim), head_dim, box)) {
             t.p.a = p.a;
-            t.p.a.part_lse = p.a.part_o + tree_slot_rows(rows) * head_dim;
+            t.p.a.part_lse = p.a.part_o + cut.slot_rows * head_dim;
             t.p.short_pieces = rows.short_pieces;
-            unsigned char *behind = static_cast<unsigned char *>(workspace) + tree_partials_bytes(rows, head_dim);
-            t.p.item_pieces = reinterpret_cast<int2 *>(behind);
-            t.p.ticket = reinterpret_cast<unsigned *>(static_cast<unsigned char *>(workspace) +
-                                                      tree_umma_workspace(pairs, tree_tokens, p.group, head_dim) - 256);
+            unsigned char *start = static_cast<unsigned char *>(workspace);
+            t.p.item_pieces = reinterpret_cast<int2 *>(start + cut.partials_bytes);
+            t.p.ticket = reinterpret_cast<unsigned *>(start + cut.ticket_offset);
             t.p.tree = p.tree;
             t.p.batch = batch;
             t.p.group = p.group;
             t.p.nodes_per_block = rows.nodes_per_block;
             t.p.row_blocks = rows.row_blocks;
             t.p.item_rows = rows.item_rows;
-            const int64_t most_tiles = items * (ceil_div(max_seq_len, kTreeTile) + kTreeItemCost);
-            t.grid = (unsigned)(most_tiles < sm_count() ? most_tiles : sm_count());
-            t.merge_grid = (unsigned)(items * row_parts);
+            t.grid = cut.grid;
+            t.merge_grid = (unsigned)(cut.items * row_parts);
             t.row_parts = row_parts;
-            t.draws = most_tiles >= (int64_t)kTreeDrawnTiles * t.grid;
+            t.draws = cut.draws;
             t.stream = stream;
             switch (head_dim) {
             case 64: return paged ? launch_tree<64, true>(rows, t) : launch_tree<64, false>(rows, t);
@@ -177,7 +185,8 @@ size_t instinfer_tree_workspace_bytes(int32_t batch, int32_t tree_tokens, int32_
     const int32_t rows = q_heads / kv_heads * tree_tokens, groups = (rows + kGroupRows - 1) / kGroupRows;
     // enough for either implementation: which one runs also depends on the cache layout
     const size_t warp_level = grouped_workspace_for(pairs, rows, head_dim, make_plan(pairs * groups, max_seq_len, tree_rules(head_dim)));
-    const size_t umma = tree_umma_workspace(pairs, tree_tokens, q_heads / kv_heads, head_dim);
+    const int32_t group = q_heads / kv_heads;
+    const size_t umma = group <= kTreeTile ? tree_cut(tree_rows(tree_tokens, group, head_dim), pairs, max_seq_len, head_dim).bytes : 0;
     return warp_level > umma ? warp_level : umma;
 }
 
