@@ -118,12 +118,6 @@ struct TreePieces {
         if (step == 0) return c < blocks ? total / blocks * c + min(c, total % blocks) : total;
         return c <= blocks ? length * c : min(total, drawn + (c - blocks) * step);
     }
-    __device__ __forceinline__ int piece_of(int tile) const
-    {
-        if (step > 0) return tile < drawn ? tile / length : blocks + (tile - drawn) / step;
-        const int share = total / blocks, longer = total % blocks;
-        return tile < longer * (share + 1) ? tile / (share + 1) : longer + (tile - longer * (share + 1)) / share;
-    }
 };
 
 // Tiles [t0, t1) of the n_tiles of one item; b < 0: no more.  `slot`: where its partial result goes: what starts
@@ -614,27 +608,28 @@ struct TreeCopies {
     }
 };
 
-// What row `r` of a segment's first row block (of the only one, for the kernel with the tokens as the long side)
-// or `row` sees of the value rows that were taken out of its tiles (rare): weights against the row's
-// log-sum-exp.  Adds dims d0 .. d0 + 31 to o, or returns dim d.
-__device__ __forceinline__ float tree_stray_weight(const AttnParams &a, const TreeSegment &s, int64_t out_row, int64_t kv_row, int D, float lse2)
+// Value rows that were taken out of their tiles (rare), given back to the rows that see them.
+// The weight of cache row kv_row for query row out_row, against that row's log-sum-exp.
+__device__ __forceinline__ float tree_stray_weight(const AttnParams &a, int64_t out_row, int64_t kv_row, int D, float lse2)
 {
     float dot = 0.f;
     #pragma unroll 1
     for (int c = 0; c < D; ++c) dot = fmaf(__half2float(a.q[out_row * D + c]), __half2float(a.k[kv_row * D + c]), dot);
     return fast_exp2(dot * a.scale_log2e - lse2);
 }
+// Adds what `row` sees of them to its dims d0 .. d0 + 31 in o.
 static __device__ __noinline__ void tree_add_poisoned(const AttnParams &a, const TreeSegment &s, const TreeRow &row, const unsigned *poison,
                                                int64_t out_row, int D, int d0, float lse2, float *o)
 {
     for (int n = 0; n < s.nodes; ++n) {
         if (!(poison[n >> 5] >> (n & 31) & 1u) || !row.sees(n)) continue;
         const int64_t kv_row = tree_cache_row(a, s.b, s.hk, s.prefix() + n);
-        const float weight = tree_stray_weight(a, s, out_row, kv_row, D, lse2);
+        const float weight = tree_stray_weight(a, out_row, kv_row, D, lse2);
 #pragma unroll 1
         for (int c = 0; c < 32; ++c) o[c] += weight * __half2float(a.v[kv_row * D + d0 + c]);
     }
 }
+// Dim d of what row r of a segment's only row block sees of them (the kernel with the tokens as the long side).
 static __device__ __noinline__ float tree_poisoned_value(const TreeParams &p, const TreeSegment &s, const unsigned *poison, int r, int D, int d,
                                                   float lse2)
 {
@@ -646,7 +641,7 @@ static __device__ __noinline__ float tree_poisoned_value(const TreeParams &p, co
     for (int n = 0; n < s.nodes; ++n) {
         if (!(poison[n >> 5] >> (n & 31) & 1u) || !row.sees(n)) continue;
         const int64_t kv_row = tree_cache_row(a, s.b, s.hk, s.prefix() + n);
-        value += tree_stray_weight(a, s, out_row, kv_row, D, lse2) * __half2float(a.v[kv_row * D + d]);
+        value += tree_stray_weight(a, out_row, kv_row, D, lse2) * __half2float(a.v[kv_row * D + d]);
     }
     return value;
 }
