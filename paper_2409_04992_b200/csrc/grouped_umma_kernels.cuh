@@ -437,6 +437,7 @@ grouped_attn_umma_kernel(const GroupedParams p, unsigned *ticket, const __grid_c
                     }
                     fence_async_proxy();
                 }
+                __syncwarp();                                // (where no copy is left to wait for, the arrival alone completes the item)
                 if (lane == 0) mbarrier_expect_bytes(bar, fetched * (unsigned)(T * 128 * kItemPanels));
                 __syncwarp();
                 if (good) {

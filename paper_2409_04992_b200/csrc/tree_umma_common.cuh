@@ -430,6 +430,7 @@ struct TreeCopies {
                 }
                 fence_async_proxy();
             }
+            __syncwarp();                                // (where no copy is left to wait for, the arrival alone completes the item)
             if (lane == 0) mbarrier_expect_bytes(bar, fetched * (unsigned)(T * 128 * Ring::kItemPanels));
             __syncwarp();
             if (good) {
