@@ -112,6 +112,8 @@ enum class Rows { kContiguous, kPaged, kGathered };
 // Programmatic dependent launch: a kernel first lets the next kernel in the stream start
 // being scheduled, then waits until the kernels before it have completed and their writes
 // are visible.  Both are no-ops for a launch without the attribute.
+// (What an earlier kernel of the stream may have written -- lengths, tables, lists -- is read by ordinary loads: this kernel
+// may have started before that one ended, and read-only (.nc) loads are for data that no one writes while a kernel runs.)
 __device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void wait_for_previous_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -444,7 +446,7 @@ decode_attn_split_kernel(const AttnParams p)
     int rows_now = 0, rows_next = 0;
     auto load_rows = [&](int tile_base) -> int {
         const int idx = begin + (warp + (tile_base + (lane >> 3)) * kWarps) * kTileRows + (lane & 7);
-        return idx < end ? __ldg(row_list + idx) : 0;
+        return idx < end ? row_list[idx] : 0;
     };
     if (kGathered) {
         if (my_tiles > 0) {
@@ -468,7 +470,7 @@ decode_attn_split_kernel(const AttnParams p)
     auto load_window = [&](int base) -> int {
         const int idx = base + lane;
         if (idx >= blocks_needed || !bounds_ok(idx < p.max_blocks_per_seq, p.status)) return 0;
-        return __ldg(table_row + idx);
+        return table_row[idx];
     };
     if (kPaged && my_tiles > 0) {
         window_now = load_window(win_base);

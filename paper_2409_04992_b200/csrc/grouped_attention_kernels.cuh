@@ -351,7 +351,7 @@ grouped_attn_split_kernel(const GroupedParams p)
         step_rem = kStepTokens - step_blk * tokens;
         block_stride = (int64_t)a.heads * tokens * G::kRowBytes;
         head_off = (int64_t)hk * tokens * G::kRowBytes;
-        next_phys = my_tiles > 0 && bounds_ok(blk < a.max_blocks_per_seq, a.status) ? __ldg(table_row + blk) : 0;
+        next_phys = my_tiles > 0 && bounds_ok(blk < a.max_blocks_per_seq, a.status) ? table_row[blk] : 0;
     } else {
         src_off = ((int64_t)pair * a.s_max + first_token) * G::kRowBytes;
     }
@@ -375,7 +375,7 @@ grouped_attn_split_kernel(const GroupedParams p)
                     ++blk;
                 }
                 if (issue_j + 1 < my_tiles)
-                    next_phys = bounds_ok(blk < a.max_blocks_per_seq, a.status) ? __ldg(table_row + blk) : -1;
+                    next_phys = bounds_ok(blk < a.max_blocks_per_seq, a.status) ? table_row[blk] : -1;
             } else {
                 off = src_off;
                 src_off += (int64_t)kStepTokens * G::kRowBytes;

@@ -400,7 +400,7 @@ grouped_attn_umma_kernel(const GroupedParams p, unsigned *ticket, const __grid_c
             const int nb = (min(c.end - tile_start, kUmmaTile) + T - 1) / T;
             const int idx = (tile_start + lane * T) / a.block_tokens;
             if (j >= c.n_tiles || lane >= nb || !bounds_ok(idx < a.max_blocks_per_seq, a.status)) return -1;
-            return __ldg(table_row + idx);
+            return table_row[idx];
         };
         int ids_next = fetch_ids(0);
         for (int j = 0; j < c.n_tiles; ++j) {
@@ -473,7 +473,7 @@ grouped_attn_umma_kernel(const GroupedParams p, unsigned *ticket, const __grid_c
             int len = 0;
             if (w < total) {
                 const int b = (w % a.pairs) / a.heads;
-                asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(len) : "l"(a.seq_lens + b) : "memory");
+                asm volatile("ld.global.b32 %0, [%1];" : "=r"(len) : "l"(a.seq_lens + b) : "memory");
             }
             return len;
         };

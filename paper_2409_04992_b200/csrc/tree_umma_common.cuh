@@ -389,7 +389,7 @@ struct TreeCopies {
         if (j >= s.t1 || lane >= (min(s.len - start, kTreeTile) + T - 1) / T) return -1;
         const int idx = (start + lane * T) / p.a.block_tokens;
         if (!bounds_ok(idx < p.a.max_blocks_per_seq, p.a.status)) return -1;
-        return __ldg(p.a.block_table + (int64_t)s.b * p.a.max_blocks_per_seq + idx);
+        return p.a.block_table[(int64_t)s.b * p.a.max_blocks_per_seq + idx];
     }
     // One tile of one cache (all lanes); false if a wait ran out.
     template <bool kIsV>

@@ -105,7 +105,7 @@ struct RowReader {
     __device__ __forceinline__ uint4 raw(int g) const
     {
         const int first = g * kVec - shift;
-        if (first >= 0 && first + kVec <= vocab) return __ldg(reinterpret_cast<const uint4 *>(row + first));
+        if (first >= 0 && first + kVec <= vocab) return *reinterpret_cast<const uint4 *>(row + first);
         uint4 some = make_uint4(0u, 0u, 0u, 0u);
         E *e = reinterpret_cast<E *>(&some);
 #pragma unroll
