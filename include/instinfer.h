@@ -265,7 +265,8 @@ size_t instinfer_grouped_workspace_bytes(int32_t batch, int32_t q_tokens, int32_
  * seq_lens[b] - tree_lens[b] + j (append them with instinfer_kv_append_bulk); seq_lens[b] counts
  * them.  One step is: make room (instinfer_kv_resize), append, instinfer_tree_mask once, in every
  * layer instinfer_decode_attention_tree, then instinfer_verify_tree, instinfer_kv_keep_path, and
- * instinfer_kv_resize to the kept length.
+ * instinfer_kv_resize to the kept length.  On a paged cache the step needs blocks of a multiple of 16
+ * tokens, which the attention asks for (the other calls take multiples of 8).
  * Limit (INSTINFER_ERR_UNSUPPORTED otherwise): tree_tokens <= INSTINFER_MAX_TREE_TOKENS.
  */
 #define INSTINFER_MAX_TREE_TOKENS 128
@@ -295,7 +296,7 @@ int instinfer_tree_mask(uint64_t *tree_mask, const int32_t *parents, const int32
  * seq_lens[b] == 0 are zero with lse = -inf.  A tree_lens[b] out of range or above seq_lens[b] is
  * flagged (INSTINFER_FLAG_TREE_RANGE) and makes the sequence inactive.  What a row does not see
  * never influences it, infinities and NaN in hidden nodes' keys and values included; a NaN that
- * it sees makes the row NaN.
+ * it sees makes the row NaN, an infinity in the rows before the tree makes it infinite or NaN.
  * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): head_dim in {64, 128, 256}; paged block_tokens a
  * multiple of 16; (q_heads / kv_heads) * tree_tokens <= INSTINFER_MAX_TREE_ROWS.
  */
@@ -322,8 +323,10 @@ size_t instinfer_tree_workspace_bytes(int32_t batch, int32_t tree_tokens, int32_
  *     uniforms[b][c] * q_v(token_c) * Z < w(token_c),
  * and the walk goes on at c; otherwise w <- max(w - Z q_v, 0) and Z <- sum w (if that sum is 0, w
  * and Z stay as they were).  When no child is taken the next token is the lowest i with
- * w_0 + ... + w_i > uniforms[b][0] * sum w.  If v's children were drawn independently from q_v the
- * emitted tokens have the target's distribution.  Computed in 64 bits.
+ * w_0 + ... + w_i > uniforms[b][0] * sum w.  Computed in 64 bits.  If v's children were drawn
+ * independently from q_v and the rows of p and q sum to 1, the emitted tokens have the target's
+ * distribution; as nothing is normalised here, it holds up to what the rows' sums are off by (bf16 and
+ * fp16 rows: their rounding).
  *   path        int32 [batch, tree_tokens]: the nodes taken, ascending, the root first; -1 behind
  *   path_lens   int32 [batch]: how many, 0 for a sequence without a tree
  *   out_tokens  int32 [batch, tree_tokens]: the tokens of path[1 ..], then the next token; -1 behind
@@ -420,7 +423,8 @@ size_t instinfer_kv_resize_workspace_bytes(int32_t batch, int64_t num_phys_block
  * new_block_refs [num_phys_blocks] (which may be block_table and block_refs themselves; entries
  * behind a sequence's last block are copied as they are), *blocks_used = U (device).  Blocks from U
  * on are free afterwards.  A listed block that counts as free is nobody's, and another one may be moved
- * over it: its entries are copied as they are and flagged INSTINFER_FLAG_POOL.
+ * over it: its entries are copied as they are and flagged INSTINFER_FLAG_POOL.  With batch == 0 nothing
+ * is enqueued, as everywhere, and nothing is written.
  *   workspace  at least instinfer_kv_defragment_workspace_bytes(num_phys_blocks) bytes
  */
 int instinfer_kv_defragment(void *const *k_pools, void *const *v_pools, int32_t n_layers,

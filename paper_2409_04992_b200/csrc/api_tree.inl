@@ -55,8 +55,12 @@ TreeCut tree_cut(const TreeRows &r, int64_t pairs, int32_t max_seq_len, int32_t 
 }
 
 // Blocks of 16, 32 or 64 tokens, or of a multiple of 128: no tile straddles blocks of another kind.  Head size 64 with at
-// most 16 rows is left to the warp-level form: a tile has half the bytes for the same work per token there
-// (16 x 40 heads x 8k-16k, 16 rows: 450 us against 329; one short sequence: 15 against 11; 20 rows: 485 against 513).
+// most 16 rows is left to the warp-level form: a tile has half the bytes for the same work per token there (16 x 40
+// heads x 8k-16k, 16 rows: 450 us, when tcgen05 had an instance for them, against 331 in short runs and 354 sustained;
+// 20 rows 473 and 473 against 468 and 559; 32 rows 476 and 483 against 492 and 581; 64 rows 581 and 627 against 937
+// and 1077).  The number of tiles does not enter: head size 128, 8 rows, 40 heads, tcgen05 against warp-level: 1
+// sequence x 1k 18.1 us against 21.6, x 4k 22.8 against 31.4; 4 x 1k 27.2 against 36.6, x 4k 72.4 against 83.2; 16 x 1k
+// 81.9 against 79.6, x 4k 212 against 234; head size 256, 1 x 16 heads x 1k 21.1 against 31.8.
 bool tree_umma_shape(int32_t head_dim, int32_t rows, int32_t group, bool paged, int32_t block_tokens)
 {
     return group <= kTreeTile && !(head_dim == 64 && rows <= 16) && (!paged || block_tokens == 16 || block_tokens == 32 || block_tokens == 64 || block_tokens % kTreeTile == 0);

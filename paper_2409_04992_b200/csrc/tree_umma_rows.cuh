@@ -17,10 +17,12 @@
 // waited for the MMAs that use the weights and for those of the next logits, 2700 of 6100 cycles a tile.
 // (Leaving the low parts out in this form gave another 11 % and 1.4 times the error.)
 //
-// Measured: 256 rows (32 nodes x 8 heads) over 8 x 32k tokens of 8 KV heads, head size 128: 460 us, 466 TFLOP/s of the
-// two products counted once (the low parts' MMAs come on top: the tensor pipe is active 55 % of the time, the
-// exponentials' pipe 38 %); 512 rows 739 TFLOP/s.  What bounds it is the chain logits -> softmax -> weights of a unit,
-// of which a block has two (or four half) in flight.
+// Measured, over 8 x 32k tokens of 8 KV heads, head size 128, the two products counted once (the low parts' MMAs come
+// on top): 256 rows (32 nodes x 8 heads) 389 us, 707 TFLOP/s, in short runs and 447 us, 615, sustained; 512 rows 744
+// us, 739 TFLOP/s, and 844 us, 651.  Trees of 16 to 32 nodes on the 256 rows 461 us.  The tensor pipe is active 55 % of
+// the time, the exponentials' pipe 38 %: what bounds it is the chain logits -> softmax -> weights of a unit, of which a
+// block has two (or four half) in flight.  Fewer rows over 16 x 40 heads x 4k to 8k: 80 rows 469 us (542 sustained),
+// 128 rows 494 (566); memory alone would take 316.
 #pragma once
 
 #include "tree_umma_common.cuh"

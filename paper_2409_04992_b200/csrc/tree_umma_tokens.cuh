@@ -17,9 +17,9 @@
 // its own share of the rows' sums.
 //
 // Measured (K and V bytes per second, 16 sequences of 4k to 8k tokens, 40 KV heads, head size 128, 32-token blocks,
-// with the merge): 8 rows 6.23 TB/s, 16 rows 6.16, 32 rows 5.91 (memory is the bound), 64 rows 5.35 in short runs and
-// 4.65 sustained, where the exponentials and the MMAs' power (the clock falls to 1.5 GHz) weigh as much as memory.
-// Head size 256: 16 rows 6.24, 64 rows 5.56.
+// with the merge; short runs of ten calls, sustained ones in brackets): 8 rows 6.3 TB/s (6.3), 16 rows 6.2 (6.2), 32
+// rows 6.0 (5.8; memory is the bound), 64 rows 5.5 (4.9), where the exponentials and the MMAs' power (the clock falls to
+// 1.5 GHz) weigh as much as memory.  Head size 256, 20 heads: 16 rows 6.3 (6.2), 64 rows 5.7 (5.2).
 #pragma once
 
 #include "tree_umma_common.cuh"
