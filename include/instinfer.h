@@ -238,7 +238,8 @@ size_t instinfer_allgather_workspace_bytes(int32_t batch, int32_t heads, int32_t
  * lse = -inf.  With q_tokens = 1 and q_heads = kv_heads the result is that of the entry points
  * above within the same tolerance (not bit for bit: the contractions run on the tensor cores).
  * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): (q_heads / kv_heads) * q_tokens <= 16;
- * head_dim in {64, 128, 256}; paged block_tokens a multiple of 16.
+ * head_dim in {64, 128, 256}; paged block_tokens a multiple of 16.  Scaled logits from some 9e7 on (2^27 to
+ * the base 2) may overflow the weights, to NaN; instinfer_decode_attention_tree has no such limit.
  *   workspace at least instinfer_grouped_workspace_bytes(...) bytes.
  */
 int instinfer_decode_attention_grouped(void *out, float *lse, const void *q, const void *k_cache,
