@@ -66,6 +66,11 @@ typedef enum {
     INSTINFER_ERR_CUDA = 4           /* the CUDA runtime refused a launch                        */
 } instinfer_status;
 
+/* Element types, where a call takes more than fp16. */
+#define INSTINFER_F32 0
+#define INSTINFER_F16 1
+#define INSTINFER_BF16 2
+
 /* Bits OR-ed into *status_flags by the kernels. */
 #define INSTINFER_FLAG_SEQ_LEN_RANGE 1  /* seq_lens[b] < 0, beyond the cache capacity, or beyond max_seq_len */
 #define INSTINFER_FLAG_BLOCK_RANGE   2  /* a block_table entry that had to be read lies outside [0, num_phys_blocks) */
@@ -256,6 +261,118 @@ size_t instinfer_grouped_workspace_bytes(int32_t batch, int32_t q_tokens, int32_
                                          int32_t kv_heads, int32_t head_dim, int32_t max_seq_len);
 
 /*
+ * ---- Rotary positions on the way into the cache ----
+ * (No counterpart in the paper, whose models have learned positions.)  Queries and keys of models with rotary
+ * positions are turned by their position before they are used: with pairs (a_i, b_i) of a head's first rope_dim dims,
+ *     (a_i, b_i) -> magnitude * (a_i cos t - b_i sin t, a_i sin t + b_i cos t),  t = position * frequencies[i],
+ * i < rope_dim / 2; pair i is dims (i, rope_dim / 2 + i) (halves), or (2 i, 2 i + 1) (interleaved != 0).  The other dims stay.
+ * The angle is computed in 64 bits (so that far positions keep their fast pairs), the turn in 32, rounded once.
+ *
+ * instinfer_rope_frequencies: the pairs' frequencies and the magnitude, HOST memory, host computation only.
+ *   plain     f_i = base^(-2 i / rope_dim), magnitude 1
+ *   linear    f_i / factor, magnitude 1 (positions squeezed into the trained range)
+ *   by parts  for a context stretched `factor` times beyond trained_len: pairs that turn at least fast_turns times over
+ *             trained_len tokens keep f_i, those that turn at most slow_turns times get f_i / factor, between them linearly
+ *             (in the number of turns); magnitude 0.1 ln(factor) + 1
+ * factor >= 1; trained_len > 0 and 0 <= slow_turns < fast_turns are looked at for "by parts" only.
+ * rope_dim even; an unknown scaling: INSTINFER_ERR_UNSUPPORTED.
+ */
+#define INSTINFER_ROPE_PLAIN 0
+#define INSTINFER_ROPE_LINEAR 1
+#define INSTINFER_ROPE_BY_PARTS 2
+int instinfer_rope_frequencies(double *frequencies, float *magnitude, int32_t rope_dim, double base,
+                               int32_t scaling, double factor, int32_t trained_len, double slow_turns,
+                               double fast_turns);
+
+/*
+ * What instinfer_kv_append_bulk does, with the keys turned on the way, and the queries turned in the same pass.
+ * Sequence b receives new_lens[b] tokens (new_lens == NULL: max_new tokens each, none for a sequence of length 0) at
+ * logical positions seq_lens[b] - new_lens[b] .. seq_lens[b] - 1 of the cache.
+ *   q_out      fp16 [batch, max_new, q_heads, head_dim], turned (what the attention calls take); rows of tokens that there
+ *              are not stay as they were.  May be q itself where type is fp16 and q_stride = q_heads * head_dim.
+ *   q, k_new, v_new  `type` (INSTINFER_F32, _F16 or _BF16), token (b, t) at (b * max_new + t) * stride elements, its heads
+ *              one after the other (so all three may be slices of one projection's output).  Strides are multiples of
+ *              16 bytes.  q_heads == 0: q and q_out are not looked at.
+ *   frequencies  fp64 [rope_dim / 2], DEVICE, radians per position; 8-byte aligned
+ *   positions  nullable int32 [batch, max_new]: the positions to turn by (any value; a draft tree's nodes, say, whose
+ *              depth is not their place in the cache).  NULL: the logical positions in the cache.
+ * fp32 and bf16 values are rounded to fp16 once (values beyond its range become infinities); fp16 values and keys' other dims are
+ * bit copies.  Layout selection and the other arguments as in instinfer_kv_append_bulk.  A sequence whose lengths are out of
+ * range is skipped and flagged; a token whose block is out of range is flagged, its K and V rows are not written.
+ * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): head_dim in {64, 128, 256}, rope_dim a multiple of 16.
+ */
+int instinfer_rope_append(void *q_out, void *k_cache, void *v_cache, const void *q, const void *k_new,
+                          const void *v_new, int32_t type, int64_t q_stride, int64_t k_stride,
+                          int64_t v_stride, const double *frequencies, int32_t rope_dim,
+                          int32_t interleaved, float magnitude, const int32_t *positions,
+                          const int32_t *seq_lens, const int32_t *new_lens, const int32_t *block_table,
+                          int32_t max_blocks_per_seq, int32_t block_tokens, int64_t num_phys_blocks,
+                          int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads,
+                          int32_t head_dim, int32_t s_max, int32_t *status_flags, void *cuda_stream);
+
+/*
+ * ---- A cache of one latent vector a token ----
+ * (No counterpart in the paper, whose models have keys and values for every head.)  Models with latent attention cache one
+ * vector of latent_dim values a token, from which the keys and values of all heads are made, and a key part of rope_dim
+ * dims with rotary position that all heads share.  In decoding the matrices that make them are absorbed by the queries
+ * and the outputs, so that a head's query is a vector of latent_dim + rope_dim values, the cache row is every head's key,
+ * and its first latent_dim values are every head's value:
+ *     out[r] = softmax_i(scale * q[r] . row_i) . row_i[0 .. latent_dim)
+ * Layouts: contiguous [batch, s_max, latent_dim + rope_dim], or a pool [num_phys_blocks, block_tokens, latent_dim + rope_dim]
+ * with a block table; fp16 or bf16 (`type`, the same for every tensor of a call but lse).
+ * The calls that share, grow and move whole blocks (instinfer_kv_fork, instinfer_kv_resize, instinfer_kv_defragment) take such pools
+ * as pools of (latent_dim + rope_dim) / 64 heads of 64, half of the layers as K and half as V pools (same block bytes).
+ * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): latent_dim 256 or 512, rope_dim 64; paged block_tokens a multiple of 8.
+ *
+ * instinfer_latent_append: the new tokens' rows, with the key part turned, and the queries' turned parts.
+ *   q_out      [batch, max_new, q_heads, latent_dim + rope_dim], the absorbed queries: the last rope_dim values of the rows of
+ *              tokens that there are get written, nothing else
+ *   q_rope     the queries' parts to turn, token (b, t) and head h at (b * max_new + t) * q_stride + h * q_head_stride elements
+ *   latent_new, rope_new  token (b, t) at (b * max_new + t) * stride elements; strides are multiples of 16 bytes
+ * frequencies [rope_dim / 2] and all else as in instinfer_rope_append.
+ */
+int instinfer_latent_append(void *q_out, void *cache, const void *q_rope, const void *latent_new,
+                            const void *rope_new, int32_t type, int64_t q_stride, int64_t q_head_stride,
+                            int64_t latent_stride, int64_t rope_stride, const double *frequencies,
+                            int32_t interleaved, float magnitude, const int32_t *positions,
+                            const int32_t *seq_lens, const int32_t *new_lens, const int32_t *block_table,
+                            int32_t max_blocks_per_seq, int32_t block_tokens, int64_t num_phys_blocks,
+                            int32_t batch, int32_t max_new, int32_t q_heads, int32_t latent_dim,
+                            int32_t rope_dim, int32_t s_max, int32_t *status_flags, void *cuda_stream);
+
+/*
+ * Decode attention over a latent cache, for one new token, several, or a draft tree (see below).
+ *   q          [batch, q_tokens, q_heads, latent_dim + rope_dim], absorbed queries with their parts turned
+ *   out        [batch, q_tokens, q_heads, latent_dim]; fp32 accumulation, rounded once
+ *   lse        nullable fp32 [batch, q_tokens, q_heads]
+ *   tree_lens  nullable int32 [batch]: how many of the q_tokens new tokens there are (NULL: all); they are the last
+ *              tree_lens[b] positions of the sequence, and the caches hold them
+ *   tree_mask  NULL: new token t attends to the positions up to its own.  Else as instinfer_tree_mask writes it, 16-byte
+ *              aligned: to every position before the new ones and to the new ones whose bits its row has.
+ *   workspace  at least instinfer_latent_workspace_bytes(...) bytes
+ * Rows of new tokens that there are not, rows that see nothing, and all rows of a sequence with seq_lens[b] == 0 are zero
+ * with lse = -inf.  A tree_lens[b] out of range or above seq_lens[b] is flagged (INSTINFER_FLAG_TREE_RANGE) and makes the
+ * sequence inactive.  What a row does not see never influences it, infinities and NaN in hidden new tokens' rows
+ * included; a row that sees a value that is not finite becomes NaN, or, where its logit is -infinity, leaves that
+ * token out if it is a new one.  Block-table entries out of range count as rows of zeros (flagged).
+ * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): q_tokens <= INSTINFER_MAX_TREE_TOKENS, q_tokens * q_heads <=
+ * INSTINFER_MAX_LATENT_ROWS, caches of fewer than 2^31 rows.
+ */
+#define INSTINFER_MAX_LATENT_ROWS 16384
+int instinfer_decode_attention_latent(void *out, float *lse, const void *q, const void *cache,
+                                      const int32_t *block_table, const int32_t *seq_lens,
+                                      const int32_t *tree_lens, const uint64_t *tree_mask, int32_t type,
+                                      int32_t batch, int32_t q_tokens, int32_t q_heads,
+                                      int32_t latent_dim, int32_t rope_dim, int32_t s_max,
+                                      int32_t block_tokens, int32_t max_blocks_per_seq,
+                                      int64_t num_phys_blocks, int32_t max_seq_len, float scale,
+                                      void *workspace, size_t workspace_bytes, int32_t *status_flags,
+                                      void *cuda_stream);
+
+size_t instinfer_latent_workspace_bytes(int32_t batch, int32_t q_tokens, int32_t q_heads,
+                                        int32_t latent_dim, int32_t rope_dim, int32_t max_seq_len);
+
+/*
  * ---- Speculative decoding: several drafted tokens per sequence and step ----
  * (No counterpart in the paper, whose decode phase adds one token per step, Sec. II-B; the work
  * stays its Logit / Attend operators, Sec. III-B, over the same cache.)
@@ -341,9 +458,6 @@ size_t instinfer_tree_workspace_bytes(int32_t batch, int32_t tree_tokens, int32_
  *   uniforms    fp32 [batch, tree_tokens] in [0, 1)
  * If w has no positive value the next token is -1, flagged.
  */
-#define INSTINFER_F32 0
-#define INSTINFER_F16 1
-#define INSTINFER_BF16 2
 int instinfer_verify_tree(int32_t *path, int32_t *path_lens, int32_t *out_tokens,
                           const void *target_probs, const void *draft_probs, int32_t probs_type,
                           int64_t row_stride, const int32_t *tokens, const int32_t *parents,

@@ -10,7 +10,7 @@ import array
 import ctypes
 import os
 from pathlib import Path
-from typing import Optional, Sequence, Union
+from typing import Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -20,7 +20,8 @@ LIBRARY = Path(os.environ.get("INSTINFER_LIBRARY") or Path(__file__).resolve().p
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA = range(5)
 FLAG_SEQ_LEN_RANGE, FLAG_BLOCK_RANGE, FLAG_COPY_TIMEOUT, FLAG_BOUNDS_CHECK = 1, 2, 4, 8
 FLAG_TREE_RANGE, FLAG_POOL = 16, 32
-MAX_TREE_TOKENS, MAX_TREE_ROWS, MAX_LAYERS = 128, 4096, 128
+MAX_TREE_TOKENS, MAX_TREE_ROWS, MAX_LAYERS, MAX_LATENT_ROWS = 128, 4096, 128, 16384
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "by_parts": 2}
 STATIC_WORKSPACE_BYTES = 16 << 20
 
 _lib: Optional[ctypes.CDLL] = None
@@ -97,6 +98,20 @@ def load() -> ctypes.CDLL:
                                                 i32, i32, i32, ptr, sz, ptr, ptr]
         lib.instinfer_kv_defragment_workspace_bytes.restype = sz
         lib.instinfer_kv_defragment_workspace_bytes.argtypes = [i64]
+        f64 = ctypes.c_double
+        lib.instinfer_rope_frequencies.restype = ctypes.c_int
+        lib.instinfer_rope_frequencies.argtypes = [ptr, ptr, i32, f64, i32, f64, i32, f64, f64]
+        lib.instinfer_rope_append.restype = ctypes.c_int
+        lib.instinfer_rope_append.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, i32, i64, i64, i64, ptr, i32, i32, f32, ptr, ptr, ptr, ptr,
+                                              i32, i32, i64, i32, i32, i32, i32, i32, i32, ptr, ptr]
+        lib.instinfer_latent_append.restype = ctypes.c_int
+        lib.instinfer_latent_append.argtypes = [ptr, ptr, ptr, ptr, ptr, i32, i64, i64, i64, i64, ptr, i32, f32, ptr, ptr, ptr, ptr,
+                                                i32, i32, i64, i32, i32, i32, i32, i32, i32, ptr, ptr]
+        lib.instinfer_decode_attention_latent.restype = ctypes.c_int
+        lib.instinfer_decode_attention_latent.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, i32, i32, i32, i32, i32, i32, i32,
+                                                          i32, i32, i64, i32, f32, ptr, sz, ptr, ptr]
+        lib.instinfer_latent_workspace_bytes.restype = sz
+        lib.instinfer_latent_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
         lib.instinfer_decode_step_host.restype = ctypes.c_int
         lib.instinfer_decode_step_host.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr,
                                                    i32, i32, i64, i32, i32, i32, i32, i32, f32,
@@ -342,6 +357,153 @@ def decode_attention_grouped(out: torch.Tensor, lse: Optional[torch.Tensor], q: 
         workspace.numel() * workspace.element_size(), _ptr(status_flags), _stream(stream)))
 
 
+def rope_frequencies(rope_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, trained_len: int = 0,
+                     slow_turns: float = 1.0, fast_turns: float = 32.0,
+                     device: torch.device | str = "cuda") -> Tuple[torch.Tensor, float]:
+    """instinfer_rope_frequencies: the pairs' frequencies, fp64 [rope_dim / 2] on `device`, and the magnitude.
+    scaling: "plain", "linear" or "by_parts"."""
+    if scaling not in ROPE_SCALINGS:
+        raise InstInferError(ERR_UNSUPPORTED)
+    pairs = (ctypes.c_double * max(1, rope_dim // 2))()
+    magnitude = ctypes.c_float()
+    _check(load().instinfer_rope_frequencies(pairs, ctypes.byref(magnitude), int(rope_dim), float(base), ROPE_SCALINGS[scaling],
+                                             float(factor), int(trained_len), float(slow_turns), float(fast_turns)))
+    return torch.tensor(list(pairs), dtype=torch.float64, device=device), magnitude.value
+
+
+def _token_stride(t: torch.Tensor) -> int:
+    """Elements from one token of t [B, N, ...] to the next, all B * N of them evenly spaced."""
+    B, N = t.shape[:2]
+    if B == 1 and N == 1:
+        return 1 << 32                 # (never taken: any stride that the library accepts will do)
+    stride = t.stride(1) if N > 1 else t.stride(0)
+    if B > 1 and N > 1 and t.stride(0) != N * stride:
+        raise InstInferError(ERR_INVALID_ARG)
+    return stride
+
+
+def _cache_shape(tokens: int, cache: torch.Tensor, block_table: Optional[torch.Tensor], batch: int):
+    """(s_max, block_tokens, max_blocks, blocks) of a cache whose dim `tokens` counts tokens; refuses one with too few sequences."""
+    if block_table is None:
+        if cache.shape[0] < batch:
+            raise InstInferError(ERR_INVALID_ARG)
+        return cache.shape[tokens], 0, 0, 0
+    if block_table.shape[0] < batch or not block_table.is_contiguous():
+        raise InstInferError(ERR_INVALID_ARG)
+    return 0, cache.shape[tokens], block_table.shape[1], cache.shape[0]
+
+
+def _check_append(batch: int, max_new: int, frequencies: torch.Tensor, seq_lens: torch.Tensor, new_lens: Optional[torch.Tensor],
+                  positions: Optional[torch.Tensor]) -> None:
+    """What the two turning appends ask of their small tensors."""
+    if frequencies.dtype != torch.float64 or not frequencies.is_contiguous() or seq_lens.numel() < batch or \
+            (new_lens is not None and new_lens.numel() < batch) or \
+            (positions is not None and (positions.shape != (batch, max_new) or not positions.is_contiguous())):
+        raise InstInferError(ERR_INVALID_ARG)
+    for t in (seq_lens, new_lens, positions):
+        if t is not None and t.dtype != torch.int32:
+            raise InstInferError(ERR_INVALID_ARG)
+
+
+def rope_append(q_out: Optional[torch.Tensor], k_cache: torch.Tensor, v_cache: torch.Tensor, q: Optional[torch.Tensor],
+                k_new: torch.Tensor, v_new: torch.Tensor, frequencies: torch.Tensor, seq_lens: torch.Tensor,
+                new_lens: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
+                positions: Optional[torch.Tensor] = None, interleaved: bool = False, magnitude: float = 1.0,
+                status_flags: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_rope_append: q [B, N, Hq, D] (None: keys and values only), k_new and v_new [B, N, H, D] in fp32, fp16 or
+    bf16, slices of one projection if need be; q_out fp16 as q; frequencies fp64 [rope_dim / 2]; caches fp16 [B, H, s_max, D]
+    or pools [P, H, T, D] with block_table; positions int32 [B, N]."""
+    batch, max_new, heads, head_dim = k_new.shape
+    here = _here(q_out, k_cache, v_cache, q, k_new, v_new, frequencies, seq_lens, new_lens, block_table, positions, status_flags)
+    if k_cache.shape != v_cache.shape or k_cache.shape[1] != heads or k_cache.shape[3] != head_dim or v_new.shape != k_new.shape or \
+            (q is None) != (q_out is None) or not (k_cache.is_contiguous() and v_cache.is_contiguous()) or \
+            k_cache.dtype != torch.float16 or v_cache.dtype != torch.float16:
+        raise InstInferError(ERR_INVALID_ARG)
+    if k_new.dtype not in _TYPES:
+        raise InstInferError(ERR_UNSUPPORTED)
+    q_heads = 0
+    if q is not None:
+        q_heads = q.shape[2]
+        if q.shape != (batch, max_new, q_heads, head_dim) or q_out.shape != q.shape or q_out.dtype != torch.float16 or not q_out.is_contiguous():
+            raise InstInferError(ERR_INVALID_ARG)
+    for t in (q, k_new, v_new):
+        if t is not None and (t.dtype != k_new.dtype or t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != head_dim)):
+            raise InstInferError(ERR_INVALID_ARG)
+    _check_append(batch, max_new, frequencies, seq_lens, new_lens, positions)
+    s_max, block_tokens, max_blocks, phys = _cache_shape(2, k_cache, block_table, batch)
+    _check(load().instinfer_rope_append(
+        _ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(q), k_new.data_ptr(), v_new.data_ptr(), _TYPES[k_new.dtype],
+        0 if q is None else _token_stride(q), _token_stride(k_new), _token_stride(v_new), frequencies.data_ptr(), 2 * frequencies.numel(),
+        int(interleaved), float(magnitude), _ptr(positions), seq_lens.data_ptr(), _ptr(new_lens), _ptr(block_table), max_blocks,
+        block_tokens, phys, batch, max_new, q_heads, heads, head_dim, s_max, _ptr(status_flags), _stream(stream, here)))
+
+
+def latent_append(q_out: Optional[torch.Tensor], cache: torch.Tensor, q_rope: Optional[torch.Tensor], latent_new: torch.Tensor,
+                  rope_new: torch.Tensor, frequencies: torch.Tensor, seq_lens: torch.Tensor,
+                  new_lens: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
+                  positions: Optional[torch.Tensor] = None, interleaved: bool = False, magnitude: float = 1.0,
+                  status_flags: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_latent_append: latent_new [B, N, L], rope_new [B, N, R], q_rope [B, N, H, R] (None: the cache's rows only),
+    slices of projections if need be; q_out [B, N, H, L + R]; cache [B, s_max, L + R] or a pool [P, T, L + R] with
+    block_table; all fp16 or all bf16."""
+    batch, max_new, latent_dim = latent_new.shape
+    rope_dim = rope_new.shape[2]
+    here = _here(q_out, cache, q_rope, latent_new, rope_new, frequencies, seq_lens, new_lens, block_table, positions, status_flags)
+    if rope_new.shape[:2] != latent_new.shape[:2] or cache.shape[2] != latent_dim + rope_dim or not cache.is_contiguous() or \
+            (q_rope is None) != (q_out is None) or frequencies.numel() * 2 != rope_dim or latent_new.stride(2) != 1 or rope_new.stride(2) != 1:
+        raise InstInferError(ERR_INVALID_ARG)
+    q_heads, head_stride = 0, 0
+    if q_rope is not None:
+        q_heads = q_rope.shape[2]
+        head_stride = q_rope.stride(2) if q_heads > 1 else rope_dim
+        if q_rope.shape != (batch, max_new, q_heads, rope_dim) or q_out.shape != (batch, max_new, q_heads, latent_dim + rope_dim) or \
+                q_rope.stride(3) != 1 or not q_out.is_contiguous():
+            raise InstInferError(ERR_INVALID_ARG)
+    if latent_new.dtype not in _TYPES:
+        raise InstInferError(ERR_UNSUPPORTED)
+    if any(t is not None and t.dtype != latent_new.dtype for t in (q_out, cache, q_rope, rope_new)):
+        raise InstInferError(ERR_INVALID_ARG)
+    _check_append(batch, max_new, frequencies, seq_lens, new_lens, positions)
+    s_max, block_tokens, max_blocks, phys = _cache_shape(1, cache, block_table, batch)
+    _check(load().instinfer_latent_append(
+        _ptr(q_out), cache.data_ptr(), _ptr(q_rope), latent_new.data_ptr(), rope_new.data_ptr(), _TYPES[latent_new.dtype],
+        0 if q_rope is None else _token_stride(q_rope), head_stride, _token_stride(latent_new), _token_stride(rope_new),
+        frequencies.data_ptr(), int(interleaved), float(magnitude), _ptr(positions), seq_lens.data_ptr(), _ptr(new_lens),
+        _ptr(block_table), max_blocks, block_tokens, phys, batch, max_new, q_heads, latent_dim, rope_dim, s_max,
+        _ptr(status_flags), _stream(stream, here)))
+
+
+def latent_workspace_bytes(batch: int, q_tokens: int, q_heads: int, latent_dim: int, rope_dim: int, max_seq_len: int) -> int:
+    return int(load().instinfer_latent_workspace_bytes(batch, q_tokens, q_heads, latent_dim, rope_dim, max_seq_len))
+
+
+def decode_attention_latent(out: torch.Tensor, lse: Optional[torch.Tensor], q: torch.Tensor, cache: torch.Tensor,
+                            block_table: Optional[torch.Tensor], seq_lens: torch.Tensor,
+                            tree_lens: Optional[torch.Tensor], mask: Optional[torch.Tensor], max_seq_len: int,
+                            scale: float, workspace: torch.Tensor, status_flags: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_decode_attention_latent: q [B, N, H, L + R], out [B, N, H, L], lse [B, N, H]; cache [B, s_max, L + R] or a pool
+    [P, T, L + R] with block_table; mask as tree_mask writes it, or None for a chain; all fp16 or all bf16."""
+    batch, q_tokens, q_heads, dims = q.shape
+    latent_dim = out.shape[3]
+    here = _here(out, lse, q, cache, block_table, seq_lens, tree_lens, mask, workspace, status_flags)
+    if out.shape != (batch, q_tokens, q_heads, latent_dim) or cache.shape[2] != dims or seq_lens.numel() < batch or \
+            (lse is not None and (lse.numel() != batch * q_tokens * q_heads or lse.dtype != torch.float32 or not lse.is_contiguous())) or \
+            (tree_lens is not None and (tree_lens.numel() < batch or tree_lens.dtype != torch.int32)) or seq_lens.dtype != torch.int32 or \
+            (mask is not None and (mask.numel() < batch * q_tokens * ((q_tokens + 63) // 64) or mask.dtype != torch.int64)) or \
+            not (out.is_contiguous() and q.is_contiguous() and cache.is_contiguous()):
+        raise InstInferError(ERR_INVALID_ARG)
+    if q.dtype not in _TYPES:
+        raise InstInferError(ERR_UNSUPPORTED)
+    if out.dtype != q.dtype or cache.dtype != q.dtype:
+        raise InstInferError(ERR_INVALID_ARG)
+    s_max, block_tokens, max_blocks, phys = _cache_shape(1, cache, block_table, batch)
+    _check(load().instinfer_decode_attention_latent(
+        out.data_ptr(), _ptr(lse), q.data_ptr(), cache.data_ptr(), _ptr(block_table), seq_lens.data_ptr(), _ptr(tree_lens), _ptr(mask),
+        _TYPES[q.dtype], batch, q_tokens, q_heads, latent_dim, dims - latent_dim, s_max, block_tokens, max_blocks, phys,
+        int(max_seq_len), float(scale), workspace.data_ptr(), workspace.nbytes, _ptr(status_flags), _stream(stream, here)))
+
+
 def tree_mask(mask: torch.Tensor, parents: torch.Tensor, tree_lens: Optional[torch.Tensor] = None,
               status_flags: Optional[torch.Tensor] = None,
               stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -385,7 +547,7 @@ def decode_attention_tree(out: torch.Tensor, lse: Optional[torch.Tensor], q: tor
         workspace.nbytes, _ptr(status_flags), _stream(stream, here)))
 
 
-_PROBS_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.Tensor,
@@ -405,11 +567,11 @@ def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.T
                 (batch > 1 and probs.stride(0) != tree_tokens * stride)):
             raise InstInferError(ERR_INVALID_ARG)
     here = _here(path, path_lens, out_tokens, target_probs, draft_probs, tokens, parents, tree_lens, uniforms, status_flags)
-    if target_probs.dtype not in _PROBS_TYPES:
+    if target_probs.dtype not in _TYPES:
         raise InstInferError(ERR_UNSUPPORTED)
     _check(load().instinfer_verify_tree(
         path.data_ptr(), path_lens.data_ptr(), out_tokens.data_ptr(), target_probs.data_ptr(), _ptr(draft_probs),
-        _PROBS_TYPES[target_probs.dtype], stride, tokens.data_ptr(), parents.data_ptr(), _ptr(tree_lens),
+        _TYPES[target_probs.dtype], stride, tokens.data_ptr(), parents.data_ptr(), _ptr(tree_lens),
         uniforms.data_ptr(), batch, tree_tokens, vocab, _ptr(status_flags), _stream(stream, here)))
 
 

@@ -2,6 +2,7 @@
 // Included by instinfer_api.cu (one translation unit: the kernels' headers define
 // non-template kernels, which must not be compiled twice).
 #include "grouped_umma_kernels.cuh"
+#include "tensor_map.cuh"
 
 namespace {
 
@@ -56,26 +57,6 @@ int launch_grouped(const GroupedParams &p, unsigned grid, cudaStream_t stream)
 }
 
 // ---- the tcgen05 form (head sizes 128 and 256; contiguous, or paged in blocks of 16, 32, 64 or a multiple of 128 tokens) ----
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's tensor-map encoder, looked up through the runtime (the library does not link libcuda).
-EncodeTiledFn tensor_map_encoder()
-{
-    static EncodeTiledFn fn = [] {
-        void *f = nullptr;
-        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            f = nullptr;
-        }
-        return reinterpret_cast<EncodeTiledFn>(f);
-    }();
-    return fn;
-}
 
 // A K or V cache as a 2-D fp16 tensor [rows][head_dim] (a row is one token of one head);
 // a box is 64 dims (128 bytes, the swizzle span) by `box_rows` tokens.
