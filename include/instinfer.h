@@ -78,6 +78,7 @@ typedef enum {
                                            distribution without a positive value */
 #define INSTINFER_FLAG_POOL          32 /* block pools: too few free blocks, an impossible fork, or reference counts that
                                            do not fit the tables */
+#define INSTINFER_FLAG_TOKEN_RANGE   64 /* logits: a token outside the vocabulary, or a history's lengths out of range */
 #define INSTINFER_FLAG_BOUNDS_CHECK  8  /* only in the bounds-checking build of the library (compiled with
                                            -DINSTINFER_BOUNDS_CHECK): a kernel computed a global offset outside the
                                            extent that the call's shapes imply and skipped that access; a defect of
@@ -464,6 +465,48 @@ int instinfer_verify_tree(int32_t *path, int32_t *path_lens, int32_t *out_tokens
                           const int32_t *tree_lens, const float *uniforms, int32_t batch,
                           int32_t tree_tokens, int32_t vocab, int32_t *status_flags,
                           void *cuda_stream);
+
+/*
+ * From the logits of a step to the probabilities that instinfer_verify_tree (or any sampling) takes: penalties for repeated
+ * tokens, biases, a grammar's mask, the temperature.  For row t of sequence b and token i, in 32 bits, in this order:
+ *     token in the sequence's prompt or output:  z = z > 0 ? z / repetition : z * repetition
+ *     z -= frequency * n + (n > 0 ? presence : 0),  n = how often the token is in the output
+ *     z += the sum of the sequence's biases of the token, in the list's order
+ *     token not allowed:  z = -infinity
+ *     probability = exp((z - max z) / T) / sum exp((z - max z) / T);  T = 0 (or less): 1 at the largest z, at the lowest
+ *     token of equal ones, 0 elsewhere
+ * What is not allowed never counts, whatever its logit.  A row in which nothing is left is all zeros (instinfer_verify_tree then
+ * flags it and gives -1); an allowed NaN or +infinity makes a row of T > 0 NaN; a NaN is never the largest.
+ *   out          out_type [batch, tree_tokens, vocab], rows out_stride >= vocab elements apart; may be logits itself where types and
+ *                strides are alike.  Rows of nodes from tree_lens[b] on stay as they were.
+ *   logits       logits_type [batch, tree_tokens, vocab], rows row_stride apart.  Either type INSTINFER_F32, _F16 or _BF16.
+ *   tokens       nullable int32 [batch, max_tokens]: the sequence's history, the first token_lens[b] (NULL: max_tokens) of them,
+ *                of which the first prompt_lens[b] (NULL: 0) are its prompt and the others its output
+ *   penalties    nullable fp32 [batch, 3]: repetition (1: none, positive), frequency (0: none), presence (0: none).  NULL: none, and
+ *                tokens and draft_tokens are not looked at.
+ *   draft_tokens nullable int32 [batch, tree_tokens]: a draft tree's tokens, which are not in `tokens`; those of the nodes that
+ *                tree_mask (as instinfer_tree_mask writes it; NULL: a chain) shows to node t are output too for row t
+ *   tree_lens    nullable int32 [batch]: rows that there are (NULL: tree_tokens)
+ *   bias_tokens, bias_values  nullable int32, fp32 [batch, max_bias]; a negative token is an unused entry
+ *   allowed      nullable uint32 [batch, tree_tokens, (vocab + 31) / 32]: bit i % 32 of word i / 32 allows token i
+ *   temperatures nullable fp32 [batch], finite (NULL: 1)
+ *   probabilities  0: out gets z / T instead (z where T is 0 or less), -infinity where not allowed
+ * Tokens >= vocab, tokens of the history or a draft < 0, and lengths out of range are flagged (INSTINFER_FLAG_TOKEN_RANGE;
+ * INSTINFER_FLAG_TREE_RANGE for tree_lens, whose rows are then left) and count nothing.
+ * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): vocab <= INSTINFER_MAX_VOCAB, max_bias <= INSTINFER_MAX_BIAS, tree_tokens <=
+ * INSTINFER_MAX_TREE_TOKENS.
+ */
+#define INSTINFER_MAX_VOCAB 262144
+#define INSTINFER_MAX_BIAS 256
+int instinfer_process_logits(void *out, int32_t out_type, int64_t out_stride, const void *logits,
+                             int32_t logits_type, int64_t row_stride, const int32_t *tokens,
+                             const int32_t *token_lens, const int32_t *prompt_lens, int32_t max_tokens,
+                             const float *penalties, const int32_t *draft_tokens,
+                             const uint64_t *tree_mask, const int32_t *tree_lens,
+                             const int32_t *bias_tokens, const float *bias_values, int32_t max_bias,
+                             const uint32_t *allowed, const float *temperatures, int32_t probabilities,
+                             int32_t batch, int32_t tree_tokens, int32_t vocab, int32_t *status_flags,
+                             void *cuda_stream);
 
 /*
  * Keeps the accepted path of a draft tree in the caches of all layers: the K and V rows of node

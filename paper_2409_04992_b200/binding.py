@@ -19,7 +19,8 @@ LIBRARY = Path(os.environ.get("INSTINFER_LIBRARY") or Path(__file__).resolve().p
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA = range(5)
 FLAG_SEQ_LEN_RANGE, FLAG_BLOCK_RANGE, FLAG_COPY_TIMEOUT, FLAG_BOUNDS_CHECK = 1, 2, 4, 8
-FLAG_TREE_RANGE, FLAG_POOL = 16, 32
+FLAG_TREE_RANGE, FLAG_POOL, FLAG_TOKEN_RANGE = 16, 32, 64
+MAX_VOCAB, MAX_BIAS = 262144, 256
 MAX_TREE_TOKENS, MAX_TREE_ROWS, MAX_LAYERS, MAX_LATENT_ROWS = 128, 4096, 128, 16384
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "by_parts": 2}
 STATIC_WORKSPACE_BYTES = 16 << 20
@@ -112,6 +113,9 @@ def load() -> ctypes.CDLL:
                                                           i32, i32, i64, i32, f32, ptr, sz, ptr, ptr]
         lib.instinfer_latent_workspace_bytes.restype = sz
         lib.instinfer_latent_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+        lib.instinfer_process_logits.restype = ctypes.c_int
+        lib.instinfer_process_logits.argtypes = [ptr, i32, i64, ptr, i32, i64, ptr, ptr, ptr, i32, ptr, ptr, ptr, ptr, ptr, ptr, i32, ptr,
+                                                 ptr, i32, i32, i32, i32, ptr, ptr]
         lib.instinfer_decode_step_host.restype = ctypes.c_int
         lib.instinfer_decode_step_host.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr,
                                                    i32, i32, i64, i32, i32, i32, i32, i32, f32,
@@ -573,6 +577,57 @@ def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.T
         path.data_ptr(), path_lens.data_ptr(), out_tokens.data_ptr(), target_probs.data_ptr(), _ptr(draft_probs),
         _TYPES[target_probs.dtype], stride, tokens.data_ptr(), parents.data_ptr(), _ptr(tree_lens),
         uniforms.data_ptr(), batch, tree_tokens, vocab, _ptr(status_flags), _stream(stream, here)))
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements from one row of t [B, T, V] to the next, all B * T of them evenly spaced (a padded vocabulary sliced to V will do)."""
+    batch, rows, vocab = t.shape
+    stride = t.stride(1) if rows > 1 else t.stride(0) if batch > 1 else (vocab + 3) // 4 * 4
+    if (vocab > 1 and t.stride(2) != 1) or (batch > 1 and t.stride(0) != rows * stride):
+        raise InstInferError(ERR_INVALID_ARG)
+    return stride
+
+
+def process_logits(out: torch.Tensor, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None,
+                   token_lens: Optional[torch.Tensor] = None, prompt_lens: Optional[torch.Tensor] = None,
+                   penalties: Optional[torch.Tensor] = None, draft_tokens: Optional[torch.Tensor] = None,
+                   mask: Optional[torch.Tensor] = None, tree_lens: Optional[torch.Tensor] = None,
+                   bias_tokens: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None,
+                   allowed: Optional[torch.Tensor] = None, temperatures: Optional[torch.Tensor] = None,
+                   probabilities: bool = True, status_flags: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+    """instinfer_process_logits: logits and out [B, T, V] in fp32, fp16 or bf16; tokens [B, M], token_lens and prompt_lens [B];
+    penalties fp32 [B, 3]; draft_tokens [B, T] with mask as tree_mask writes it; bias_tokens and bias_values [B, n]; allowed
+    int32 [B, T, ceil(V / 32)] (the bits of the header's uint32 words); temperatures fp32 [B]."""
+    batch, tree_tokens, vocab = logits.shape
+    here = _here(out, logits, tokens, token_lens, prompt_lens, penalties, draft_tokens, mask, tree_lens, bias_tokens, bias_values, allowed,
+                 temperatures, status_flags)
+    if out.shape != logits.shape or (bias_tokens is None) != (bias_values is None) or \
+            (mask is not None and (mask.dtype != torch.int64 or mask.numel() < batch * tree_tokens * ((tree_tokens + 63) // 64))):
+        raise InstInferError(ERR_INVALID_ARG)
+    n = batch * tree_tokens
+    for t, dtype, least in ((tokens, torch.int32, batch), (token_lens, torch.int32, batch), (prompt_lens, torch.int32, batch),
+                            (penalties, torch.float32, 3 * batch), (draft_tokens, torch.int32, n), (tree_lens, torch.int32, batch),
+                            (bias_tokens, torch.int32, batch), (allowed, torch.int32, n * ((vocab + 31) // 32)),
+                            (temperatures, torch.float32, batch)):
+        if t is not None and (t.dtype != dtype or t.numel() < least or not t.is_contiguous()):
+            raise InstInferError(ERR_INVALID_ARG)
+    max_tokens = max_bias = 0
+    if tokens is not None:
+        max_tokens = tokens.shape[1]
+        if tokens.shape[0] < batch:
+            raise InstInferError(ERR_INVALID_ARG)
+    if bias_tokens is not None:
+        max_bias = bias_tokens.shape[1]
+        if bias_tokens.shape[0] < batch or bias_values.shape != bias_tokens.shape or bias_values.dtype != torch.float32 or not bias_values.is_contiguous():
+            raise InstInferError(ERR_INVALID_ARG)
+    if out.dtype not in _TYPES or logits.dtype not in _TYPES:
+        raise InstInferError(ERR_UNSUPPORTED)
+    _check(load().instinfer_process_logits(
+        out.data_ptr(), _TYPES[out.dtype], _row_stride(out), logits.data_ptr(), _TYPES[logits.dtype], _row_stride(logits), _ptr(tokens),
+        _ptr(token_lens), _ptr(prompt_lens), max_tokens, _ptr(penalties), _ptr(draft_tokens), _ptr(mask), _ptr(tree_lens),
+        _ptr(bias_tokens), _ptr(bias_values), max_bias, _ptr(allowed), _ptr(temperatures), int(probabilities), batch, tree_tokens, vocab,
+        _ptr(status_flags), _stream(stream, here)))
 
 
 _bytes_of = torch.Tensor.nbytes.__get__

@@ -15,7 +15,7 @@ CHECKED_LIBRARY = _HERE / "libinstinfer_checked.so"     # the bounds-checking bu
 # instinfer_api.cu includes the api_*.inl parts; tree_* and latent_* hold instances of large kernels, one head size or type
 # each; the others are parts of the C ABI with kernels of their own
 SOURCES = [CSRC / "instinfer_api.cu", CSRC / "tree_d64.cu", CSRC / "tree_d128.cu", CSRC / "tree_d256.cu",
-           CSRC / "rope.cu", CSRC / "latent.cu", CSRC / "latent_f16.cu", CSRC / "latent_bf16.cu"]
+           CSRC / "rope.cu", CSRC / "logits.cu", CSRC / "latent.cu", CSRC / "latent_f16.cu", CSRC / "latent_bf16.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
               "-Xcompiler", "-fPIC", "-cudart", "static", "-Xptxas", "-v"]
 
