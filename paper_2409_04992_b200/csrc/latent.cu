@@ -62,7 +62,7 @@ int instinfer_decode_attention_latent(void *out, float *lse, const void *q, cons
     const LatentRows r = latent_rows(rows);
     const LatentCut cut = latent_cut(r, batch, max_seq_len, latent_dim);
     if (!usable(workspace) || workspace_bytes < cut.bytes) return INSTINFER_ERR_WORKSPACE;
-    const int row_parts = (int)ceil_div(r.block_rows, kLatentMergeRows);
+    const int row_parts = (int)ceil_div(r.block_rows, kLatentMergeThreads / 32 / (latent_dim / 128));
     if (cut.items * row_parts >= (int64_t)1 << 31 || cut.most_tiles >= (int64_t)1 << 31 || (int64_t)batch * s_max >= (int64_t)1 << 31)
         return INSTINFER_ERR_INVALID_ARG;
 
@@ -80,8 +80,7 @@ int instinfer_decode_attention_latent(void *out, float *lse, const void *q, cons
     unsigned char *start = static_cast<unsigned char *>(workspace);
     p.part_o = static_cast<float *>(workspace);
     p.part_lse = p.part_o + cut.slots * r.block_rows * latent_dim;
-    p.item_pieces = reinterpret_cast<int2 *>(start + cut.partials_bytes);
-    p.tickets = reinterpret_cast<unsigned *>(start + cut.ticket_offset);
+    p.item_shares = reinterpret_cast<int2 *>(start + cut.partials_bytes);
     p.num_phys_blocks = paged ? num_phys_blocks : 0;
     p.cache_rows = cache_rows;
     p.batch = batch;
@@ -90,8 +89,6 @@ int instinfer_decode_attention_latent(void *out, float *lse, const void *q, cons
     p.block_rows = r.block_rows;
     p.row_blocks = r.row_blocks;
     p.planes = r.planes;
-    p.plane_slots = (int32_t)cut.plane_slots;
-    p.short_pieces = r.short_pieces;
     p.max_seq_len = max_seq_len;
     p.s_max = paged ? 0 : s_max;
     p.block_tokens = paged ? block_tokens : 0;
@@ -108,10 +105,9 @@ int instinfer_decode_attention_latent(void *out, float *lse, const void *q, cons
     if (!make_latent_map(&t.map_q, kind, q, dims, rows, batch, r.columns) ||
         !make_latent_map(&t.map_cache, kind, cache, dims, cache_rows, 0, p.run_tokens))
         return INSTINFER_ERR_CUDA;
-    t.grid = cut.teams * r.planes;
+    t.grid = cut.grid;
     t.merge_grid = (unsigned)(cut.items * row_parts);
     t.row_parts = row_parts;
-    t.draws = cut.draws;
     t.stream = static_cast<cudaStream_t>(cuda_stream);
     return type == INSTINFER_F16 ? launch_latent<__half>(latent_dim, r.columns, t) : launch_latent<__nv_bfloat16>(latent_dim, r.columns, t);
 }

@@ -20,10 +20,6 @@ int launch_latent_instance(const LatentLaunch &t)
         }
         done[dev] = true;
     }
-    if (t.draws && cudaMemsetAsync(t.p.tickets, 0, t.p.planes * sizeof(unsigned), t.stream) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return INSTINFER_ERR_CUDA;
-    }
     cudaError_t err = launch_overlapped(latent_attn_kernel<E, L, N>, t.grid, Geo::kThreads, Geo::kSmemBytes, t.stream, t.p, t.map_q, t.map_cache);
     if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) return INSTINFER_ERR_CUDA;
     err = launch_overlapped(latent_merge_kernel<E, L>, t.merge_grid, kLatentMergeThreads, 0, t.stream, t.p, t.row_parts);

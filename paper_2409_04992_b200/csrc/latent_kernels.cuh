@@ -14,11 +14,16 @@
 // each: their tiles are cut alike, so that the blocks of all planes that work on the same tokens run at about the same
 // time and all but the first find them in L2.
 //
-// A block is persistent and has softmax warps (four, or two groups of four with half of the rows each) and three
-// single-purpose warps that hand tiles over through mbarriers, as in the kernels for draft trees, whose cut of the work
-// (TreePieces) this one shares:
-//   producer                 draws pieces, announces their segments through a queue in shared memory, copies tiles
-//                            (64-dim panels by tensor-map copies, 128-byte swizzle) and the segments' query rows;
+// Work split: a plane's tiles, item after item (an item is a row block of a sequence), lie in one row that is cut into
+// equal shares, one per block.  Only the items that a share starts or ends inside leave partial results, two per block at
+// most.  (Shorter pieces drawn from a counter, which the kernels for draft trees take, lose here: a partial result is four
+// times as large and each of its segments costs some three tiles; 128 sequences of 16k, 16 heads: 408 us with equal
+// shares, 465 with four drawn pieces a block.)  An item counts some tiles more than it has, for its segment's set-up.
+//
+// A block has softmax warps (four, or two groups of four with half of the rows each) and three single-purpose warps that
+// hand tiles over through mbarriers, as in the kernels for draft trees:
+//   producer                 finds the share's segments (its parts of items), announces them through a queue in shared
+//                            memory, copies tiles (64-dim panels by tensor-map copies, 128-byte swizzle) and query rows;
 //   logit and output issuer  one elected thread each issues the MMAs.  An item (128 dims of the tile) goes back to the producer as
 //                            soon as its accumulator's MMAs are complete, the turned part after the logits'.
 // A thread of the softmax warps has two tokens and a quarter of its group's rows (the 16-lane shape of the tensor-memory
@@ -37,7 +42,7 @@ constexpr int kLatentTile = 64;                          // tokens per tile
 constexpr int kLatentRope = 64;                          // turned dims
 constexpr int kLatentPanel = kLatentTile * 128;          // 64 dims of a tile
 constexpr int kLatentItem = 2 * kLatentPanel;            // 128 dims
-constexpr int kLatentItemCost = 6;                       // what a segment's set-up and end count in tiles
+constexpr int kLatentItemCost = 3;                       // what a segment's set-up and end count in tiles
 
 struct LatentParams {
     TreeShape tree;              // mask == nullptr: a chain, node t sees nodes 0 .. t
@@ -48,8 +53,7 @@ struct LatentParams {
     float *lse;                  // nullable [batch, rows]
     float *part_o;               // [slots, block_rows, L]
     float *part_lse;             // [slots, block_rows]
-    int2 *item_pieces;           // [batch * row_blocks] the pieces with an item's first and last tile
-    unsigned *tickets;           // [planes]
+    int2 *item_shares;           // [batch * row_blocks] the shares with an item's first and last tile, for the merge
     int64_t num_phys_blocks;
     int64_t cache_rows;
     int32_t batch;
@@ -58,8 +62,6 @@ struct LatentParams {
     int32_t block_rows;          // of a row block (the last one may have fewer)
     int32_t row_blocks;
     int32_t planes;
-    int32_t plane_slots;         // partial results of a plane
-    int32_t short_pieces;        // drawn pieces per block
     int32_t max_seq_len;
     int32_t s_max;
     int32_t block_tokens;
@@ -82,8 +84,8 @@ constexpr int kLatBarQEmpty = 312;
 constexpr int kLatBarSegFull = 320;    // [4]
 constexpr int kLatBarSegEmpty = 352;   // [4]
 constexpr int kLatTmemPtr = 384;
-constexpr int kLatTotal = 388;
-constexpr int kLatScan = 392;          // [16] ints, before the first segment
+constexpr int kLatTotal = 388;         // the plane's tiles; a window's first sequence and its start
+constexpr int kLatScan = 400;          // [16] ints, before the first segment
 constexpr int kLatSegments = 464;      // [4] LatentSegment
 constexpr int kLatSegmentBytes = 56;
 constexpr int kLatMiscBytes = 704;
@@ -140,120 +142,117 @@ __device__ __forceinline__ int latent_weight(int tiles) { return tiles > 0 ? til
 // Row blocks of a sequence that a plane has: plane, plane + planes, ...
 __device__ __forceinline__ int latent_plane_items(const LatentParams &p, int plane) { return (p.row_blocks - plane + p.planes - 1) / p.planes; }
 
-// Draws this block's pieces and finds their segments (all 32 lanes of one warp together); see TreeFinder.
+// Finds the segments of this block's share (all 32 lanes of one warp together).
 struct LatentFinder {
-    TreePieces pieces;
-    int n_pieces, piece, tile, end, plane, items;
-    unsigned drawn;                // lane 0: the next piece, asked for when this one began
-    int b, len, nodes;             // a sequence with tiles ...
-    int base, limit;               // ... the plane's tiles [base, limit)
-    __device__ __forceinline__ LatentFinder() : pieces(0, 1, 1) {}
-    __device__ __noinline__ void start(const LatentParams &p, int total, int lane)
+    int plane, items, team;        // the block's plane, row blocks of a sequence there, its number in it
+    int tile, end;                 // what is left of the share
+    // 32 sequences from w0 on, one a lane: length, new tokens, and where its items end in the plane's row; start: the first one's start
+    int w0, start, len, nodes, stop;
+    __device__ __forceinline__ void load(const LatentParams &p, int lane)
     {
-        plane = blockIdx.x % p.planes;
-        items = latent_plane_items(p, plane);
-        pieces = TreePieces(total, gridDim.x / p.planes, p.short_pieces);
-        n_pieces = pieces.count();
-        b = -1;
-        len = nodes = base = limit = 0;
-        const int team = blockIdx.x / p.planes;
-        begin(p, team < pieces.blocks ? team : n_pieces, lane);
+        len = nodes = 0;
+        if (w0 + lane < p.batch) len = checked_tree(p.tree, p.seq_lens, p.max_seq_len, nullptr, w0 + lane, false, nodes);
+        stop = latent_weight(latent_tiles(len, nodes)) * items;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, stop, o);
+            if (lane >= o) stop += up;
+        }
+        stop += start;
     }
-    __device__ __forceinline__ void begin(const LatentParams &p, int which, int lane)
+    // The share of a plane of `total` tiles; the window lies at or before its first tile.
+    __device__ __forceinline__ void begin(int total)
     {
-        piece = min(which, n_pieces);
-        tile = end = 0;
-        drawn = n_pieces;
-        if (piece >= n_pieces) return;
-        tile = pieces.first(piece);
-        end = pieces.first(piece + 1);
-        if (lane == 0 && pieces.step > 0) drawn = pieces.blocks + atomicAdd(p.tickets + plane, 1u);
+        const int teams = gridDim.x / planes_of_grid, blocks = min(teams, total);
+        tile = end = total;
+        if (team >= blocks) return;
+        const int length = total / blocks, longer = total - length * blocks;       // (the first `longer` shares are one tile longer)
+        tile = length * team + min(team, longer);
+        end = tile + length + (team < longer ? 1 : 0);
     }
+    int planes_of_grid;
     template <typename E, int L>
     __device__ __noinline__ LatentSegment next(const LatentParams &p, int lane)
     {
         LatentSegment s;
         s.b = -1;
-        int rb;
-        do {
-            if (tile >= end && piece < n_pieces) {
-                const unsigned got = __shfl_sync(0xffffffffu, drawn, 0);
-                begin(p, got < (unsigned)n_pieces ? (int)got : n_pieces, lane);
+        for (;;) {
+            if (tile >= end) return s;
+            unsigned reached = __ballot_sync(0xffffffffu, stop > tile);
+            while (reached == 0) {
+                w0 += 32;
+                if (w0 >= p.batch) return s;          // (lengths that change under the kernel's hands)
+                start = __shfl_sync(0xffffffffu, stop, 31);
+                load(p, lane);
+                reached = __ballot_sync(0xffffffffu, stop > tile);
             }
-            if (piece >= n_pieces) return s;
-            while (tile >= limit) {    // (tile < W: some sequence has it)
-                const int from = b + 1;
-                if (from >= p.batch) return s;
-                int n = 0, l = 0;
-                if (from + lane < p.batch) l = checked_tree(p.tree, p.seq_lens, p.max_seq_len, nullptr, from + lane, false, n);
-                const int mine = latent_weight(latent_tiles(l, n)) * items;
-                int sum = mine;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int up = __shfl_up_sync(0xffffffffu, sum, o);
-                    if (lane >= o) sum += up;
-                }
-                const unsigned reached = __ballot_sync(0xffffffffu, limit + sum > tile);
-                const int at = reached ? __ffs(reached) - 1 : 31;
-                len = __shfl_sync(0xffffffffu, l, at);
-                nodes = __shfl_sync(0xffffffffu, n, at);
-                base = limit + __shfl_sync(0xffffffffu, sum - mine, at);
-                limit = limit + __shfl_sync(0xffffffffu, sum, at);
-                b = from + at;
-            }
-            s.n_tiles = latent_tiles(len, nodes);
-            if (b >= p.batch || s.n_tiles == 0) return s;     // (lengths that change under the kernel's hands)
-            const int weight = latent_weight(s.n_tiles), inside = tile - base, item = inside / weight;
-            const int from = inside - item * weight;
-            int to = min(weight, from + (end - tile));
-            rb = plane + item * p.planes;
+            const int at = __ffs(reached) - 1;
+            const int before = __shfl_sync(0xffffffffu, stop, max(at - 1, 0));
+            s.len = __shfl_sync(0xffffffffu, len, at);
+            s.nodes = __shfl_sync(0xffffffffu, nodes, at);
+            s.n_tiles = latent_tiles(s.len, s.nodes);
+            const int weight = latent_weight(s.n_tiles), inside = tile - (at == 0 ? start : before), item = items == 1 ? 0 : inside / weight;
+            const int from = inside - item * weight, to = min(weight, from + (end - tile));
+            const int rb = plane + item * planes_of_grid;
             s.t0 = max(0, from - kLatentItemCost);
-            // An item that is short next to the long pieces and starts in one stays whole, with the piece that has its start.
-            if (pieces.step > 0 && 2 * weight <= pieces.length && tile - from < pieces.drawn) {
-                to = weight;
-                if (from > 0) s.t0 = weight;                  // another piece has it
-            }
             s.t1 = to - kLatentItemCost;
             tile += to - from;
-        } while (s.t1 <= s.t0);                               // only of the item's extra weight
-        s.b = b;
-        s.len = len;
-        s.nodes = nodes;
-        s.row0 = rb * p.block_rows;
-        s.rows = min(p.block_rows, p.rows - s.row0);
-        s.pad = 0;
-        if (lane == 0) {
-            int2 *of_item = p.item_pieces + (int64_t)b * p.row_blocks + rb;
-            if (s.t0 == 0) of_item->x = piece;
-            if (s.t1 == s.n_tiles) of_item->y = piece;
+            if (s.t1 <= s.t0) continue;               // only of the item's extra weight
+            s.b = w0 + at;
+            s.row0 = rb * p.block_rows;
+            s.rows = min(p.block_rows, p.rows - s.row0);
+            s.pad = 0;
+            if (lane == 0) {
+                int2 *of_item = p.item_shares + (int64_t)s.b * p.row_blocks + rb;
+                if (s.t0 == 0) of_item->x = team;
+                if (s.t1 == s.n_tiles) of_item->y = team;
+            }
+            // (what starts inside an item goes to its block's first slot, what ends inside one to its second)
+            s.slot = 2 * (plane + team * planes_of_grid) + (s.t0 == 0 ? 1 : 0);
+            const int64_t row = (int64_t)s.b * p.rows + s.row0, slot_row = (int64_t)s.slot * p.block_rows;
+            s.out = s.whole() ? static_cast<void *>(static_cast<E *>(p.out) + row * L) : static_cast<void *>(p.part_o + slot_row * L);
+            s.lse = !s.whole() ? p.part_lse + slot_row : p.lse ? p.lse + row : nullptr;
+            return s;
         }
-        s.slot = plane * p.plane_slots + 2 * piece + (s.t0 == 0 ? 1 : 0);
-        const int64_t row = (int64_t)b * p.rows + s.row0, slot_row = (int64_t)s.slot * p.block_rows;
-        s.out = s.whole() ? static_cast<void *>(static_cast<E *>(p.out) + row * L) : static_cast<void *>(p.part_o + slot_row * L);
-        s.lse = !s.whole() ? p.part_lse + slot_row : p.lse ? p.lse + row : nullptr;
-        return s;
     }
 };
 
-// Adds up all sequences' tiles of this block's plane (all threads; the caller synchronises).
-__device__ __forceinline__ void latent_count_tiles(const LatentParams &p, unsigned char *misc_ptr, int threads)
+// More than 32 sequences: all threads add up the plane's tiles (and report lengths out of range), and leave the total and
+// where the window of 32 sequences around this block's first tile starts in the misc region.
+__device__ __forceinline__ void latent_scan(const LatentParams &p, unsigned char *misc_ptr, int threads, int plane, int items, int team)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int per = (p.batch + threads - 1) / threads, b0 = threadIdx.x * per;
     int mine = 0;                      // (all tiles are fewer than 2^31: checked by the host)
-    for (int b = threadIdx.x; b < p.batch; b += threads) {
+    for (int b = b0; b < min(b0 + per, p.batch); ++b) {
         int nodes;
         const int len = checked_tree(p.tree, p.seq_lens, p.max_seq_len, p.status, b, blockIdx.x == 0, nodes);
-        mine += latent_weight(latent_tiles(len, nodes));
+        mine += latent_weight(latent_tiles(len, nodes)) * items;
     }
+    int sum = mine;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += up;
+    }
     int *scan = reinterpret_cast<int *>(misc_ptr + kLatScan);
-    if (lane == 0) scan[warp] = mine;
+    if (lane == 31) scan[warp] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        int total = 0;
-        for (int w = 0; w < threads / 32; ++w) total += scan[w];
-        *reinterpret_cast<int *>(misc_ptr + kLatTotal) = total * latent_plane_items(p, blockIdx.x % p.planes);
+    int total = 0, before = 0;
+    for (int w = 0; w < threads / 32; ++w) {
+        if (w == warp) before = total;
+        total += scan[w];
+    }
+    before += sum - mine;
+    LatentFinder share;
+    share.planes_of_grid = p.planes;
+    share.team = team;
+    share.begin(total);
+    int *found = reinterpret_cast<int *>(misc_ptr + kLatTotal);
+    if (threadIdx.x == 0) found[0] = total;
+    if (share.tile < share.end && before <= share.tile && share.tile < before + mine) {
+        found[1] = b0;
+        found[2] = before;
     }
 }
 
@@ -334,6 +333,19 @@ __device__ __forceinline__ E latent_round(float x)
     if constexpr (std::is_same<E, __half>::value) return __float2half_rn(x);
     else return __float2bfloat16_rn(x);
 }
+// The new token that query row r belongs to, r / q_heads: (r + 1/2) / q_heads is further from a whole number than 32 bits
+// are off, with r < 2^14.
+__device__ __forceinline__ int latent_node(int r, float heads_inverse) { return (int)(((float)r + 0.5f) * heads_inverse); }
+
+// Which of the new tokens `at` and at + 8 (negative: positions before them) node `node` of `nodes` sees, by the mask.
+__device__ __forceinline__ unsigned latent_sees(const TreeShape &tree, int b, int node, int nodes, int at)
+{
+    if (node >= nodes) return 0;
+    const uint64_t *words = tree.mask + ((int64_t)b * tree.tokens + node) * tree.words;
+    auto one = [&](int j) -> unsigned { return j < 0 ? 1u : j < nodes ? (unsigned)(words[j >> 6] >> (j & 63) & 1u) : 0u; };
+    return one(at) | one(at + 8) << 1;
+}
+
 // Whether none of 8 values is an infinity or a NaN.
 template <typename E>
 __device__ __forceinline__ bool latent_finite8(const uint4 &x)
@@ -369,12 +381,28 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
         if (lane == 0) mbarrier_arrive(misc + kLatBarSegEmpty + (k & 3) * 8);
     };
 
-    latent_count_tiles(p, misc_ptr, Geo::kThreads);
+    LatentFinder finder;               // (of the copying warp)
+    finder.planes_of_grid = p.planes;
+    finder.plane = blockIdx.x % p.planes;
+    finder.team = blockIdx.x / p.planes;
+    finder.items = latent_plane_items(p, finder.plane);
+    finder.w0 = finder.start = 0;
+    if (p.batch > 32) latent_scan(p, misc_ptr, Geo::kThreads, finder.plane, finder.items, finder.team);
+    LatentSegment seg;
     if (warp == kWarpLogits) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      :: "r"(misc + kLatTmemPtr), "n"(Geo::kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    } else if (warp == kWarpCopy && lane == 0) {
+    } else if (warp == kWarpCopy && p.batch <= 32) {
+        if (lane < 2) asm volatile("prefetch.tensormap [%0];" :: "l"(reinterpret_cast<uint64_t>(lane ? &map_cache : &map_q)) : "memory");
+        finder.load(p, lane);
+        if (blockIdx.x == 0 && lane < p.batch) {                  // lengths out of range
+            int nodes;
+            (void)checked_tree(p.tree, p.seq_lens, p.max_seq_len, p.status, lane, true, nodes);
+        }
+        finder.begin(__shfl_sync(0xffffffffu, finder.stop, 31));
+        seg = finder.template next<E, L>(p, lane);
+    } else if (warp == kWarpOutput && lane == 0) {
         for (int s = 0; s < 12; ++s) {
             mbarrier_init(misc + kLatBarFull + s * 8, 1);
             mbarrier_init(misc + kLatBarEmpty + s * 8, 1);
@@ -404,8 +432,16 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
         // ================================ copies ================================
         const bool paged = p.block_table != nullptr;
         const int T = p.run_tokens;
-        LatentFinder finder;
-        finder.start(p, *reinterpret_cast<const int *>(misc_ptr + kLatTotal), lane);
+        if (p.batch > 32) {
+            const int *found = reinterpret_cast<const int *>(misc_ptr + kLatTotal);
+            finder.begin(found[0]);
+            if (finder.tile < finder.end) {
+                finder.w0 = found[1];
+                finder.start = found[2];
+                finder.load(p, lane);
+            }
+            seg = finder.template next<E, L>(p, lane);
+        }
         int g = 0, k = 0;                                 // tiles and segments so far
         bool fine = true;
         // lane i: the physical block of the i-th run of tile j (asked for one tile ahead)
@@ -430,26 +466,30 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                 row = s.b * p.s_max + start;              // rows past the tensor's end read as zeros
             }
             const unsigned fetched = __popc(__ballot_sync(0xffffffffu, good));
+            const bool missing = lane < nb && !good;      // a block that cannot be read counts as zeros
+            const bool any_missing = __any_sync(0xffffffffu, missing);
+            // (lane r + 8 q asks for panel q of run r)
+            const int my_row = __shfl_sync(0xffffffffu, row, lane & 7);
+            const bool my_good = __shfl_sync(0xffffffffu, (int)good, lane & 7) != 0;
+            const unsigned my_at = (lane & 7) * T * 128 + (lane >> 3) * kLatentPanel;
             // One item of `panels` panels into a slot; the slot is free.
             auto copy_item = [&](unsigned slot_offset, unsigned bar, int dim, int panels) {
-                const unsigned at = slot_offset + lane * T * 128;
-                if (lane < nb && !good) {                 // a block that cannot be read counts as zeros
-                    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                if (any_missing) {
+                    if (missing) {
+                        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll 1
-                    for (int panel = 0; panel < panels; ++panel)
+                        for (int panel = 0; panel < panels; ++panel)
 #pragma unroll 1
-                        for (int i = 0; i < T * 8; ++i) *reinterpret_cast<uint4 *>(smem + at + panel * kLatentPanel + i * 16) = zero;
-                    fence_async_proxy();
+                            for (int i = 0; i < T * 8; ++i) *reinterpret_cast<uint4 *>(smem + slot_offset + lane * T * 128 + panel * kLatentPanel + i * 16) = zero;
+                        fence_async_proxy();
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
                 if (lane == 0) mbarrier_expect_bytes(bar, fetched * (unsigned)(T * 128 * panels));
                 __syncwarp();
-                if (good) {
-                    for (int panel = 0; panel < panels; ++panel)
-                        tma_load_2d(base + at + panel * kLatentPanel, &map_cache, dim + panel * 64, row, bar);
-                }
+                if (my_good && lane < 8 * panels) tma_load_2d(base + slot_offset + my_at, &map_cache, dim + (lane >> 3) * 64, my_row, bar);
             };
-#pragma unroll
+#pragma unroll 1
             for (int item = 0; item < kItems; ++item) {
                 const int n = g * kItems + item, slot = n % kSlots;
                 if (n >= kSlots && !__all_sync(0xffffffffu, tree_wait(misc + kLatBarEmpty + slot * 8, (n / kSlots - 1) & 1))) return false;
@@ -468,29 +508,22 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
             }
             return true;
         };
-        // Segments are found two ahead: lengths, block ids and the ticket's answer come from a busy memory system.
-        LatentSegment seg = finder.template next<E, L>(p, lane);
+        // A segment is found while the copies of the one before run.
         (void)announce(seg, 0);
         int ids = seg.b >= 0 ? fetch_ids(seg, seg.t0) : -1;
-        LatentSegment after = seg;
-        if (seg.b >= 0) {
-            after = finder.template next<E, L>(p, lane);
-            (void)announce(after, 1);
-        }
         bool asked_q = false;
         for (; fine && seg.b >= 0; ++k) {
-            LatentSegment later = after;                  // segment k + 2
+            LatentSegment after = seg;                    // segment k + 1
             int ids_after = -1;
             for (int j = seg.t0; j < seg.t1 && fine; ++j) {
                 if (j == seg.t0) {
                     // the query rows wait for the last segment's logits
                     if (k >= 1) fine = __all_sync(0xffffffffu, tree_wait(misc + kLatBarQEmpty, (k - 1) & 1));
                     if (!fine) break;
-                    if (lane == 0) {
-                        mbarrier_expect_bytes(misc + kLatBarQFull, (unsigned)Geo::kQBytes);
-                        for (int panel = 0; panel <= kPanels; ++panel)       // (rows behind the sequence's last are zeros)
-                            tma_load_3d(q_smem + panel * Geo::kQPanel, &map_q, panel * 64, seg.row0, seg.b, misc + kLatBarQFull);
-                    }
+                    if (lane == 0) mbarrier_expect_bytes(misc + kLatBarQFull, (unsigned)Geo::kQBytes);
+                    __syncwarp();
+                    if (lane <= kPanels)                      // (rows behind the sequence's last are zeros)
+                        tma_load_3d(q_smem + lane * Geo::kQPanel, &map_q, lane * 64, seg.row0, seg.b, misc + kLatBarQFull);
                     asked_q = true;
                     __syncwarp();
                 }
@@ -499,16 +532,13 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                 fine = copy_tile(seg, j, now);
                 if (fine) ++g;
                 if (j > seg.t0 || !fine) continue;
-                if (after.b >= 0) {
-                    ids_after = fetch_ids(after, after.t0);
-                    later = finder.template next<E, L>(p, lane);
-                    fine = fine && announce(later, k + 2);
-                }
+                after = finder.template next<E, L>(p, lane);
+                fine = announce(after, k + 1);
+                if (after.b >= 0) ids_after = fetch_ids(after, after.t0);
             }
             if (!fine) break;
             asked_q = false;
             seg = after;
-            after = later;
             ids = ids_after;
         }
         if (!fine) {
@@ -618,7 +648,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
         constexpr int kPer = kCols / 8;                               // pairs of columns of a thread
         float *by_warp = reinterpret_cast<float *>(misc_ptr + kLatMiscBytes);        // [N][4]: a row's maxima, or sums, by warp
         float *offsets = by_warp + N * 4;                             // [N]: the rows' references (negated) as they were last moved
-        const float scale = p.scale_log2e, sign = copysignf(1.f, scale);
+        const float scale = p.scale_log2e, sign = copysignf(1.f, scale), heads_inverse = 1.f / (float)p.q_heads;
         bool fine = true;
         int g = 0;
         for (int k = 0;; ++k) {
@@ -643,29 +673,14 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                 const bool masked = start + kLatentTile > prefix;     // uniform
                 unsigned hidden = 0;                                  // bit 4 i + 2 u + c: column c of pair i does not see token u
                 if (masked) {
+                    const int at = start + token - prefix;            // the first token as a new one; the second is at + 8
 #pragma unroll 1
-                    for (int i = 0; i < kPer; ++i) {
-#pragma unroll 1
-                        for (int c = 0; c < 2; ++c) {
-                            const int node = (row0 + 8 * i + column + c) / p.q_heads;
-                            uint64_t words[2] = {0, 0};
-                            if (node < nodes) {
-                                if (p.tree.mask == nullptr) {
-                                    words[0] = node >= 63 ? ~0ull : (1ull << (node + 1)) - 1;
-                                    words[1] = node >= 127 ? ~0ull : node >= 64 ? (1ull << (node - 63)) - 1 : 0;
-                                } else {
-                                    const uint64_t *from = p.tree.mask + ((int64_t)seg.b * p.tree.tokens + node) * p.tree.words;
-                                    words[0] = from[0];
-                                    if (p.tree.words > 1) words[1] = from[1];
-                                }
-                            }
-#pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                const int pos = start + token + 8 * u, at = pos - prefix;
-                                const bool sees = pos < len && node < nodes && (at < 0 || ((at < 64 ? words[0] : words[1]) >> (at & 63) & 1u) != 0);
-                                hidden |= (unsigned)!sees << (4 * i + 2 * u + c);
-                            }
-                        }
+                    for (int i = 0; i < 2 * kPer; ++i) {              // column i % 2 of pair i / 2
+                        const int node = latent_node(row0 + 8 * (i >> 1) + column + (i & 1), heads_inverse);
+                        unsigned sees = (at <= node ? 1u : 0u) | (at + 8 <= node ? 2u : 0u);
+                        if (p.tree.mask != nullptr) sees = latent_sees(p.tree, seg.b, node, nodes, at);
+                        if (node >= nodes) sees = 0;
+                        hidden |= ((~sees & 1u) | (~sees & 2u) << 1) << (4 * (i >> 1) + (i & 1));
                     }
                 }
                 if (fine) fine = tree_wait(misc + kLatBarSFull + buf * 8, (g >> 1) & 1);
@@ -778,33 +793,28 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                     // Value rows behind the sequence get weight 0 but may hold anything, and 0 x NaN is NaN: they are
                     // cleared.  So are new tokens' rows that are not finite: a row that sees one has a logit that is
                     // not finite (its values are part of its key), which makes the row NaN without them.
-                    const int first = quarter * 16 + group * (16 / Geo::kGroups);
-                    if (start + first + 16 / Geo::kGroups > prefix) {
-#pragma unroll 1
-                        for (int item = 0; item < kItems; ++item) {   // (the logits have read them: they have landed)
-                            const int n = g * kItems + item, slot = n % kSlots;
-                            if (fine) fine = tree_wait(misc + kLatBarFull + slot * 8, (n / kSlots) & 1);
-                        }
+                    // A row is L / 8 chunks of 16 bytes, a lane's are those of panel lane / 8 and of the panel four further on.
+                    const int first = quarter * 16 + group * (16 / Geo::kGroups), last = first + 16 / Geo::kGroups;
+                    if (start + last > prefix) {
+                        // (the logits have read the tile: it has landed)
+                        const int item = g * kItems + min(lane, kItems - 1);
+                        if (fine) fine = tree_wait(misc + kLatBarFull + item % kSlots * 8, (item / kSlots) & 1);
                         __syncwarp();
+                        unsigned char *chunks[kPanels / 4];
+#pragma unroll
+                        for (int i = 0; i < kPanels / 4; ++i)
+                            chunks[i] = smem + (g * kItems + (lane >> 4) + 2 * i) % kSlots * kLatentItem + (lane >> 3 & 1) * kLatentPanel + (lane & 7) * 16;
 #pragma unroll 1
-                        for (int r0 = first; r0 < first + 16 / Geo::kGroups; r0 += 4) {        // four rows at a time, 8 lanes a row
-                            const int pos = start + r0 + (lane >> 3);
-                            bool bad = false;
-#pragma unroll 1
-                            for (int panel = 0; panel < kPanels; ++panel) {
-                                const int slot = (g * kItems + panel / 2) % kSlots;
-                                bad = bad || !latent_finite8<E>(*reinterpret_cast<const uint4 *>(smem + slot * kLatentItem + (panel & 1) * kLatentPanel + r0 * 128 + lane * 16));
+                        for (int r = max(first, prefix - start); r < last; ++r) {
+                            if (start + r < len) {
+                                bool bad = false;
+#pragma unroll
+                                for (int i = 0; i < kPanels / 4; ++i) bad = bad | !latent_finite8<E>(*reinterpret_cast<const uint4 *>(chunks[i] + r * 128));
+                                if (!__any_sync(0xffffffffu, bad)) continue;
                             }
-                            const unsigned found = __ballot_sync(0xffffffffu, bad && pos >= prefix);
-                            if ((found >> (lane & 24) & 0xffu) != 0 || pos >= len) {
-#pragma unroll 1
-                                for (int panel = 0; panel < kPanels; ++panel) {
-                                    const int slot = (g * kItems + panel / 2) % kSlots;
-                                    *reinterpret_cast<uint4 *>(smem + slot * kLatentItem + (panel & 1) * kLatentPanel + r0 * 128 + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
-                                }
-                            }
+#pragma unroll
+                            for (int i = 0; i < kPanels / 4; ++i) *reinterpret_cast<uint4 *>(chunks[i] + r * 128) = make_uint4(0u, 0u, 0u, 0u);
                         }
-                        __syncwarp();
                     }
                 }
                 // Lane i has the address of token row i % 8 of block i / 8: tokens 0-7 and 8-15 of two blocks of 8 columns.
@@ -897,84 +907,71 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
     }
 }
 
-// Joins the partial results of the items that more than one piece has a part of, and zeroes the rows of sequences
-// without work; a warp takes one row after the other (see tree_merge_kernel).
+// Joins the partial results of the items that more than one share has a part of, and zeroes the rows of sequences
+// without work.  A warp takes 128 dims of one row, so that the partials of an item of some shares are few rounds of loads:
+// the kernel is a chain of those (the item's shares, their log-sum-exps, the partials).
 constexpr int kLatentMergeThreads = 256;
-constexpr int kLatentMergeRows = 8;       // rows of a block: one a warp
+constexpr int kLatentMergeDeep = 8;
 
 template <typename E, int L>
 __global__ void __launch_bounds__(kLatentMergeThreads)
 latent_merge_kernel(const LatentParams p, int row_parts)
 {
-    const int lane = threadIdx.x & 31;
+    constexpr int kRows = kLatentMergeThreads / 32 / (L / 128);       // rows of a block
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int part = blockIdx.x % row_parts, item = blockIdx.x / row_parts;           // (sequence, row block)
     const int b = item / p.row_blocks, rb = item - b * p.row_blocks;
+    const int r = part * kRows + warp / (L / 128), row = rb * p.block_rows + r, d = warp % (L / 128) * 128 + lane * 4;
     allow_next_kernel();
     wait_for_previous_kernels();
     int nodes;
-    const int2 pieces = p.item_pieces[item];
+    const int2 shares = p.item_shares[item];
     const int len = checked_tree(p.tree, p.seq_lens, p.max_seq_len, nullptr, b, false, nodes);
-    const int c0 = pieces.x, n = latent_tiles(len, nodes) > 0 ? pieces.y - c0 + 1 : 0;
-    if (n == 1) return;                                               // one piece had it all: the result is written
-    const int r = part * kLatentMergeRows + (threadIdx.x >> 5), row = rb * p.block_rows + r;
+    const int c0 = shares.x, n = latent_tiles(len, nodes) > 0 ? shares.y - c0 + 1 : 0;
+    if (n == 1) return;                                               // one share had it all: the result is written
     if (r >= p.block_rows || row >= p.rows) return;
     const int64_t out_row = (int64_t)b * p.rows + row;
-    // (the item's start went to its piece's second slot, all else to the first one)
-    const int64_t slot0 = (int64_t)(rb % p.planes) * p.plane_slots;
-    auto slot_row = [&](int i) -> int64_t { return (slot0 + 2 * (c0 + i) + (i == 0 ? 1 : 0)) * p.block_rows + r; };
+    // (the item's start went to its block's second slot, all else to the first one)
+    auto slot_row = [&](int i) -> int64_t { return (int64_t)(2 * (rb % p.planes + (c0 + i) * p.planes) + (i == 0 ? 1 : 0)) * p.block_rows + r; };
     float top = kMinusHuge, total = 0.f;
     bool any_nan = false;
+    float first_lse = kMinusHuge;                                     // of the first 32 partials, a lane each
     for (int i = lane; i < n; i += 32) {
         const float lse = p.part_lse[slot_row(i)];
+        if (i < 32) first_lse = lse;
         top = fmaxf(top, lse);
         any_nan = any_nan || lse != lse;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const bool empty = !(top > kMinusHuge) && !__any_sync(0xffffffffu, any_nan);
-    constexpr int kVecs = L / 128;                                    // a lane's dims: kVecs runs of four
-    float4 acc[kVecs];
-#pragma unroll
-    for (int v = 0; v < kVecs; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i0 = 0; i0 < n && !empty; i0 += 32) {
-        const float mine = i0 + lane < n ? fast_exp2((p.part_lse[slot_row(i0 + lane)] - top) * 1.44269504088896340736f) : 0.f;
+        const float lse = i0 == 0 ? first_lse : i0 + lane < n ? p.part_lse[slot_row(i0 + lane)] : kMinusHuge;
+        const float mine = i0 + lane < n ? fast_exp2((lse - top) * 1.44269504088896340736f) : 0.f;
         const int here = min(32, n - i0);
-        constexpr int kDeep = 4;
-        for (int i = 0; i < here; i += kDeep) {
-            float4 x[kDeep][kVecs];
+        for (int i = 0; i < here; i += kLatentMergeDeep) {
+            float4 x[kLatentMergeDeep];
 #pragma unroll
-            for (int u = 0; u < kDeep; ++u) {
-                if (i + u < here) {
-                    const float *from = p.part_o + slot_row(i0 + i + u) * L + lane * 4;
+            for (int u = 0; u < kLatentMergeDeep; ++u) x[u] = i + u < here ? *reinterpret_cast<const float4 *>(p.part_o + slot_row(i0 + i + u) * L + d) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                    for (int v = 0; v < kVecs; ++v) x[u][v] = *reinterpret_cast<const float4 *>(from + v * 128);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kDeep; ++u) {
+            for (int u = 0; u < kLatentMergeDeep; ++u) {
                 const float w = __shfl_sync(0xffffffffu, mine, (i + u) & 31);
                 if (i + u < here) {
                     total += w;
-#pragma unroll
-                    for (int v = 0; v < kVecs; ++v) {
-                        acc[v].x = fmaf(w, x[u][v].x, acc[v].x);
-                        acc[v].y = fmaf(w, x[u][v].y, acc[v].y);
-                        acc[v].z = fmaf(w, x[u][v].z, acc[v].z);
-                        acc[v].w = fmaf(w, x[u][v].w, acc[v].w);
-                    }
+                    acc.x = fmaf(w, x[u].x, acc.x);
+                    acc.y = fmaf(w, x[u].y, acc.y);
+                    acc.z = fmaf(w, x[u].z, acc.z);
+                    acc.w = fmaf(w, x[u].w, acc.w);
                 }
             }
         }
     }
     const float inverse = empty ? 0.f : 1.f / total;
-    E *to = static_cast<E *>(p.out) + out_row * L + lane * 4;
-#pragma unroll
-    for (int v = 0; v < kVecs; ++v) {
-        E four[4] = {latent_round<E>(empty ? 0.f : acc[v].x * inverse), latent_round<E>(empty ? 0.f : acc[v].y * inverse),
-                     latent_round<E>(empty ? 0.f : acc[v].z * inverse), latent_round<E>(empty ? 0.f : acc[v].w * inverse)};
-        *reinterpret_cast<uint2 *>(to + v * 128) = *reinterpret_cast<const uint2 *>(four);
-    }
-    if (p.lse && lane == 0) p.lse[out_row] = empty ? -INFINITY : top + logf(total);
+    E four[4] = {latent_round<E>(empty ? 0.f : acc.x * inverse), latent_round<E>(empty ? 0.f : acc.y * inverse),
+                 latent_round<E>(empty ? 0.f : acc.z * inverse), latent_round<E>(empty ? 0.f : acc.w * inverse)};
+    *reinterpret_cast<uint2 *>(static_cast<E *>(p.out) + out_row * L + d) = *reinterpret_cast<const uint2 *>(four);
+    if (p.lse && d == 0) p.lse[out_row] = empty ? -INFINITY : top + logf(total);
 }
 
 }  // namespace instinfer
