@@ -62,7 +62,9 @@ int instinfer_decode_attention_latent(void *out, float *lse, const void *q, cons
     const LatentRows r = latent_rows(rows);
     const LatentCut cut = latent_cut(r, batch, max_seq_len, latent_dim);
     if (!usable(workspace) || workspace_bytes < cut.bytes) return INSTINFER_ERR_WORKSPACE;
-    const int row_parts = (int)ceil_div(r.block_rows, kLatentMergeThreads / 32 / (latent_dim / 128));
+    // The merge in whole rows where there are more than 16 warps of 128 dims for every SM.
+    const int merge_dims = cut.items * r.block_rows * (latent_dim / 128) > 16 * (int64_t)sm_count() ? latent_dim : 128;
+    const int row_parts = (int)ceil_div(r.block_rows, kLatentMergeThreads / 32 / (latent_dim / merge_dims));
     if (cut.items * row_parts >= (int64_t)1 << 31 || cut.most_tiles >= (int64_t)1 << 31 || (int64_t)batch * s_max >= (int64_t)1 << 31)
         return INSTINFER_ERR_INVALID_ARG;
 
@@ -75,6 +77,7 @@ int instinfer_decode_attention_latent(void *out, float *lse, const void *q, cons
     p.seq_lens = seq_lens;
     p.block_table = block_table;
     p.status = status_flags;
+    p.cache = cache;
     p.out = out;
     p.lse = lse;
     unsigned char *start = static_cast<unsigned char *>(workspace);
@@ -89,6 +92,9 @@ int instinfer_decode_attention_latent(void *out, float *lse, const void *q, cons
     p.block_rows = r.block_rows;
     p.row_blocks = r.row_blocks;
     p.planes = r.planes;
+    p.teams = cut.teams;
+    p.tile_shift = cut.tile_shift;
+    p.item_cost = cut.item_cost;
     p.max_seq_len = max_seq_len;
     p.s_max = paged ? 0 : s_max;
     p.block_tokens = paged ? block_tokens : 0;
@@ -102,12 +108,13 @@ int instinfer_decode_attention_latent(void *out, float *lse, const void *q, cons
     p.scale_log2e = p.scale * 1.44269504088896340736f;
     const CUtensorMapDataType kind = type == INSTINFER_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     const int32_t dims = latent_dim + rope_dim;
-    if (!make_latent_map(&t.map_q, kind, q, dims, rows, batch, r.columns) ||
+    if (!make_latent_map(&t.map_q, kind, q, dims, rows, batch, r.columns ? r.columns : kPairRows) ||
         !make_latent_map(&t.map_cache, kind, cache, dims, cache_rows, 0, p.run_tokens))
         return INSTINFER_ERR_CUDA;
     t.grid = cut.grid;
     t.merge_grid = (unsigned)(cut.items * row_parts);
     t.row_parts = row_parts;
+    t.merge_dims = merge_dims;
     t.stream = static_cast<cudaStream_t>(cuda_stream);
     return type == INSTINFER_F16 ? launch_latent<__half>(latent_dim, r.columns, t) : launch_latent<__nv_bfloat16>(latent_dim, r.columns, t);
 }

@@ -42,13 +42,13 @@ constexpr int kLatentTile = 64;                          // tokens per tile
 constexpr int kLatentRope = 64;                          // turned dims
 constexpr int kLatentPanel = kLatentTile * 128;          // 64 dims of a tile
 constexpr int kLatentItem = 2 * kLatentPanel;            // 128 dims
-constexpr int kLatentItemCost = 3;                       // what a segment's set-up and end count in tiles
 
 struct LatentParams {
     TreeShape tree;              // mask == nullptr: a chain, node t sees nodes 0 .. t
     const int32_t *seq_lens;
     const int32_t *block_table;  // nullptr: contiguous
     int32_t *status;
+    const void *cache;
     void *out;                   // [batch, rows, L]
     float *lse;                  // nullable [batch, rows]
     float *part_o;               // [slots, block_rows, L]
@@ -62,6 +62,9 @@ struct LatentParams {
     int32_t block_rows;          // of a row block (the last one may have fewer)
     int32_t row_blocks;
     int32_t planes;
+    int32_t teams;               // blocks (or pairs of blocks) of a plane
+    int32_t tile_shift;          // tokens of a tile: 2^tile_shift
+    int32_t item_cost;           // what a segment's set-up and end count in tiles
     int32_t max_seq_len;
     int32_t s_max;
     int32_t block_tokens;
@@ -134,11 +137,11 @@ struct LatentSegment {
 };
 static_assert(sizeof(LatentSegment) == kLatSegmentBytes, "queue entry");
 
-__device__ __forceinline__ int latent_tiles(int len, int nodes)
+__device__ __forceinline__ int latent_tiles(const LatentParams &p, int len, int nodes)
 {
-    return nodes > 0 ? (int)(((unsigned)len + kLatentTile - 1) / kLatentTile) : 0;
+    return nodes > 0 ? (int)(((unsigned)len + (1u << p.tile_shift) - 1) >> p.tile_shift) : 0;
 }
-__device__ __forceinline__ int latent_weight(int tiles) { return tiles > 0 ? tiles + kLatentItemCost : 0; }
+__device__ __forceinline__ int latent_weight(const LatentParams &p, int tiles) { return tiles > 0 ? tiles + p.item_cost : 0; }
 // Row blocks of a sequence that a plane has: plane, plane + planes, ...
 __device__ __forceinline__ int latent_plane_items(const LatentParams &p, int plane) { return (p.row_blocks - plane + p.planes - 1) / p.planes; }
 
@@ -152,7 +155,7 @@ struct LatentFinder {
     {
         len = nodes = 0;
         if (w0 + lane < p.batch) len = checked_tree(p.tree, p.seq_lens, p.max_seq_len, nullptr, w0 + lane, false, nodes);
-        stop = latent_weight(latent_tiles(len, nodes)) * items;
+        stop = latent_weight(p, latent_tiles(p, len, nodes)) * items;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int up = __shfl_up_sync(0xffffffffu, stop, o);
@@ -161,16 +164,15 @@ struct LatentFinder {
         stop += start;
     }
     // The share of a plane of `total` tiles; the window lies at or before its first tile.
-    __device__ __forceinline__ void begin(int total)
+    __device__ __forceinline__ void begin(const LatentParams &p, int total)
     {
-        const int teams = gridDim.x / planes_of_grid, blocks = min(teams, total);
+        const int blocks = min(p.teams, total);
         tile = end = total;
         if (team >= blocks) return;
         const int length = total / blocks, longer = total - length * blocks;       // (the first `longer` shares are one tile longer)
         tile = length * team + min(team, longer);
         end = tile + length + (team < longer ? 1 : 0);
     }
-    int planes_of_grid;
     template <typename E, int L>
     __device__ __noinline__ LatentSegment next(const LatentParams &p, int lane)
     {
@@ -190,12 +192,12 @@ struct LatentFinder {
             const int before = __shfl_sync(0xffffffffu, stop, max(at - 1, 0));
             s.len = __shfl_sync(0xffffffffu, len, at);
             s.nodes = __shfl_sync(0xffffffffu, nodes, at);
-            s.n_tiles = latent_tiles(s.len, s.nodes);
-            const int weight = latent_weight(s.n_tiles), inside = tile - (at == 0 ? start : before), item = items == 1 ? 0 : inside / weight;
+            s.n_tiles = latent_tiles(p, s.len, s.nodes);
+            const int weight = latent_weight(p, s.n_tiles), inside = tile - (at == 0 ? start : before), item = items == 1 ? 0 : inside / weight;
             const int from = inside - item * weight, to = min(weight, from + (end - tile));
-            const int rb = plane + item * planes_of_grid;
-            s.t0 = max(0, from - kLatentItemCost);
-            s.t1 = to - kLatentItemCost;
+            const int rb = plane + item * p.planes;
+            s.t0 = max(0, from - p.item_cost);
+            s.t1 = to - p.item_cost;
             tile += to - from;
             if (s.t1 <= s.t0) continue;               // only of the item's extra weight
             s.b = w0 + at;
@@ -208,7 +210,7 @@ struct LatentFinder {
                 if (s.t1 == s.n_tiles) of_item->y = team;
             }
             // (what starts inside an item goes to its block's first slot, what ends inside one to its second)
-            s.slot = 2 * (plane + team * planes_of_grid) + (s.t0 == 0 ? 1 : 0);
+            s.slot = 2 * (plane + team * p.planes) + (s.t0 == 0 ? 1 : 0);
             const int64_t row = (int64_t)s.b * p.rows + s.row0, slot_row = (int64_t)s.slot * p.block_rows;
             s.out = s.whole() ? static_cast<void *>(static_cast<E *>(p.out) + row * L) : static_cast<void *>(p.part_o + slot_row * L);
             s.lse = !s.whole() ? p.part_lse + slot_row : p.lse ? p.lse + row : nullptr;
@@ -227,7 +229,7 @@ __device__ __forceinline__ void latent_scan(const LatentParams &p, unsigned char
     for (int b = b0; b < min(b0 + per, p.batch); ++b) {
         int nodes;
         const int len = checked_tree(p.tree, p.seq_lens, p.max_seq_len, p.status, b, blockIdx.x == 0, nodes);
-        mine += latent_weight(latent_tiles(len, nodes)) * items;
+        mine += latent_weight(p, latent_tiles(p, len, nodes)) * items;
     }
     int sum = mine;
 #pragma unroll
@@ -245,9 +247,8 @@ __device__ __forceinline__ void latent_scan(const LatentParams &p, unsigned char
     }
     before += sum - mine;
     LatentFinder share;
-    share.planes_of_grid = p.planes;
     share.team = team;
-    share.begin(total);
+    share.begin(p, total);
     int *found = reinterpret_cast<int *>(misc_ptr + kLatTotal);
     if (threadIdx.x == 0) found[0] = total;
     if (share.tile < share.end && before <= share.tile && share.tile < before + mine) {
@@ -256,6 +257,15 @@ __device__ __forceinline__ void latent_scan(const LatentParams &p, unsigned char
     }
 }
 
+// Lane i (row >= 0): brings the T cache rows from `row` on into L2.  (A hint: nothing waits for it.)
+__device__ __forceinline__ void latent_prefetch(const LatentParams &p, int row, int T, int row_bytes)
+{
+    if (row < 0) return;
+    const int64_t rows = min((int64_t)T, p.cache_rows - row);
+    if (rows > 0)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;"
+                     :: "l"(static_cast<const char *>(p.cache) + (int64_t)row * row_bytes), "r"((unsigned)rows * (unsigned)row_bytes) : "memory");
+}
 __device__ __forceinline__ void tma_load_3d(unsigned dst, const CUtensorMap *map, int x, int y, int z, unsigned bar)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
@@ -382,7 +392,6 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
     };
 
     LatentFinder finder;               // (of the copying warp)
-    finder.planes_of_grid = p.planes;
     finder.plane = blockIdx.x % p.planes;
     finder.team = blockIdx.x / p.planes;
     finder.items = latent_plane_items(p, finder.plane);
@@ -400,7 +409,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
             int nodes;
             (void)checked_tree(p.tree, p.seq_lens, p.max_seq_len, p.status, lane, true, nodes);
         }
-        finder.begin(__shfl_sync(0xffffffffu, finder.stop, 31));
+        finder.begin(p, __shfl_sync(0xffffffffu, finder.stop, 31));
         seg = finder.template next<E, L>(p, lane);
     } else if (warp == kWarpOutput && lane == 0) {
         for (int s = 0; s < 12; ++s) {
@@ -434,7 +443,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
         const int T = p.run_tokens;
         if (p.batch > 32) {
             const int *found = reinterpret_cast<const int *>(misc_ptr + kLatTotal);
-            finder.begin(found[0]);
+            finder.begin(p, found[0]);
             if (finder.tile < finder.end) {
                 finder.w0 = found[1];
                 finder.start = found[2];
@@ -444,7 +453,8 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
         }
         int g = 0, k = 0;                                 // tiles and segments so far
         bool fine = true;
-        // lane i: the physical block of the i-th run of tile j (asked for one tile ahead)
+        // lane i: the physical block of the i-th run of tile j (asked for one tile ahead; bringing the next tile into L2 meanwhile,
+        // as the pairs' kernel does, costs 12 % here: 64 sequences of 4k-16k, 16 heads, 159 us against 140)
         auto fetch_ids = [&](const LatentSegment &s, int j) -> int {
             if (!paged) return 0;
             const int start = j * kLatentTile;
@@ -908,26 +918,27 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
 }
 
 // Joins the partial results of the items that more than one share has a part of, and zeroes the rows of sequences
-// without work.  A warp takes 128 dims of one row, so that the partials of an item of some shares are few rounds of loads:
-// the kernel is a chain of those (the item's shares, their log-sum-exps, the partials).
+// without work.  A warp takes kDims dims of one row: the kernel is a chain of loads (the item's shares, their
+// log-sum-exps, the partials), so few rows are cut into 128 dims each, whose partials are few rounds of loads, while
+// whole rows leave the fewest warps where there are more than fit the GPU at once.
 constexpr int kLatentMergeThreads = 256;
-constexpr int kLatentMergeDeep = 8;
 
-template <typename E, int L>
+template <typename E, int L, int kDims>
 __global__ void __launch_bounds__(kLatentMergeThreads)
 latent_merge_kernel(const LatentParams p, int row_parts)
 {
-    constexpr int kRows = kLatentMergeThreads / 32 / (L / 128);       // rows of a block
+    constexpr int kPieces = L / kDims, kRows = kLatentMergeThreads / 32 / kPieces;      // warps of a row, rows of a block
+    constexpr int kVecs = kDims / 128, kDeep = 8 / kVecs;             // a lane's dims: kVecs runs of four; partials in flight
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int part = blockIdx.x % row_parts, item = blockIdx.x / row_parts;           // (sequence, row block)
     const int b = item / p.row_blocks, rb = item - b * p.row_blocks;
-    const int r = part * kRows + warp / (L / 128), row = rb * p.block_rows + r, d = warp % (L / 128) * 128 + lane * 4;
+    const int r = part * kRows + warp / kPieces, row = rb * p.block_rows + r, d = warp % kPieces * kDims + lane * 4;
     allow_next_kernel();
     wait_for_previous_kernels();
     int nodes;
     const int2 shares = p.item_shares[item];
     const int len = checked_tree(p.tree, p.seq_lens, p.max_seq_len, nullptr, b, false, nodes);
-    const int c0 = shares.x, n = latent_tiles(len, nodes) > 0 ? shares.y - c0 + 1 : 0;
+    const int c0 = shares.x, n = latent_tiles(p, len, nodes) > 0 ? shares.y - c0 + 1 : 0;
     if (n == 1) return;                                               // one share had it all: the result is written
     if (r >= p.block_rows || row >= p.rows) return;
     const int64_t out_row = (int64_t)b * p.rows + row;
@@ -945,32 +956,44 @@ latent_merge_kernel(const LatentParams p, int row_parts)
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const bool empty = !(top > kMinusHuge) && !__any_sync(0xffffffffu, any_nan);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 acc[kVecs];
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i0 = 0; i0 < n && !empty; i0 += 32) {
         const float lse = i0 == 0 ? first_lse : i0 + lane < n ? p.part_lse[slot_row(i0 + lane)] : kMinusHuge;
         const float mine = i0 + lane < n ? fast_exp2((lse - top) * 1.44269504088896340736f) : 0.f;
         const int here = min(32, n - i0);
-        for (int i = 0; i < here; i += kLatentMergeDeep) {
-            float4 x[kLatentMergeDeep];
+        for (int i = 0; i < here; i += kDeep) {
+            float4 x[kDeep][kVecs];
 #pragma unroll
-            for (int u = 0; u < kLatentMergeDeep; ++u) x[u] = i + u < here ? *reinterpret_cast<const float4 *>(p.part_o + slot_row(i0 + i + u) * L + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int u = 0; u < kDeep; ++u) {
 #pragma unroll
-            for (int u = 0; u < kLatentMergeDeep; ++u) {
+                for (int v = 0; v < kVecs; ++v)
+                    x[u][v] = i + u < here ? *reinterpret_cast<const float4 *>(p.part_o + slot_row(i0 + i + u) * L + d + v * 128) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) {
                 const float w = __shfl_sync(0xffffffffu, mine, (i + u) & 31);
                 if (i + u < here) {
                     total += w;
-                    acc.x = fmaf(w, x[u].x, acc.x);
-                    acc.y = fmaf(w, x[u].y, acc.y);
-                    acc.z = fmaf(w, x[u].z, acc.z);
-                    acc.w = fmaf(w, x[u].w, acc.w);
+#pragma unroll
+                    for (int v = 0; v < kVecs; ++v) {
+                        acc[v].x = fmaf(w, x[u][v].x, acc[v].x);
+                        acc[v].y = fmaf(w, x[u][v].y, acc[v].y);
+                        acc[v].z = fmaf(w, x[u][v].z, acc[v].z);
+                        acc[v].w = fmaf(w, x[u][v].w, acc[v].w);
+                    }
                 }
             }
         }
     }
     const float inverse = empty ? 0.f : 1.f / total;
-    E four[4] = {latent_round<E>(empty ? 0.f : acc.x * inverse), latent_round<E>(empty ? 0.f : acc.y * inverse),
-                 latent_round<E>(empty ? 0.f : acc.z * inverse), latent_round<E>(empty ? 0.f : acc.w * inverse)};
-    *reinterpret_cast<uint2 *>(static_cast<E *>(p.out) + out_row * L + d) = *reinterpret_cast<const uint2 *>(four);
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+        const E four[4] = {latent_round<E>(empty ? 0.f : acc[v].x * inverse), latent_round<E>(empty ? 0.f : acc[v].y * inverse),
+                           latent_round<E>(empty ? 0.f : acc[v].z * inverse), latent_round<E>(empty ? 0.f : acc[v].w * inverse)};
+        *reinterpret_cast<uint2 *>(static_cast<E *>(p.out) + out_row * L + d + v * 128) = *reinterpret_cast<const uint2 *>(four);
+    }
     if (p.lse && d == 0) p.lse[out_row] = empty ? -INFINITY : top + logf(total);
 }
 
