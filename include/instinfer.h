@@ -323,7 +323,7 @@ int instinfer_rope_append(void *q_out, void *k_cache, void *v_cache, const void 
  * with a block table; fp16 or bf16 (`type`, the same for every tensor of a call but lse).
  * The calls that share, grow and move whole blocks (instinfer_kv_fork, instinfer_kv_resize, instinfer_kv_defragment) take such pools
  * as pools of (latent_dim + rope_dim) / 64 heads of 64, half of the layers as K and half as V pools (same block bytes).
- * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): latent_dim 256 or 512, rope_dim 64; paged block_tokens a multiple of 8.
+ * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): latent_dim 512, rope_dim 64; paged block_tokens a multiple of 8.
  *
  * instinfer_latent_append: the new tokens' rows, with the key part turned, and the queries' turned parts.
  *   q_out      [batch, max_new, q_heads, latent_dim + rope_dim], the absorbed queries: the last rope_dim values of the rows of

@@ -375,38 +375,40 @@ def rope_frequencies(rope_dim: int, base: float = 10000.0, scaling: str = "plain
     return torch.tensor(list(pairs), dtype=torch.float64, device=device), magnitude.value
 
 
-def _token_stride(t: torch.Tensor) -> int:
-    """Elements from one token of t [B, N, ...] to the next, all B * N of them evenly spaced."""
-    B, N = t.shape[:2]
-    if B == 1 and N == 1:
-        return 1 << 32                 # (never taken: any stride that the library accepts will do)
-    stride = t.stride(1) if N > 1 else t.stride(0)
-    if B > 1 and N > 1 and t.stride(0) != N * stride:
-        raise InstInferError(ERR_INVALID_ARG)
-    return stride
+# (The calls below are short next to Python's part of them: shapes and strides are asked for once, and devices, types
+# and addresses in passes in C.)
+_device_of, _type_of, _address_of, _is_contiguous = (torch.Tensor.get_device, torch.Tensor.dtype.__get__, torch.Tensor.data_ptr,
+                                                     torch.Tensor.is_contiguous)
 
 
-def _cache_shape(tokens: int, cache: torch.Tensor, block_table: Optional[torch.Tensor], batch: int):
-    """(s_max, block_tokens, max_blocks, blocks) of a cache whose dim `tokens` counts tokens; refuses one with too few sequences."""
-    if block_table is None:
-        if cache.shape[0] < batch:
-            raise InstInferError(ERR_INVALID_ARG)
-        return cache.shape[tokens], 0, 0, 0
-    if block_table.shape[0] < batch or not block_table.is_contiguous():
+def _token_stride(shape, strides) -> int:
+    """Elements from one token of a tensor [B, N, ...] to the next, all B * N of them evenly spaced."""
+    if shape[1] == 1:
+        # (one token in all: any stride that the library accepts will do)
+        return strides[0] if shape[0] > 1 else 1 << 32
+    if shape[0] > 1 and strides[0] != shape[1] * strides[1]:
         raise InstInferError(ERR_INVALID_ARG)
-    return 0, cache.shape[tokens], block_table.shape[1], cache.shape[0]
+    return strides[1]
 
 
 def _check_append(batch: int, max_new: int, frequencies: torch.Tensor, seq_lens: torch.Tensor, new_lens: Optional[torch.Tensor],
-                  positions: Optional[torch.Tensor]) -> None:
-    """What the two turning appends ask of their small tensors."""
-    if frequencies.dtype != torch.float64 or not frequencies.is_contiguous() or seq_lens.numel() < batch or \
-            (new_lens is not None and new_lens.numel() < batch) or \
-            (positions is not None and (positions.shape != (batch, max_new) or not positions.is_contiguous())):
+                  block_table: Optional[torch.Tensor], positions: Optional[torch.Tensor], tokens: int, shape):
+    """What the two turning appends ask of their small tensors, for a cache of this shape whose dim `tokens` counts tokens;
+    (s_max, block_tokens, max_blocks, blocks)."""
+    ints = [t for t in (seq_lens, new_lens, positions, block_table) if t is not None]
+    if frequencies.dtype is not torch.float64 or set(map(_type_of, ints)) != {torch.int32} or \
+            not all(map(_is_contiguous, (frequencies, *ints))) or len(seq_lens) < batch or \
+            (new_lens is not None and len(new_lens) < batch) or \
+            (positions is not None and positions.shape != (batch, max_new)):
         raise InstInferError(ERR_INVALID_ARG)
-    for t in (seq_lens, new_lens, positions):
-        if t is not None and t.dtype != torch.int32:
+    if block_table is None:
+        if shape[0] < batch:
             raise InstInferError(ERR_INVALID_ARG)
+        return shape[tokens], 0, 0, 0
+    sequences, max_blocks = block_table.shape
+    if sequences < batch:
+        raise InstInferError(ERR_INVALID_ARG)
+    return 0, shape[tokens], max_blocks, shape[0]
 
 
 def rope_append(q_out: Optional[torch.Tensor], k_cache: torch.Tensor, v_cache: torch.Tensor, q: Optional[torch.Tensor],
@@ -417,28 +419,33 @@ def rope_append(q_out: Optional[torch.Tensor], k_cache: torch.Tensor, v_cache: t
     """instinfer_rope_append: q [B, N, Hq, D] (None: keys and values only), k_new and v_new [B, N, H, D] in fp32, fp16 or
     bf16, slices of one projection if need be; q_out fp16 as q; frequencies fp64 [rope_dim / 2]; caches fp16 [B, H, s_max, D]
     or pools [P, H, T, D] with block_table; positions int32 [B, N]."""
-    batch, max_new, heads, head_dim = k_new.shape
+    shape = k_new.shape
+    batch, max_new, heads, head_dim = shape
+    cache = k_cache.shape
     here = _here(q_out, k_cache, v_cache, q, k_new, v_new, frequencies, seq_lens, new_lens, block_table, positions, status_flags)
-    if k_cache.shape != v_cache.shape or k_cache.shape[1] != heads or k_cache.shape[3] != head_dim or v_new.shape != k_new.shape or \
-            (q is None) != (q_out is None) or not (k_cache.is_contiguous() and v_cache.is_contiguous()) or \
-            k_cache.dtype != torch.float16 or v_cache.dtype != torch.float16:
-        raise InstInferError(ERR_INVALID_ARG)
-    if k_new.dtype not in _TYPES:
+    kind = k_new.dtype
+    if kind not in _TYPES:
         raise InstInferError(ERR_UNSUPPORTED)
-    q_heads = 0
+    if v_cache.shape != cache or cache[1] != heads or cache[3] != head_dim or v_new.shape != shape or v_new.dtype is not kind or \
+            (q is None) != (q_out is None) or not (k_cache.is_contiguous() and v_cache.is_contiguous()) or \
+            k_cache.dtype is not torch.float16 or v_cache.dtype is not torch.float16:
+        raise InstInferError(ERR_INVALID_ARG)
+    k_strides, v_strides = k_new.stride(), v_new.stride()
+    if k_strides[3] != 1 or v_strides[3] != 1 or (heads > 1 and (k_strides[2] != head_dim or v_strides[2] != head_dim)):
+        raise InstInferError(ERR_INVALID_ARG)
+    q_heads = q_stride = 0
     if q is not None:
-        q_heads = q.shape[2]
-        if q.shape != (batch, max_new, q_heads, head_dim) or q_out.shape != q.shape or q_out.dtype != torch.float16 or not q_out.is_contiguous():
+        q_shape, q_strides = q.shape, q.stride()
+        q_heads = q_shape[2]
+        if q_shape != (batch, max_new, q_heads, head_dim) or q_out.shape != q_shape or q.dtype is not kind or \
+                q_out.dtype is not torch.float16 or not q_out.is_contiguous() or q_strides[3] != 1 or (q_heads > 1 and q_strides[2] != head_dim):
             raise InstInferError(ERR_INVALID_ARG)
-    for t in (q, k_new, v_new):
-        if t is not None and (t.dtype != k_new.dtype or t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != head_dim)):
-            raise InstInferError(ERR_INVALID_ARG)
-    _check_append(batch, max_new, frequencies, seq_lens, new_lens, positions)
-    s_max, block_tokens, max_blocks, phys = _cache_shape(2, k_cache, block_table, batch)
+        q_stride = _token_stride(q_shape, q_strides)
+    s_max, block_tokens, max_blocks, phys = _check_append(batch, max_new, frequencies, seq_lens, new_lens, block_table, positions, 2, cache)
     _check(load().instinfer_rope_append(
-        _ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(q), k_new.data_ptr(), v_new.data_ptr(), _TYPES[k_new.dtype],
-        0 if q is None else _token_stride(q), _token_stride(k_new), _token_stride(v_new), frequencies.data_ptr(), 2 * frequencies.numel(),
-        int(interleaved), float(magnitude), _ptr(positions), seq_lens.data_ptr(), _ptr(new_lens), _ptr(block_table), max_blocks,
+        _ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(q), k_new.data_ptr(), v_new.data_ptr(), _TYPES[kind],
+        q_stride, _token_stride(shape, k_strides), _token_stride(shape, v_strides), frequencies.data_ptr(), 2 * len(frequencies),
+        interleaved, magnitude, _ptr(positions), seq_lens.data_ptr(), _ptr(new_lens), _ptr(block_table), max_blocks,
         block_tokens, phys, batch, max_new, q_heads, heads, head_dim, s_max, _ptr(status_flags), _stream(stream, here)))
 
 
@@ -450,29 +457,32 @@ def latent_append(q_out: Optional[torch.Tensor], cache: torch.Tensor, q_rope: Op
     """instinfer_latent_append: latent_new [B, N, L], rope_new [B, N, R], q_rope [B, N, H, R] (None: the cache's rows only),
     slices of projections if need be; q_out [B, N, H, L + R]; cache [B, s_max, L + R] or a pool [P, T, L + R] with
     block_table; all fp16 or all bf16."""
-    batch, max_new, latent_dim = latent_new.shape
-    rope_dim = rope_new.shape[2]
+    shape, rope_shape, cache_shape = latent_new.shape, rope_new.shape, cache.shape
+    batch, max_new, latent_dim = shape
+    rope_dim = rope_shape[2]
     here = _here(q_out, cache, q_rope, latent_new, rope_new, frequencies, seq_lens, new_lens, block_table, positions, status_flags)
-    if rope_new.shape[:2] != latent_new.shape[:2] or cache.shape[2] != latent_dim + rope_dim or not cache.is_contiguous() or \
-            (q_rope is None) != (q_out is None) or frequencies.numel() * 2 != rope_dim or latent_new.stride(2) != 1 or rope_new.stride(2) != 1:
-        raise InstInferError(ERR_INVALID_ARG)
-    q_heads, head_stride = 0, 0
-    if q_rope is not None:
-        q_heads = q_rope.shape[2]
-        head_stride = q_rope.stride(2) if q_heads > 1 else rope_dim
-        if q_rope.shape != (batch, max_new, q_heads, rope_dim) or q_out.shape != (batch, max_new, q_heads, latent_dim + rope_dim) or \
-                q_rope.stride(3) != 1 or not q_out.is_contiguous():
-            raise InstInferError(ERR_INVALID_ARG)
-    if latent_new.dtype not in _TYPES:
+    kind = latent_new.dtype
+    if kind not in _TYPES:
         raise InstInferError(ERR_UNSUPPORTED)
-    if any(t is not None and t.dtype != latent_new.dtype for t in (q_out, cache, q_rope, rope_new)):
+    strides, rope_strides = latent_new.stride(), rope_new.stride()
+    if rope_shape[:2] != shape[:2] or cache_shape[2] != latent_dim + rope_dim or not cache.is_contiguous() or \
+            (q_rope is None) != (q_out is None) or len(frequencies) * 2 != rope_dim or strides[2] != 1 or rope_strides[2] != 1 or \
+            cache.dtype is not kind or rope_new.dtype is not kind:
         raise InstInferError(ERR_INVALID_ARG)
-    _check_append(batch, max_new, frequencies, seq_lens, new_lens, positions)
-    s_max, block_tokens, max_blocks, phys = _cache_shape(1, cache, block_table, batch)
+    q_heads = q_stride = head_stride = 0
+    if q_rope is not None:
+        q_shape, q_strides = q_rope.shape, q_rope.stride()
+        q_heads = q_shape[2]
+        head_stride = q_strides[2] if q_heads > 1 else rope_dim
+        if q_shape != (batch, max_new, q_heads, rope_dim) or q_out.shape != (batch, max_new, q_heads, latent_dim + rope_dim) or \
+                q_strides[3] != 1 or not q_out.is_contiguous() or q_rope.dtype is not kind or q_out.dtype is not kind:
+            raise InstInferError(ERR_INVALID_ARG)
+        q_stride = _token_stride(q_shape, q_strides)
+    s_max, block_tokens, max_blocks, phys = _check_append(batch, max_new, frequencies, seq_lens, new_lens, block_table, positions, 1, cache_shape)
     _check(load().instinfer_latent_append(
-        _ptr(q_out), cache.data_ptr(), _ptr(q_rope), latent_new.data_ptr(), rope_new.data_ptr(), _TYPES[latent_new.dtype],
-        0 if q_rope is None else _token_stride(q_rope), head_stride, _token_stride(latent_new), _token_stride(rope_new),
-        frequencies.data_ptr(), int(interleaved), float(magnitude), _ptr(positions), seq_lens.data_ptr(), _ptr(new_lens),
+        _ptr(q_out), cache.data_ptr(), _ptr(q_rope), latent_new.data_ptr(), rope_new.data_ptr(), _TYPES[kind],
+        q_stride, head_stride, _token_stride(shape, strides), _token_stride(rope_shape, rope_strides),
+        frequencies.data_ptr(), interleaved, magnitude, _ptr(positions), seq_lens.data_ptr(), _ptr(new_lens),
         _ptr(block_table), max_blocks, block_tokens, phys, batch, max_new, q_heads, latent_dim, rope_dim, s_max,
         _ptr(status_flags), _stream(stream, here)))
 
@@ -489,22 +499,28 @@ def decode_attention_latent(out: torch.Tensor, lse: Optional[torch.Tensor], q: t
     """instinfer_decode_attention_latent: q [B, N, H, L + R], out [B, N, H, L], lse [B, N, H]; cache [B, s_max, L + R] or a pool
     [P, T, L + R] with block_table; mask as tree_mask writes it, or None for a chain; all fp16 or all bf16."""
     batch, q_tokens, q_heads, dims = q.shape
-    latent_dim = out.shape[3]
+    out_shape, cache_shape = out.shape, cache.shape
+    latent_dim = out_shape[3]
     here = _here(out, lse, q, cache, block_table, seq_lens, tree_lens, mask, workspace, status_flags)
-    if out.shape != (batch, q_tokens, q_heads, latent_dim) or cache.shape[2] != dims or seq_lens.numel() < batch or \
-            (lse is not None and (lse.numel() != batch * q_tokens * q_heads or lse.dtype != torch.float32 or not lse.is_contiguous())) or \
-            (tree_lens is not None and (tree_lens.numel() < batch or tree_lens.dtype != torch.int32)) or seq_lens.dtype != torch.int32 or \
-            (mask is not None and (mask.numel() < batch * q_tokens * ((q_tokens + 63) // 64) or mask.dtype != torch.int64)) or \
-            not (out.is_contiguous() and q.is_contiguous() and cache.is_contiguous()):
-        raise InstInferError(ERR_INVALID_ARG)
-    if q.dtype not in _TYPES:
+    kind = q.dtype
+    if kind not in _TYPES:
         raise InstInferError(ERR_UNSUPPORTED)
-    if out.dtype != q.dtype or cache.dtype != q.dtype:
+    ints = [t for t in (seq_lens, tree_lens, block_table) if t is not None]
+    if out_shape != (batch, q_tokens, q_heads, latent_dim) or cache_shape[2] != dims or out.dtype is not kind or cache.dtype is not kind or \
+            len(seq_lens) < batch or (tree_lens is not None and len(tree_lens) < batch) or set(map(_type_of, ints)) != {torch.int32} or \
+            not all(map(_is_contiguous, (out, q, cache, *ints))) or \
+            (lse is not None and (lse.numel() != batch * q_tokens * q_heads or lse.dtype is not torch.float32 or not lse.is_contiguous())) or \
+            (mask is not None and (mask.numel() < batch * q_tokens * ((q_tokens + 63) // 64) or mask.dtype is not torch.int64 or not mask.is_contiguous())):
         raise InstInferError(ERR_INVALID_ARG)
-    s_max, block_tokens, max_blocks, phys = _cache_shape(1, cache, block_table, batch)
+    if block_table is None:
+        sequences, s_max, block_tokens, max_blocks, phys = cache_shape[0], cache_shape[1], 0, 0, 0
+    else:
+        (sequences, max_blocks), (phys, block_tokens, _), s_max = block_table.shape, cache_shape, 0
+    if sequences < batch:
+        raise InstInferError(ERR_INVALID_ARG)
     _check(load().instinfer_decode_attention_latent(
         out.data_ptr(), _ptr(lse), q.data_ptr(), cache.data_ptr(), _ptr(block_table), seq_lens.data_ptr(), _ptr(tree_lens), _ptr(mask),
-        _TYPES[q.dtype], batch, q_tokens, q_heads, latent_dim, dims - latent_dim, s_max, block_tokens, max_blocks, phys,
+        _TYPES[kind], batch, q_tokens, q_heads, latent_dim, dims - latent_dim, s_max, block_tokens, max_blocks, phys,
         int(max_seq_len), float(scale), workspace.data_ptr(), workspace.nbytes, _ptr(status_flags), _stream(stream, here)))
 
 

@@ -210,7 +210,7 @@ inline size_t workspace_for(int64_t pairs, const SplitPlan &plan)
 inline bool append_head_dim_ok(int32_t head_dim) { return head_dim == 64 || head_dim == 128 || head_dim == 256; }
 
 // Widths of a latent cache's row that the latent calls take.
-inline bool latent_dims_ok(int32_t latent_dim, int32_t rope_dim) { return (latent_dim == 256 || latent_dim == 512) && rope_dim == 64; }
+inline bool latent_dims_ok(int32_t latent_dim, int32_t rope_dim) { return latent_dim == 512 && rope_dim == 64; }
 
 inline bool sizes_ok(int32_t batch, int32_t heads, int32_t max_seq_len)
 {

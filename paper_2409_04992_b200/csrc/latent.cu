@@ -116,7 +116,7 @@ int instinfer_decode_attention_latent(void *out, float *lse, const void *q, cons
     t.row_parts = row_parts;
     t.merge_dims = merge_dims;
     t.stream = static_cast<cudaStream_t>(cuda_stream);
-    return type == INSTINFER_F16 ? launch_latent<__half>(latent_dim, r.columns, t) : launch_latent<__nv_bfloat16>(latent_dim, r.columns, t);
+    return type == INSTINFER_F16 ? launch_latent<__half>(r.columns, t) : launch_latent<__nv_bfloat16>(r.columns, t);
 }
 
 size_t instinfer_latent_workspace_bytes(int32_t batch, int32_t q_tokens, int32_t q_heads, int32_t latent_dim, int32_t rope_dim,

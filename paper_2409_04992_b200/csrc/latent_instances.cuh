@@ -46,10 +46,9 @@ int launch_latent_pairs(const LatentLaunch &t)
 }
 
 template <typename E>
-int launch_latent(int32_t latent_dim, int32_t columns, const LatentLaunch &t)
+int launch_latent(int32_t columns, const LatentLaunch &t)
 {
-    if (latent_dim == 512) return columns == 16 ? launch_latent_tokens<E, 512, 16>(t) : columns == 32 ? launch_latent_tokens<E, 512, 32>(t) : launch_latent_pairs<E, 512>(t);
-    return columns == 16 ? launch_latent_tokens<E, 256, 16>(t) : columns == 32 ? launch_latent_tokens<E, 256, 32>(t) : launch_latent_pairs<E, 256>(t);
+    return columns == 16 ? launch_latent_tokens<E, 512, 16>(t) : columns == 32 ? launch_latent_tokens<E, 512, 32>(t) : launch_latent_pairs<E, 512>(t);
 }
 
 }  // namespace api

@@ -96,13 +96,13 @@ static_assert(kLatSegments + 4 * kLatSegmentBytes <= kLatMiscBytes && kLatScan +
 
 template <int L, int N>
 struct LatentGeometry {
-    static_assert((L == 256 || L == 512) && (N == 16 || N == 32 || N == 64), "instances");
+    static_assert(L == 512 && (N == 16 || N == 32), "instances");
     static constexpr int kPanels = L / 64;                               // latent panels of a tile; the turned part is one more
     static constexpr int kItems = L / 128;
     static constexpr int kQPanel = N * 128;
     static constexpr int kQBytes = (kPanels + 1) * kQPanel;
     static constexpr int kPPart = N * kLatentTile * 2;                   // weights of a tile: high parts, then low parts
-    static constexpr int kGroups = N == 64 ? 2 : 1;
+    static constexpr int kGroups = 1;
     static constexpr int kCols = N / kGroups;                            // rows of a group of softmax warps
     static constexpr int kThreads = (4 * kGroups + 3) * 32;
     static constexpr int kExtraBytes = kLatMiscBytes + N * 20;           // a row's numbers by warp, and its reference

@@ -60,7 +60,7 @@ struct LatentLaunch {
 };
 
 template <typename E>
-int launch_latent(int32_t latent_dim, int32_t columns, const LatentLaunch &t);
+int launch_latent(int32_t columns, const LatentLaunch &t);
 
 }  // namespace api
 }  // namespace instinfer

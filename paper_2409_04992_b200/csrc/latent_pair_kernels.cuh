@@ -54,7 +54,7 @@ static_assert(kPairScan - kPairTotal == kLatScan - kLatTotal && kPairSegments + 
 
 template <int L>
 struct PairGeometry {
-    static_assert(L == 256 || L == 512, "instances");
+    static_assert(L == 512, "instances");
     static constexpr int kPanels = L / 64 + 1;                           // key panels of a tile, the turned part the last
     static constexpr int kParts = L / 256;                               // 128-dim parts of a block's half of the dims
     // Large items, because an item's wait and commit cost the issuers 0.2 us whatever its size (with keys by the panel that
@@ -68,7 +68,8 @@ struct PairGeometry {
     static constexpr int kMiscOffset = kPOffset + 4 * kPairPanel;
     static constexpr int kSmemBytes = kMiscOffset + kPairMiscBytes + 1024;
     static constexpr int kOColumn = 128;                                 // two logit buffers of 64 columns, then the output
-    static constexpr int kTmemCols = kOColumn + L / 2 > 256 ? 512 : 256;
+    static constexpr int kTmemCols = 512;
+    static_assert(kOColumn + (kParts - 1) * 128 + 256 <= kTmemCols, "tensor memory");
     static_assert(kSmemBytes <= 227 * 1024, "one block per SM must fit");
 };
 
