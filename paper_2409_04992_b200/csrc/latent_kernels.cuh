@@ -6,13 +6,13 @@
 //   out[r] = softmax_i(scale q[r] . [c_i, k_i]) . c_i
 // so R = new tokens x heads query rows share every byte of the cache: 2 R (2 L + 64) operations for 2 (L + 64) bytes.
 //
-// The TOKENS are the long side of the MMAs, N = 16, 32 or 64 rows the short one, and both products read the one tile of
+// The TOKENS are the long side of the MMAs, N = 16 or 32 rows the short one, and both products read the one tile of
 // 64 tokens that lies in shared memory, row-major for the first and column-major for the second:
 //   S^T[64 tokens x N]     = tile[64 x (L + 64)] Q^T[(L + 64) x N]
 //   O^T[128 dims x N] (L / 128 accumulators) += tile^T[128 x 64] P^T[64 x N]
-// More than 64 rows are cut into row blocks of equal size.  The blocks of a row of SMs ("plane") take one row block
-// each: their tiles are cut alike, so that the blocks of all planes that work on the same tokens run at about the same
-// time and all but the first find them in L2.
+// More than 32 rows take pairs of SMs (latent_pair_kernels.cuh).  Those cut more than 128 rows into row blocks; the pairs of a
+// "plane" take one row block each, their tiles cut alike, so that the pairs of all planes that work on the same tokens run
+// at about the same time and all but the first find them in L2.
 //
 // Work split: a plane's tiles, item after item (an item is a row block of a sequence), lie in one row that is cut into
 // equal shares, one per block.  Only the items that a share starts or ends inside leave partial results, two per block at
@@ -20,8 +20,11 @@
 // times as large and each of its segments costs some three tiles; 128 sequences of 16k, 16 heads: 408 us with equal
 // shares, 465 with four drawn pieces a block.)  An item counts some tiles more than it has, for its segment's set-up.
 //
-// A block has softmax warps (four, or two groups of four with half of the rows each) and three single-purpose warps that
-// hand tiles over through mbarriers, as in the kernels for draft trees:
+// Measured: 16 rows, 64 sequences of 4k to 16k tokens in 64-token pages 140 us (5.4 TB/s), 128 of 16k 412 us (5.9 TB/s); 32 rows,
+// 32 sequences of 8k 71 us; one sequence of 1000 tokens 14 us, a chain of set-up, one tile and the merge.
+//
+// A block has four softmax warps and three single-purpose warps that hand tiles over through mbarriers, as in the kernels
+// for draft trees:
 //   producer                 finds the share's segments (its parts of items), announces them through a queue in shared
 //                            memory, copies tiles (64-dim panels by tensor-map copies, 128-byte swizzle) and query rows;
 //   logit and output issuer  one elected thread each issues the MMAs.  An item (128 dims of the tile) goes back to the producer as
@@ -115,10 +118,8 @@ struct LatentGeometry {
     static constexpr int kPOffset = kQOffset + kQBytes;
     static constexpr int kMiscOffset = kPOffset + 2 * kPPart;
     static constexpr int kSmemBytes = kMiscOffset + kExtraBytes + 1024;  // room to align to 1024 bytes
-    // Up to 32 rows the low parts are further columns of the same MMAs, whose time is that of reading the tile; 64 rows
-    // have no columns of tensor memory left for that, and their low parts are MMAs of their own into the same accumulators.
-    static constexpr bool kWide = N < 64;
-    static constexpr int kAccCols = kWide ? 2 * N : N;
+    // The low parts are further columns of the same MMAs, whose time is that of reading the tile.
+    static constexpr int kAccCols = 2 * N;
     static constexpr int kOColumn = 2 * N;                               // two logit buffers, then the accumulators
     static constexpr int kUsedCols = kOColumn + kItems * kAccCols;
     static constexpr int kTmemCols = kUsedCols > 256 ? 512 : kUsedCols > 128 ? 256 : 128;
@@ -635,11 +636,6 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
 #pragma unroll
                         for (int ks = 0; ks < 4; ++ks)
                             tc_mma_f16(acc, v_desc + (uint64_t)((ks * 2048) >> 4), p_desc + (uint64_t)((ks * 256) >> 4), idesc, j > t0 || ks > 0);
-                        if constexpr (!Geo::kWide) {
-#pragma unroll
-                            for (int ks = 0; ks < 4; ++ks)
-                                tc_mma_f16(acc, v_desc + (uint64_t)((ks * 2048) >> 4), p_desc + (uint64_t)((Geo::kPPart + ks * 256) >> 4), idesc, 1u);
-                        }
                         tc_commit(misc + kLatBarEmpty + slot * 8);
                         if (item + 1 == kItems) tc_commit(misc + kLatBarPvDone);
                     }
@@ -771,7 +767,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
 #pragma unroll 1
                         for (int acc = 0; acc < kItems; ++acc) {
 #pragma unroll 1
-                            for (int part = 0; part < (Geo::kWide ? 2 : 1); ++part) {          // high and low columns
+                            for (int part = 0; part < 2; ++part) {          // high and low columns
 #pragma unroll 1
                                 for (int c0 = 0; c0 < kCols; c0 += 16) {
                                     const unsigned at = lanes + Geo::kOColumn + acc * Geo::kAccCols + part * N + col0 + c0;
@@ -872,16 +868,12 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                 const unsigned at = lanes + Geo::kOColumn + acc * Geo::kAccCols + first;
                 float o[16];
                 tc_issue_load16(o, at);
-                if constexpr (Geo::kWide) {
-                    float low[16];
-                    tc_issue_load16(low, at + N);
-                    tc_loaded16(o);
-                    tc_loaded16(low);
+                float low[16];
+                tc_issue_load16(low, at + N);
+                tc_loaded16(o);
+                tc_loaded16(low);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[i] += low[i];
-                } else {
-                    tc_loaded16(o);
-                }
+                for (int i = 0; i < 16; ++i) o[i] += low[i];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float inverse = by_warp[(first + i) * 4];
