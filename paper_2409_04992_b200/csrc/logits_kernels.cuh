@@ -401,7 +401,8 @@ process_logits_kernel(const LogitParams p)
         for (int w = 0; w < kLogitWarps; ++w) top = fmaxf(top, top_by_warp[w]);
 
         // ---- exponentials against the block's own maximum, and their sum; or where the first of the largest is ----
-        const float rate = greedy ? 0.f : fminf(1.44269504088896340736f / temperature, 1e30f);
+        // (finite, so that the largest, 0 times it, keeps the exponent 0 at every temperature)
+        const float rate = greedy ? 0.f : fminf(1.44269504088896340736f / temperature, 3.402823466e38f);
         float sum = 0.f;
         if (greedy) {
             int at = INT32_MAX;
@@ -413,13 +414,15 @@ process_logits_kernel(const LogitParams p)
             }
             if (top > -INFINITY && at != INT32_MAX) atomicMin(first_place + turn, at);
         } else {
-            // (2^(rate z - rate top): one rounding of the exponent, and what rate top is off by is the same factor for all)
-            const float offset = top == -INFINITY ? 0.f : -top * rate;        // (nothing is left: all exponentials are 0)
+            // (The difference first: it is exact near the maximum, so that the blocks' sums join whatever their maxima.  As
+            // 2^(rate z - rate top), in one instruction, the exponents are off by the rounding of rate top, another one in every
+            // block and more than their whole range at small temperatures.)
+            const float from_top = top == -INFINITY ? 0.f : top;              // (nothing is left: all exponentials are 0)
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
-                    z[g][i] = logit_exp2(fmaf(z[g][i], rate, offset));        // (0 where nothing is allowed)
+                    z[g][i] = logit_exp2((z[g][i] - from_top) * rate);      // (0 where nothing is allowed)
                     sum += z[g][i];
                 }
             }
