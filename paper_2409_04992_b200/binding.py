@@ -619,7 +619,8 @@ def process_logits(out: torch.Tensor, logits: torch.Tensor, tokens: Optional[tor
     here = _here(out, logits, tokens, token_lens, prompt_lens, penalties, draft_tokens, mask, tree_lens, bias_tokens, bias_values, allowed,
                  temperatures, status_flags)
     if out.shape != logits.shape or (bias_tokens is None) != (bias_values is None) or \
-            (mask is not None and (mask.dtype != torch.int64 or mask.numel() < batch * tree_tokens * ((tree_tokens + 63) // 64))):
+            (mask is not None and (mask.dtype != torch.int64 or mask.numel() < batch * tree_tokens * ((tree_tokens + 63) // 64) or
+                                  not mask.is_contiguous())):
         raise InstInferError(ERR_INVALID_ARG)
     n = batch * tree_tokens
     for t, dtype, least in ((tokens, torch.int32, batch), (token_lens, torch.int32, batch), (prompt_lens, torch.int32, batch),
