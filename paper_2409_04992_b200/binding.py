@@ -510,7 +510,8 @@ def decode_attention_latent(out: torch.Tensor, lse: Optional[torch.Tensor], q: t
             len(seq_lens) < batch or (tree_lens is not None and len(tree_lens) < batch) or set(map(_type_of, ints)) != {torch.int32} or \
             not all(map(_is_contiguous, (out, q, cache, *ints))) or \
             (lse is not None and (lse.numel() != batch * q_tokens * q_heads or lse.dtype is not torch.float32 or not lse.is_contiguous())) or \
-            (mask is not None and (mask.numel() < batch * q_tokens * ((q_tokens + 63) // 64) or mask.dtype is not torch.int64 or not mask.is_contiguous())):
+            (mask is not None and (mask.shape[1:] != (q_tokens, (q_tokens + 63) // 64) or len(mask) < batch or mask.dtype is not torch.int64 or
+                                  not mask.is_contiguous())):
         raise InstInferError(ERR_INVALID_ARG)
     if block_table is None:
         sequences, s_max, block_tokens, max_blocks, phys = cache_shape[0], cache_shape[1], 0, 0, 0
@@ -619,25 +620,21 @@ def process_logits(out: torch.Tensor, logits: torch.Tensor, tokens: Optional[tor
     here = _here(out, logits, tokens, token_lens, prompt_lens, penalties, draft_tokens, mask, tree_lens, bias_tokens, bias_values, allowed,
                  temperatures, status_flags)
     if out.shape != logits.shape or (bias_tokens is None) != (bias_values is None) or \
-            (mask is not None and (mask.dtype != torch.int64 or mask.numel() < batch * tree_tokens * ((tree_tokens + 63) // 64) or
-                                  not mask.is_contiguous())):
+            (bias_tokens is not None and bias_values.shape != bias_tokens.shape):
         raise InstInferError(ERR_INVALID_ARG)
-    n = batch * tree_tokens
-    for t, dtype, least in ((tokens, torch.int32, batch), (token_lens, torch.int32, batch), (prompt_lens, torch.int32, batch),
-                            (penalties, torch.float32, 3 * batch), (draft_tokens, torch.int32, n), (tree_lens, torch.int32, batch),
-                            (bias_tokens, torch.int32, batch), (allowed, torch.int32, n * ((vocab + 31) // 32)),
-                            (temperatures, torch.float32, batch)):
-        if t is not None and (t.dtype != dtype or t.numel() < least or not t.is_contiguous()):
+    # (what a sequence has of each; None: a list of any length)
+    for t, dtype, each in ((tokens, torch.int32, None), (token_lens, torch.int32, ()), (prompt_lens, torch.int32, ()), (penalties, torch.float32, (3,)),
+                           (draft_tokens, torch.int32, (tree_tokens,)), (mask, torch.int64, (tree_tokens, (tree_tokens + 63) // 64)),
+                           (tree_lens, torch.int32, ()), (bias_tokens, torch.int32, None), (bias_values, torch.float32, None),
+                           (allowed, torch.int32, (tree_tokens, (vocab + 31) // 32)), (temperatures, torch.float32, ())):
+        if t is None:
+            continue
+        shape = t.shape
+        if t.dtype is not dtype or not t.is_contiguous() or (len(shape) != 2 if each is None else shape[1:] != each) or \
+                len(shape) == 0 or shape[0] < batch:
             raise InstInferError(ERR_INVALID_ARG)
-    max_tokens = max_bias = 0
-    if tokens is not None:
-        max_tokens = tokens.shape[1]
-        if tokens.shape[0] < batch:
-            raise InstInferError(ERR_INVALID_ARG)
-    if bias_tokens is not None:
-        max_bias = bias_tokens.shape[1]
-        if bias_tokens.shape[0] < batch or bias_values.shape != bias_tokens.shape or bias_values.dtype != torch.float32 or not bias_values.is_contiguous():
-            raise InstInferError(ERR_INVALID_ARG)
+    max_tokens = tokens.shape[1] if tokens is not None else 0
+    max_bias = bias_tokens.shape[1] if bias_tokens is not None else 0
     if out.dtype not in _TYPES or logits.dtype not in _TYPES:
         raise InstInferError(ERR_UNSUPPORTED)
     _check(load().instinfer_process_logits(
