@@ -383,9 +383,9 @@ _device_of, _type_of, _address_of, _is_contiguous = (torch.Tensor.get_device, to
 
 def _token_stride(shape, strides) -> int:
     """Elements from one token of a tensor [B, N, ...] to the next, all B * N of them evenly spaced."""
-    if shape[1] == 1:
-        # (one token in all: any stride that the library accepts will do)
-        return strides[0] if shape[0] > 1 else 1 << 32
+    if shape[1] <= 1:
+        # (one token in all, or none: any stride that the library accepts will do)
+        return strides[0] if shape[0] > 1 and shape[1] == 1 else 1 << 32
     if shape[0] > 1 and strides[0] != shape[1] * strides[1]:
         raise InstInferError(ERR_INVALID_ARG)
     return strides[1]

@@ -38,3 +38,14 @@ def test_an_empty_history_and_no_biases_are_taken(lib):  # noqa: F811
     empty = dict(tokens=torch.zeros(B, 0, dtype=torch.int32), bias_tokens=torch.zeros(B, 0, dtype=torch.int32), bias_values=torch.zeros(B, 0))
     binding.process_logits(**dict(CALLS["process_logits"](), **empty), stream=STREAM)
     assert lib.args[9] == 0 and lib.args[16] == 0
+
+
+@pytest.mark.parametrize("call", ["rope_append", "latent_append"])
+@pytest.mark.parametrize("batch,tokens", [(B, 0), (0, N), (0, 0), (1, 0)])
+def test_no_new_tokens_are_a_call_without_work(lib, call, batch, tokens):  # noqa: F811
+    args = CALLS[call]()
+    for name in ("q_out", "q", "k_new", "v_new", "q_rope", "latent_new", "rope_new", "positions"):
+        if name in args:
+            args[name] = torch.zeros(batch, tokens, *args[name].shape[2:], dtype=args[name].dtype)
+    getattr(binding, call)(**args, stream=STREAM)
+    assert lib.called == ["instinfer_" + call]
