@@ -301,16 +301,15 @@ latent_pair_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                 latent_prefetch(p, rows, T, (L + kLatentRope) * 2);
                 const Rows of_tile = rows_of(now);
 #pragma unroll 1
-                for (int item = 0; item < kKeyItems; ++item) {
-                    // (one decision for the warp at the tile's end: what a lane does not wait for it does not ask for)
+                for (int item = 0; item < kKeyItems && fine; ++item) {
+                    // (one answer for the warp: a copy has full-warp barriers, and its bytes are announced by one lane for all)
                     const int slot = n % kKSlots;
-                    if (fine && n >= kKSlots) fine = tree_wait(misc + kPairBarKEmpty + slot * 8, (n / kKSlots - 1) & 1);
+                    if (n >= kKSlots) fine = __all_sync(0xffffffffu, tree_wait(misc + kPairBarKEmpty + slot * 8, (n / kKSlots - 1) & 1));
                     if (fine)
                         copy_rows(of_tile, slot * kKeyPanels * kPairPanel, item * kKeyPanels * 64, min(kKeyPanels, kPanels - item * kKeyPanels),
                                   first_misc + kPairBarKFull + slot * 8, false);
                     ++n;
                 }
-                fine = __all_sync(0xffffffffu, fine);
                 if (j > seg.t0 || !fine) continue;
                 after = finder.template next<E, L>(p, lane);
                 fine = announce(after, k + 1);
@@ -346,13 +345,12 @@ latent_pair_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                 }
                 const bool looked_at = start + kPairTile > prefix;
 #pragma unroll 1
-                for (int half = 0; half < 2; ++half) {
-                    if (fine && g > 0) fine = tree_wait(misc + kPairBarPvDone + half * 8, (g - 1) & 1);
+                for (int half = 0; half < 2 && fine; ++half) {
+                    if (g > 0) fine = __all_sync(0xffffffffu, tree_wait(misc + kPairBarPvDone + half * 8, (g - 1) & 1));
                     if (fine)
                         copy_rows(half == 0 ? half0 : half1, Geo::kVOffset + half * Geo::kItemBytes, rank * (L / 2), Geo::kValuePanels,
                                   looked_at ? misc + kPairBarVOwn + half * 8 : first_misc + kPairBarVFull + half * 8, looked_at);
                 }
-                fine = __all_sync(0xffffffffu, fine);
                 if (!looked_at) continue;
                 // The halves land here, and rows that must not meet a weight of 0 are cleared.
 #pragma unroll 1
