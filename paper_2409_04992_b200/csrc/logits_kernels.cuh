@@ -161,7 +161,7 @@ process_logits_kernel(const LogitParams p)
     namespace cg = cooperative_groups;
     constexpr int kGroups = kHeld / kVec;
     using Bits = typename std::conditional<(kHeld > 32), uint64_t, uint32_t>::type;       // one of every held token
-    extern __shared__ unsigned table[];                       // [slice], where there is anything to look up
+    extern __shared__ __align__(16) unsigned table[];         // [slice], where there is anything to look up
     __shared__ float top_by_warp[kLogitWarps], sum_by_warp[kLogitWarps];
     __shared__ LogitShare by_cta[2][kLogitMaxCtas];
     __shared__ uint64_t arrived[2];                           // mbarriers: all blocks' shares of a row are here
