@@ -14,6 +14,6 @@ def test_every_dynamic_array_is_aligned():
         for found in re.finditer(r"extern __shared__ (__align__\((\d+)\) )?[\w ]+ (\w+)\[\];", text):
             seen += 1
             aligned = found.group(2) is not None and int(found.group(2)) >= 16
-            rounded = re.search(r"__cvta_generic_to_shared\(%s\)\);\s*const unsigned base = \(raw \+ \d+u\) & ~\d+u;" % found.group(3), text)
+            rounded = re.search(r"__cvta_generic_to_shared\(%s\)\);\s*const unsigned \w+ = \(raw \+ \d+u\) & ~\d+u;" % found.group(3), text)
             assert aligned or rounded or (path.name, found.group(3)) in ONE_AT_A_TIME, (path.name, found.group(0))
     assert seen >= 12
