@@ -321,8 +321,9 @@ int instinfer_rope_append(void *q_out, void *k_cache, void *v_cache, const void 
  *     out[r] = softmax_i(scale * q[r] . row_i) . row_i[0 .. latent_dim)
  * Layouts: contiguous [batch, s_max, latent_dim + rope_dim], or a pool [num_phys_blocks, block_tokens, latent_dim + rope_dim]
  * with a block table; fp16 or bf16 (`type`, the same for every tensor of a call but lse).
- * The calls that share, grow and move whole blocks (instinfer_kv_fork, instinfer_kv_resize, instinfer_kv_defragment) take such pools
- * as pools of (latent_dim + rope_dim) / 64 heads of 64, half of the layers as K and half as V pools (same block bytes).
+ * The calls that move rows and blocks (instinfer_kv_keep_path, instinfer_kv_fork, instinfer_kv_resize, instinfer_kv_defragment) take
+ * such caches as caches of one head of latent_dim + rope_dim, half of the layers as K and half as V caches; with an odd number
+ * of layers one of them stands in both lists, at the same place (instinfer_kv_keep_path refuses one that stands at two places).
  * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): latent_dim 512, rope_dim 64; paged block_tokens a multiple of 8.
  *
  * instinfer_latent_append: the new tokens' rows, with the key part turned, and the queries' turned parts.
@@ -518,7 +519,9 @@ int instinfer_process_logits(void *out, int32_t out_type, int64_t out_stride, co
  *   new_lens   int32 [batch], a buffer of its own (not seq_lens)
  * Layout selection and the other arguments as in instinfer_kv_append.  A path or tree out of range
  * is flagged (INSTINFER_FLAG_TREE_RANGE, or INSTINFER_FLAG_SEQ_LEN_RANGE for the length), the
- * sequence is left alone and new_lens[b] = seq_lens[b].  n_layers <= INSTINFER_MAX_LAYERS.
+ * sequence is left alone and new_lens[b] = seq_lens[b].
+ * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): n_layers <= INSTINFER_MAX_LAYERS, head_dim in {64, 128, 256}, or a latent
+ * cache's row as one head.
  */
 #define INSTINFER_MAX_LAYERS 128
 int instinfer_kv_keep_path(void *const *k_caches, void *const *v_caches, int32_t n_layers,
@@ -537,7 +540,7 @@ int instinfer_kv_keep_path(void *const *k_caches, void *const *v_caches, int32_t
  * They must not run at the same time on one pool.  Arguments as in instinfer_kv_append, layers'
  * pools as in instinfer_kv_keep_path.
  * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): batch <= 8192, batch * max_blocks_per_seq <= 2^28,
- * n_layers <= INSTINFER_MAX_LAYERS, head_dim in {64, 128, 256}.
+ * n_layers <= INSTINFER_MAX_LAYERS, head_dim in {64, 128, 256} or a latent cache's row as one head.
  *
  * instinfer_kv_fork: sequence dst[i] (empty: length 0) becomes a copy of src[i] that shares all of
  * its blocks, the partly filled last one included; nothing is copied but table entries.

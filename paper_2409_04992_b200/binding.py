@@ -649,7 +649,8 @@ _bytes_of = torch.Tensor.nbytes.__get__
 
 def _layers(here: int, k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor]):
     """The two HOST pointer arrays of the calls that work on all layers at once, and the caches' shape: as many V as K
-    caches, fp16, contiguous, of one size, all on the device `here`."""
+    caches, fp16, contiguous, of one size, all on the device `here`.  (Latent caches [B, s_max, 576] or pools [P, T, 576] come as
+    cache.view(torch.float16).unsqueeze(1), half of the layers as K and half as V caches, an odd one as both of one place.)"""
     n = len(k_caches)
     caches = [*k_caches, *v_caches]
     # (whole passes in C: a model has some hundred caches, and a Python loop over them outlasts the kernel.  One shape

@@ -212,6 +212,12 @@ inline bool append_head_dim_ok(int32_t head_dim) { return head_dim == 64 || head
 // Widths of a latent cache's row that the latent calls take.
 inline bool latent_dims_ok(int32_t latent_dim, int32_t rope_dim) { return latent_dim == 512 && rope_dim == 64; }
 
+// Rows that the calls which move rows and blocks take: those of K and V caches, and a latent cache's as one head.
+inline bool moved_rows_ok(int32_t heads, int32_t head_dim)
+{
+    return append_head_dim_ok(head_dim) || (heads == 1 && latent_dims_ok(head_dim - 64, 64));
+}
+
 inline bool sizes_ok(int32_t batch, int32_t heads, int32_t max_seq_len)
 {
     if (batch < 0 || heads <= 0 || max_seq_len <= 0) return false;

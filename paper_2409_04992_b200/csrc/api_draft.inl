@@ -19,6 +19,16 @@ bool collect_layers(LayerCaches *all, void *const *k, void *const *v, int32_t n_
     return true;
 }
 
+// Whether a cache stands at two places of the lists (K and V of one layer are one place): its rows would be moved by different
+// blocks, one of which reads what another has moved.
+bool listed_twice(const LayerCaches &all, int32_t n_layers)
+{
+    for (int i = 0; i < n_layers; ++i)
+        for (int j = 0; j < i; ++j)
+            if (all.k[i] == all.k[j] || all.k[i] == all.v[j] || all.v[i] == all.k[j] || all.v[i] == all.v[j]) return true;
+    return false;
+}
+
 int launched(cudaError_t err)
 {
     return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? INSTINFER_OK : INSTINFER_ERR_CUDA;
@@ -42,7 +52,7 @@ int pool_shape(int32_t batch, int32_t max_blocks_per_seq, int32_t block_tokens, 
 int layers_shape(int32_t n_layers, int32_t heads, int32_t head_dim)
 {
     if (n_layers <= 0 || heads <= 0 || head_dim <= 0) return INSTINFER_ERR_INVALID_ARG;
-    return n_layers > kMaxLayers || !append_head_dim_ok(head_dim) ? INSTINFER_ERR_UNSUPPORTED : INSTINFER_OK;
+    return n_layers > kMaxLayers || !moved_rows_ok(heads, head_dim) ? INSTINFER_ERR_UNSUPPORTED : INSTINFER_OK;
 }
 
 int tree_shape(int32_t batch, int32_t tree_tokens)
@@ -146,6 +156,8 @@ int instinfer_kv_keep_path(void *const *k_caches, void *const *v_caches, int32_t
     if (path == nullptr || path_lens == nullptr || seq_lens == nullptr || new_lens == nullptr || new_lens == seq_lens ||
         !collect_layers(&caches, k_caches, v_caches, n_layers))
         return INSTINFER_ERR_INVALID_ARG;
+    // (layers of K and V caches are no pairs of one cache; latent ones may be, so that their lists are looked at)
+    if (!append_head_dim_ok(head_dim) && listed_twice(caches, n_layers)) return INSTINFER_ERR_INVALID_ARG;
     KeepPathParams p = {};
     p.path = path;
     p.path_lens = path_lens;
