@@ -355,8 +355,9 @@ int instinfer_latent_append(void *q_out, void *cache, const void *q_rope, const 
  * Rows of new tokens that there are not, rows that see nothing, and all rows of a sequence with seq_lens[b] == 0 are zero
  * with lse = -inf.  A tree_lens[b] out of range or above seq_lens[b] is flagged (INSTINFER_FLAG_TREE_RANGE) and makes the
  * sequence inactive.  What a row does not see never influences it, infinities and NaN in hidden new tokens' rows
- * included; a row that sees a value that is not finite becomes NaN, or, where its logit is -infinity, leaves that
- * token out if it is a new one.  Block-table entries out of range count as rows of zeros (flagged).
+ * included.  A row that sees a token whose values make its logit NaN or +infinity becomes NaN.  A token whose logit is
+ * -infinity counts nothing; the dims in which its vector is infinite may become NaN if it is not one of the new
+ * tokens.  Block-table entries out of range count as rows of zeros (flagged).
  * Limits (INSTINFER_ERR_UNSUPPORTED otherwise): q_tokens <= INSTINFER_MAX_TREE_TOKENS, q_tokens * q_heads <=
  * INSTINFER_MAX_LATENT_ROWS, caches of fewer than 2^31 rows.
  */

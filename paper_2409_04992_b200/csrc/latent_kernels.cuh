@@ -798,7 +798,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                 if (masked) {
                     // Value rows behind the sequence get weight 0 but may hold anything, and 0 x NaN is NaN: they are
                     // cleared.  So are new tokens' rows that are not finite: a row that sees one has a logit that is
-                    // not finite (its values are part of its key), which makes the row NaN without them.
+                    // not finite (its values are part of its key), which makes the row NaN, or leaves the token out, without them.
                     // A row is L / 8 chunks of 16 bytes, a lane's are those of panel lane / 8 and of the panel four further on.
                     const int first = quarter * 16 + group * (16 / Geo::kGroups), last = first + 16 / Geo::kGroups;
                     if (start + last > prefix) {
