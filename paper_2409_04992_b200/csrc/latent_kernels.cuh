@@ -29,7 +29,7 @@
 //                            memory, copies tiles (64-dim panels by tensor-map copies, 128-byte swizzle) and query rows;
 //   logit and output issuer  one elected thread each issues the MMAs.  An item (128 dims of the tile) goes back to the producer as
 //                            soon as its accumulator's MMAs are complete, the turned part after the logits'.
-// A thread of the softmax warps has two tokens and a quarter of its group's rows (the 16-lane shape of the tensor-memory
+// A thread of the softmax warps has two tokens and a quarter of the rows (the 16-lane shape of the tensor-memory
 // load: 64 tokens fill 16 lanes of every warp's 32).  References are logits before the scale and follow the maximum
 // lazily, weights enter the second product as 16-bit high and low parts, and sums are 32-bit: as in tree_umma_tokens.cuh,
 // which has the reasons.
@@ -105,9 +105,7 @@ struct LatentGeometry {
     static constexpr int kQPanel = N * 128;
     static constexpr int kQBytes = (kPanels + 1) * kQPanel;
     static constexpr int kPPart = N * kLatentTile * 2;                   // weights of a tile: high parts, then low parts
-    static constexpr int kGroups = 1;
-    static constexpr int kCols = N / kGroups;                            // rows of a group of softmax warps
-    static constexpr int kThreads = (4 * kGroups + 3) * 32;
+    static constexpr int kThreads = (4 + 3) * 32;
     static constexpr int kExtraBytes = kLatMiscBytes + N * 20;           // a row's numbers by warp, and its reference
     static constexpr int kRoom = 226 * 1024 - kQBytes - 2 * kPPart - kExtraBytes;
     static constexpr int kTiles = kRoom / (kItems * kLatentItem + kLatentPanel);     // whole tiles that fit
@@ -371,8 +369,8 @@ __global__ void __launch_bounds__(LatentGeometry<L, N>::kThreads, 1)
 latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_cache)
 {
     using Geo = LatentGeometry<L, N>;
-    constexpr int kItems = Geo::kItems, kPanels = Geo::kPanels, kSlots = Geo::kSlots, kRopeSlots = Geo::kRopeSlots, kCols = Geo::kCols;
-    constexpr int kSoftmaxWarps = 4 * Geo::kGroups;
+    constexpr int kItems = Geo::kItems, kPanels = Geo::kPanels, kSlots = Geo::kSlots, kRopeSlots = Geo::kRopeSlots;
+    constexpr int kSoftmaxWarps = 4;
     constexpr int kWarpCopy = kSoftmaxWarps, kWarpLogits = kWarpCopy + 1, kWarpOutput = kWarpCopy + 2;
     constexpr unsigned kTypes = std::is_same<E, __half>::value ? 0u : 1u << 7 | 1u << 10;      // of A and B in the instruction descriptor
     extern __shared__ unsigned char smem_raw[];
@@ -646,26 +644,25 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
         if (!fine && lane == 0 && p.status) atomicOr(p.status, kFlagCopyTimeout);
     } else {
         // ================================ softmax and epilogue ================================
-        const int group = warp >> 2, quarter = warp & 3;              // this warp's rows: [col0, col0 + kCols), its tokens: 16 of the tile
-        const int col0 = group * kCols, vote_id = 1 + 2 * group, sync_id = 2 + 2 * group;
+        const int quarter = warp;                                     // this warp's tokens: 16 of the tile
         const int t = threadIdx.x & 127;
         const int token = quarter * 16 + (lane >> 2), column = 2 * (lane & 3);        // this thread's tokens: token, token + 8
         const unsigned lanes = tmem + ((unsigned)(quarter * 32) << 16);
-        constexpr int kPer = kCols / 8;                               // pairs of columns of a thread
+        constexpr int kPer = N / 8;                                   // pairs of columns of a thread
         float *by_warp = reinterpret_cast<float *>(misc_ptr + kLatMiscBytes);        // [N][4]: a row's maxima, or sums, by warp
         float *offsets = by_warp + N * 4;                             // [N]: the rows' references (negated) as they were last moved
         const float scale = p.scale_log2e, sign = copysignf(1.f, scale), heads_inverse = 1.f / (float)p.q_heads;
         bool fine = true;
         int g = 0;
         for (int k = 0;; ++k) {
-            // (one decision for the group: its barriers have to stay in step)
-            if (group_any(vote_id, !wait_segment(k) || !fine)) {
+            // (one decision for all: their barriers have to stay in step)
+            if (group_any(1, !wait_segment(k) || !fine)) {
                 fine = false;
                 break;
             }
             const LatentSegment &seg = entry(k);
             if (seg.b < 0) break;
-            const int len = seg.len, nodes = seg.nodes, prefix = seg.prefix(), t0 = seg.t0, t1 = seg.t1, row0 = seg.row0 + col0;
+            const int len = seg.len, nodes = seg.nodes, prefix = seg.prefix(), t0 = seg.t0, t1 = seg.t1, row0 = seg.row0;
             // [pair of columns][one of the pair]: the negated reference, a logit before the scale; sums of this thread's tokens
             float2 offset[kPer], l[kPer];
 #pragma unroll
@@ -675,7 +672,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
             }
             for (int j = t0; j < t1; ++j, ++g) {
                 const int buf = g & 1, start = j * kLatentTile;
-                const unsigned logits = lanes + buf * N + col0;
+                const unsigned logits = lanes + buf * N;
                 const bool masked = start + kLatentTile > prefix;     // uniform
                 unsigned hidden = 0;                                  // bit 4 i + 2 u + c: column c of pair i does not see token u
                 if (masked) {
@@ -715,7 +712,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                         most = max3(most, e[i], e[i + 1]);
                         most_odd = max3(most_odd, e[i + 2], e[i + 3]);
                     }
-                    if (attempt > 0 || !group_any(vote_id, fmaxf(most, most_odd) > kGroupLag)) break;
+                    if (attempt > 0 || !group_any(1, fmaxf(most, most_odd) > kGroupLag)) break;
                     // ---- some row's reference moves (rare after a segment's first tile) ----
                     if (j > t0) {                                     // the accumulators hold the tiles before this one
                         if (fine) fine = tree_wait(misc + kLatBarPvDone, (g - 1) & 1);
@@ -732,16 +729,16 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                             top[c] = fmaxf(a, b);
 #pragma unroll
                             for (int o = 4; o < 32; o <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], o));
-                            if (lane < 4) by_warp[(col0 + 8 * i + column + c) * 4 + quarter] = top[c];
+                            if (lane < 4) by_warp[(8 * i + column + c) * 4 + quarter] = top[c];
                         }
                     }
-                    group_sync(sync_id);
+                    group_sync(2);
                     float2 alpha[kPer];                               // 2^(old - new reference)
 #pragma unroll
                     for (int i = 0; i < kPer; ++i) {
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            const float4 tops = *reinterpret_cast<const float4 *>(by_warp + (col0 + 8 * i + column + c) * 4);
+                            const float4 tops = *reinterpret_cast<const float4 *>(by_warp + (8 * i + column + c) * 4);
                             const float top = max3(fmaxf(tops.x, tops.y), tops.z, tops.w);
                             float &off = c ? offset[i].y : offset[i].x, &sum = c ? l[i].y : l[i].x, &factor = c ? alpha[i].y : alpha[i].x;
                             factor = 1.f;
@@ -749,38 +746,38 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                             if (rise > kGroupLag) {
                                 factor = fast_exp2(-rise);
                                 off = moved;
-                                if (quarter == 0 && lane < 4) offsets[col0 + 8 * i + column + c] = off;
+                                if (quarter == 0 && lane < 4) offsets[8 * i + column + c] = off;
                             }
                             sum *= factor;
                         }
                     }
-                    group_sync(sync_id);                              // the maxima have been read
+                    group_sync(2);                                    // the maxima have been read
                     if (j > t0) {
                         if (quarter == 0 && lane < 4) {
 #pragma unroll
                             for (int i = 0; i < kPer; ++i) {
-                                by_warp[(col0 + 8 * i + column) * 4] = alpha[i].x;
-                                by_warp[(col0 + 8 * i + column + 1) * 4] = alpha[i].y;
+                                by_warp[(8 * i + column) * 4] = alpha[i].x;
+                                by_warp[(8 * i + column + 1) * 4] = alpha[i].y;
                             }
                         }
-                        group_sync(sync_id);
+                        group_sync(2);
 #pragma unroll 1
                         for (int acc = 0; acc < kItems; ++acc) {
 #pragma unroll 1
                             for (int part = 0; part < 2; ++part) {          // high and low columns
 #pragma unroll 1
-                                for (int c0 = 0; c0 < kCols; c0 += 16) {
-                                    const unsigned at = lanes + Geo::kOColumn + acc * Geo::kAccCols + part * N + col0 + c0;
+                                for (int c0 = 0; c0 < N; c0 += 16) {
+                                    const unsigned at = lanes + Geo::kOColumn + acc * Geo::kAccCols + part * N + c0;
                                     float o[16];
                                     tc_issue_load16(o, at);
                                     tc_loaded16(o);
 #pragma unroll
-                                    for (int c = 0; c < 16; ++c) o[c] *= by_warp[(col0 + c0 + c) * 4];
+                                    for (int c = 0; c < 16; ++c) o[c] *= by_warp[(c0 + c) * 4];
                                     tc_store16(at, o);
                                 }
                             }
                         }
-                        group_sync(sync_id);                          // the factors have been read
+                        group_sync(2);                                // the factors have been read
                     }
                     tc_issue_load_16lanes(x, logits);
                 }
@@ -800,7 +797,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                     // cleared.  So are new tokens' rows that are not finite: a row that sees one has a logit that is
                     // not finite (its values are part of its key), which makes the row NaN, or leaves the token out, without them.
                     // A row is L / 8 chunks of 16 bytes, a lane's are those of panel lane / 8 and of the panel four further on.
-                    const int first = quarter * 16 + group * (16 / Geo::kGroups), last = first + 16 / Geo::kGroups;
+                    const int first = quarter * 16, last = first + 16;
                     if (start + last > prefix) {
                         // (the logits have read the tile: it has landed)
                         const int item = g * kItems + min(lane, kItems - 1);
@@ -824,7 +821,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                     }
                 }
                 // Lane i has the address of token row i % 8 of block i / 8: tokens 0-7 and 8-15 of two blocks of 8 columns.
-                const unsigned to = p_smem + (col0 / 8 + (lane >> 4)) * 1024 + (quarter * 16 + (lane >> 3 & 1) * 8 + (lane & 7)) * 16;
+                const unsigned to = p_smem + (lane >> 4) * 1024 + (quarter * 16 + (lane >> 3 & 1) * 8 + (lane & 7)) * 16;
 #pragma unroll
                 for (int i = 0; i < kPer; i += 2) {
                     store_matrices(to + i * 1024, hi[2 * i], hi[2 * i + 1], hi[2 * i + 2], hi[2 * i + 3]);
@@ -843,14 +840,14 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                     float sum = c ? l[i].y : l[i].x;
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                    if (lane < 4) by_warp[(col0 + 8 * i + column + c) * 4 + quarter] = sum;
+                    if (lane < 4) by_warp[(8 * i + column + c) * 4 + quarter] = sum;
                 }
             }
-            group_sync(sync_id);
+            group_sync(2);
             const bool whole = seg.whole();
-            if (t < kCols) {
+            if (t < N) {
                 // one thread per row: its sum's inverse (0: a row of zeros) and its log-sum-exp
-                const int r = col0 + t;
+                const int r = t;
                 const float4 sums = *reinterpret_cast<const float4 *>(by_warp + r * 4);
                 const float total = (sums.x + sums.y) + (sums.z + sums.w);
                 const bool empty = r >= seg.rows || (seg.row0 + r) / p.q_heads >= nodes || total == 0.f;     // (a NaN sum is not an empty row's)
@@ -861,10 +858,10 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
             if (fine) fine = tree_wait(misc + kLatBarPvDone, (g - 1) & 1);
             fine = __all_sync(0xffffffffu, fine);
             tc_fence_after();
-            group_sync(sync_id);
+            group_sync(2);
 #pragma unroll 1
-            for (int block = 0; block < kCols / 16 * kItems; ++block) {
-                const int first = col0 + block / kItems * 16, acc = block % kItems, d = acc * 128 + t;
+            for (int block = 0; block < N / 16 * kItems; ++block) {
+                const int first = block / kItems * 16, acc = block % kItems, d = acc * 128 + t;
                 const unsigned at = lanes + Geo::kOColumn + acc * Geo::kAccCols + first;
                 float o[16];
                 tc_issue_load16(o, at);
@@ -894,7 +891,7 @@ latent_attn_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                 __syncwarp();
             }
             tc_fence_before();                                        // the accumulators have been read: the next tile may overwrite them
-            group_sync(sync_id);                                      // so have the rows' numbers
+            group_sync(2);                                            // so have the rows' numbers
             done_segment(k);
         }
         if (!fine && lane == 0 && p.status) atomicOr(p.status, kFlagCopyTimeout);

@@ -358,17 +358,13 @@ latent_pair_kernel(const __grid_constant__ LatentParams p, const __grid_constant
                     fine = __all_sync(0xffffffffu, tree_wait(misc + kPairBarVOwn + half * 8, own >> half & 1u));
                     if (!fine) break;
                     own ^= 1u << half;
-                    constexpr int kLanes = 8 * Geo::kValuePanels, kAtOnce = 32 / kLanes;      // lanes of a row, rows of a round
-                    const int first = start + half * 64, of_row = lane / kLanes;               // row r of the half is position first + r
-                    unsigned char *chunk = smem + Geo::kVOffset + half * Geo::kItemBytes + (lane % kLanes >> 3) * kPairPanel + of_row * 128 + (lane & 7) * 16;
-                    const unsigned mine = kAtOnce == 1 ? ~0u : 0xffffu << (16 * of_row);       // the row's lanes
+                    static_assert(8 * Geo::kValuePanels == 32, "a lane has one chunk of a row");
+                    const int first = start + half * 64;                   // row r of the half is position first + r
+                    unsigned char *chunk = smem + Geo::kVOffset + half * Geo::kItemBytes + (lane >> 3) * kPairPanel + (lane & 7) * 16;
 #pragma unroll 1
-                    for (int r = max(0, (prefix - first) & ~(kAtOnce - 1)); r < 64; r += kAtOnce) {
-                        const int pos = first + r + of_row;
+                    for (int r = max(0, prefix - first); r < 64; ++r) {
                         uint4 *at = reinterpret_cast<uint4 *>(chunk + r * 128);
-                        bool clear = pos >= len;
-                        if (first + r < len) clear = clear || (__ballot_sync(0xffffffffu, !latent_finite8<E>(*at) && pos >= prefix) & mine) != 0;
-                        if (clear) *at = make_uint4(0u, 0u, 0u, 0u);
+                        if (first + r >= len || __any_sync(0xffffffffu, !latent_finite8<E>(*at))) *at = make_uint4(0u, 0u, 0u, 0u);
                     }
                     fence_async_proxy();
                     __syncwarp();
