@@ -32,6 +32,8 @@ bool stride_ok(int64_t stride, int64_t least, int32_t element_bytes)
     return stride >= least && stride < (int64_t)1 << 40 && stride * element_bytes % 16 == 0;
 }
 
+bool frequencies_ok(const double *frequencies) { return frequencies != nullptr && (reinterpret_cast<uintptr_t>(frequencies) & 7u) == 0; }
+
 template <typename In, typename Out, bool kLatent>
 int launch_rope(RopeParams p, bool interleaved, cudaStream_t stream)
 {
@@ -101,7 +103,7 @@ int instinfer_rope_append(void *q_out, void *k_cache, void *v_cache, const void 
         !stride_ok(v_stride, (int64_t)kv_heads * head_dim, bytes))
         return INSTINFER_ERR_INVALID_ARG;
     if (batch == 0 || max_new == 0) return INSTINFER_OK;
-    if (!usable(k_cache) || !usable(v_cache) || !usable(k_new) || !usable(v_new) || frequencies == nullptr || seq_lens == nullptr ||
+    if (!usable(k_cache) || !usable(v_cache) || !usable(k_new) || !usable(v_new) || !frequencies_ok(frequencies) || seq_lens == nullptr ||
         (q_heads > 0 && (!usable(q) || !usable(q_out))))
         return INSTINFER_ERR_INVALID_ARG;
     RopeParams p = {};
@@ -158,7 +160,7 @@ int instinfer_latent_append(void *q_out, void *cache, const void *q_rope, const 
         !stride_ok(latent_stride, latent_dim, 2) || !stride_ok(rope_stride, rope_dim, 2))
         return INSTINFER_ERR_INVALID_ARG;
     if (batch == 0 || max_new == 0) return INSTINFER_OK;
-    if (!usable(cache) || !usable(latent_new) || !usable(rope_new) || frequencies == nullptr || seq_lens == nullptr ||
+    if (!usable(cache) || !usable(latent_new) || !usable(rope_new) || !frequencies_ok(frequencies) || seq_lens == nullptr ||
         (q_heads > 0 && (!usable(q_rope) || !usable(q_out))))
         return INSTINFER_ERR_INVALID_ARG;
     RopeParams p = {};
