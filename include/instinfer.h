@@ -330,6 +330,7 @@ int instinfer_rope_append(void *q_out, void *k_cache, void *v_cache, const void 
  *   q_out      [batch, max_new, q_heads, latent_dim + rope_dim], the absorbed queries: the last rope_dim values of the rows of
  *              tokens that there are get written, nothing else
  *   q_rope     the queries' parts to turn, token (b, t) and head h at (b * max_new + t) * q_stride + h * q_head_stride elements
+ *              (token after token or head after head; they must not overlap)
  *   latent_new, rope_new  token (b, t) at (b * max_new + t) * stride elements; strides are multiples of 16 bytes
  * frequencies [rope_dim / 2] and all else as in instinfer_rope_append.
  */

@@ -32,6 +32,13 @@ bool stride_ok(int64_t stride, int64_t least, int32_t element_bytes)
     return stride >= least && stride < (int64_t)1 << 40 && stride * element_bytes % 16 == 0;
 }
 
+// Parts of `dims` values, of tokens q_stride and of heads q_head_stride apart, do not overlap: a token's heads lie before the next
+// token's, or a head's tokens before the next head's.
+bool parts_apart(int64_t q_stride, int64_t q_head_stride, int64_t tokens, int64_t heads, int64_t dims)
+{
+    return heads - 1 <= (q_stride - dims) / q_head_stride || tokens - 1 <= (q_head_stride - dims) / q_stride;
+}
+
 bool frequencies_ok(const double *frequencies) { return frequencies != nullptr && (reinterpret_cast<uintptr_t>(frequencies) & 7u) == 0; }
 
 template <typename In, typename Out, bool kLatent>
@@ -156,7 +163,8 @@ int instinfer_latent_append(void *q_out, void *cache, const void *q_rope, const 
     if (rc != INSTINFER_OK) return rc;
     if (!latent_dims_ok(latent_dim, rope_dim) || (type != INSTINFER_F16 && type != INSTINFER_BF16)) return INSTINFER_ERR_UNSUPPORTED;
     if (q_heads > 1 << 20) return INSTINFER_ERR_INVALID_ARG;
-    if ((q_heads > 0 && (!stride_ok(q_head_stride, rope_dim, 2) || !stride_ok(q_stride, (q_heads - 1) * q_head_stride + rope_dim, 2))) ||
+    if ((q_heads > 0 && (!stride_ok(q_head_stride, rope_dim, 2) || !stride_ok(q_stride, rope_dim, 2) ||
+                         !parts_apart(q_stride, q_head_stride, (int64_t)batch * max_new, q_heads, rope_dim))) ||
         !stride_ok(latent_stride, latent_dim, 2) || !stride_ok(rope_stride, rope_dim, 2))
         return INSTINFER_ERR_INVALID_ARG;
     if (batch == 0 || max_new == 0) return INSTINFER_OK;
