@@ -203,6 +203,10 @@ process_logits_kernel(const LogitParams p)
         const int here = max(0, min(p.slice, p.vocab - first));
         const E *from = static_cast<const E *>(p.logits) + row * p.row_stride + first;
         auto place = [&](int g) -> int { return (g * kLogitThreads + threadIdx.x) * kVec; };
+        // Whether n places from `at` on are the row's, and the block's (looked at in the bounds-checking build only).
+        auto inside = [&](int at, int n) -> bool {
+            return bounds_ok(at >= 0 && at + n <= p.slice && first + at >= 0 && first + at + n <= p.vocab, p.status);
+        };
         // Places [lead, here) are the row's; a group of kVec places may stick out at either end.
         const int lead = rank == 0 ? shift : 0, last = here - kVec;
         const bool ragged = lead != 0 || here % kVec != 0;    // (the same for the block: what sticks out is kept out of the loops over all)
@@ -221,7 +225,7 @@ process_logits_kernel(const LogitParams p)
         for (int g = 0; g < kGroups; ++g) {
             const int at = place(g);
             raw[g].nothing();
-            if (at >= lead && at <= last) raw[g].word = *reinterpret_cast<const typename LogitRaw<E, kVec>::Word *>(from + at);
+            if (at >= lead && at <= last && inside(at, kVec)) raw[g].word = *reinterpret_cast<const typename LogitRaw<E, kVec>::Word *>(from + at);
         }
         Bits may = 0;                                         // bit g * kVec + i: the token is allowed
         if (p.allowed) {
@@ -248,7 +252,7 @@ process_logits_kernel(const LogitParams p)
                 const int at = place(g);
 #pragma unroll
                 for (int i = 0; i < kVec; ++i)
-                    if (!(at >= lead && at <= last) && at + i < here && at + i >= lead) z[g][i] = logit_value(from[at + i]);
+                    if (!(at >= lead && at <= last) && at + i < here && at + i >= lead && inside(at + i, 1)) z[g][i] = logit_value(from[at + i]);
             }
         }
 
@@ -262,7 +266,7 @@ process_logits_kernel(const LogitParams p)
                     return -1;
                 }
                 const int at = which - first;
-                if (at < 0 || at >= here) return -1;
+                if (at < 0 || at >= here || !inside(at, 1)) return -1;
                 if (count) atomicAdd(table + at, what);
                 else atomicOr(table + at, what);
                 return at;
@@ -369,7 +373,7 @@ process_logits_kernel(const LogitParams p)
                 const int at = place(g);
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) z[g][i] *= times;
-                if (at >= lead && at <= last) logit_store<Out, kVec>(out + at, z[g]);
+                if (at >= lead && at <= last && inside(at, kVec)) logit_store<Out, kVec>(out + at, z[g]);
             }
             if (ragged) {
 #pragma unroll
@@ -377,7 +381,7 @@ process_logits_kernel(const LogitParams p)
                     const int at = place(g);
 #pragma unroll
                     for (int i = 0; i < kVec; ++i)
-                        if (!(at >= lead && at <= last) && at + i < here && at + i >= lead) logit_store_one(p.out, type, to + at + i, z[g][i]);
+                        if (!(at >= lead && at <= last) && at + i < here && at + i >= lead && inside(at + i, 1)) logit_store_one(p.out, type, to + at + i, z[g][i]);
                 }
             }
         };
