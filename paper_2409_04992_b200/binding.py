@@ -569,6 +569,7 @@ def decode_attention_tree(out: torch.Tensor, lse: Optional[torch.Tensor], q: tor
 
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_INT32, _FLOAT32 = {torch.int32}, {torch.float32}
 
 
 def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.Tensor,
@@ -596,11 +597,12 @@ def verify_tree(path: torch.Tensor, path_lens: torch.Tensor, out_tokens: torch.T
         uniforms.data_ptr(), batch, tree_tokens, vocab, _ptr(status_flags), _stream(stream, here)))
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    """Elements from one row of t [B, T, V] to the next, all B * T of them evenly spaced (a padded vocabulary sliced to V will do)."""
-    batch, rows, vocab = t.shape
-    stride = t.stride(1) if rows > 1 else t.stride(0) if batch > 1 else (vocab + 3) // 4 * 4
-    if (vocab > 1 and t.stride(2) != 1) or (batch > 1 and t.stride(0) != rows * stride):
+def _row_stride(strides, batch: int, rows: int, vocab: int) -> int:
+    """Elements from one row of a tensor [batch, rows, vocab] to the next, all evenly spaced (a padded vocabulary sliced to V will do)."""
+    far, stride, near = strides
+    if rows == 1:
+        stride = far if batch > 1 else (vocab + 3) // 4 * 4
+    if (vocab > 1 and near != 1) or (batch > 1 and far != rows * stride):
         raise InstInferError(ERR_INVALID_ARG)
     return stride
 
@@ -616,30 +618,39 @@ def process_logits(out: torch.Tensor, logits: torch.Tensor, tokens: Optional[tor
     """instinfer_process_logits: logits and out [B, T, V] in fp32, fp16 or bf16; tokens [B, M], token_lens and prompt_lens [B];
     penalties fp32 [B, 3]; draft_tokens [B, T] with mask as tree_mask writes it; bias_tokens and bias_values [B, n]; allowed
     int32 [B, T, ceil(V / 32)] (the bits of the header's uint32 words); temperatures fp32 [B]."""
-    batch, tree_tokens, vocab = logits.shape
+    shape = logits.shape
+    batch, tree_tokens, vocab = shape
     here = _here(out, logits, tokens, token_lens, prompt_lens, penalties, draft_tokens, mask, tree_lens, bias_tokens, bias_values, allowed,
                  temperatures, status_flags)
-    if out.shape != logits.shape or (bias_tokens is None) != (bias_values is None) or \
-            (bias_tokens is not None and bias_values.shape != bias_tokens.shape):
+    ints = [t for t in (tokens, token_lens, prompt_lens, draft_tokens, tree_lens, bias_tokens, allowed) if t is not None]
+    floats = [t for t in (penalties, bias_values, temperatures) if t is not None]
+    if out.shape != shape or (bias_tokens is None) != (bias_values is None) or \
+            not set(map(_type_of, ints)) <= _INT32 or not set(map(_type_of, floats)) <= _FLOAT32 or \
+            not all(map(_is_contiguous, (*ints, *floats))) or (mask is not None and (mask.dtype is not torch.int64 or not mask.is_contiguous())):
         raise InstInferError(ERR_INVALID_ARG)
-    # (what a sequence has of each; None: a list of any length)
-    for t, dtype, each in ((tokens, torch.int32, None), (token_lens, torch.int32, ()), (prompt_lens, torch.int32, ()), (penalties, torch.float32, (3,)),
-                           (draft_tokens, torch.int32, (tree_tokens,)), (mask, torch.int64, (tree_tokens, (tree_tokens + 63) // 64)),
-                           (tree_lens, torch.int32, ()), (bias_tokens, torch.int32, None), (bias_values, torch.float32, None),
-                           (allowed, torch.int32, (tree_tokens, (vocab + 31) // 32)), (temperatures, torch.float32, ())):
-        if t is None:
-            continue
-        shape = t.shape
-        if t.dtype is not dtype or not t.is_contiguous() or (len(shape) != 2 if each is None else shape[1:] != each) or \
-                len(shape) == 0 or shape[0] < batch:
+    each = (batch,)
+    for t, rows in ((token_lens, each), (prompt_lens, each), (tree_lens, each), (temperatures, each), (penalties, (batch, 3)),
+                    (draft_tokens, (batch, tree_tokens)), (mask, (batch, tree_tokens, (tree_tokens + 63) // 64)),
+                    (allowed, (batch, tree_tokens, (vocab + 31) // 32))):
+        # (more sequences than the batch has will do)
+        if t is not None and t.shape != rows and (t.shape[1:] != rows[1:] or t.dim() == 0 or len(t) < batch):
             raise InstInferError(ERR_INVALID_ARG)
-    max_tokens = tokens.shape[1] if tokens is not None else 0
-    max_bias = bias_tokens.shape[1] if bias_tokens is not None else 0
+    max_tokens = max_bias = 0
+    if tokens is not None:
+        listed = tokens.shape
+        if len(listed) != 2 or listed[0] < batch:
+            raise InstInferError(ERR_INVALID_ARG)
+        max_tokens = listed[1]
+    if bias_tokens is not None:
+        listed = bias_tokens.shape
+        if len(listed) != 2 or listed[0] < batch or bias_values.shape != listed:
+            raise InstInferError(ERR_INVALID_ARG)
+        max_bias = listed[1]
     if out.dtype not in _TYPES or logits.dtype not in _TYPES:
         raise InstInferError(ERR_UNSUPPORTED)
     _check(load().instinfer_process_logits(
-        out.data_ptr(), _TYPES[out.dtype], _row_stride(out), logits.data_ptr(), _TYPES[logits.dtype], _row_stride(logits), _ptr(tokens),
-        _ptr(token_lens), _ptr(prompt_lens), max_tokens, _ptr(penalties), _ptr(draft_tokens), _ptr(mask), _ptr(tree_lens),
+        out.data_ptr(), _TYPES[out.dtype], _row_stride(out.stride(), *shape), logits.data_ptr(), _TYPES[logits.dtype],
+        _row_stride(logits.stride(), *shape), _ptr(tokens), _ptr(token_lens), _ptr(prompt_lens), max_tokens, _ptr(penalties), _ptr(draft_tokens), _ptr(mask), _ptr(tree_lens),
         _ptr(bias_tokens), _ptr(bias_values), max_bias, _ptr(allowed), _ptr(temperatures), int(probabilities), batch, tree_tokens, vocab,
         _ptr(status_flags), _stream(stream, here)))
 
