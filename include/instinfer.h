@@ -276,7 +276,7 @@ size_t instinfer_grouped_workspace_bytes(int32_t batch, int32_t q_tokens, int32_
  *             trained_len tokens keep f_i, those that turn at most slow_turns times get f_i / factor, between them linearly
  *             (in the number of turns); magnitude 0.1 ln(factor) + 1
  * factor >= 1; trained_len > 0 and 0 <= slow_turns < fast_turns are looked at for "by parts" only.
- * rope_dim even; an unknown scaling: INSTINFER_ERR_UNSUPPORTED.
+ * rope_dim is positive and even.  An unknown scaling: INSTINFER_ERR_UNSUPPORTED.
  */
 #define INSTINFER_ROPE_PLAIN 0
 #define INSTINFER_ROPE_LINEAR 1

@@ -17,8 +17,10 @@
 // The grid is as many clusters as the GPU holds at once, each with a run of consecutive rows, and rows of one tree share the
 // table but for their own drafts.  Logits are asked for without a branch between the loads, and what sticks out of a row at
 // its ends is kept out of the loops over all of it.  Measured: one row of 32,000 fp32 5.8 us; 192 rows of 50,257 bf16 with
-// everything on 77 us and 512 rows of 131,072 in trees 270 us, six to eight times what their bytes take: some thirty
-// instructions a logit, and two blocks of 512 threads per SM that wait together at each of a row's steps.
+// everything on 65 to 76 us and 512 rows of 131,072 in trees 251 to 262 us, six to eight times what their bytes take.  The softmax
+// alone is 38 and 163 us of them: two blocks of 512 threads per SM wait together at each of a row's steps with nothing of the
+// next row under way, and leave a thread 64 registers, so that the instance with 32 logits a thread spills (234 bytes of stores
+// and 306 of loads).  History and drafts add 20 and 75 us, biases 4, the grammar 3 and 15.
 #pragma once
 
 #include <cooperative_groups.h>
